@@ -345,6 +345,202 @@ size_t biq_noalloc_scratch_bytes(void);
 biq_status biq_gemm_noalloc(const uint8_t* K, const float* alpha, const float* X, float* Y,
                             int m, int n, int q, int batch, int mu, void* stream);
 
+/* ---- the rest of a decoder step: positions, cache, attention, drafted tokens ---- */
+
+/*
+ * What stands between the projections that biq_gemm computes and the tokens that a model answers with.
+ *
+ * Every operation takes one descriptor (read during the call only), a workspace where it needs one, and a stream.  The
+ * general rules above hold: device pointers of the caller, no allocation, no synchronisation, statuses.  Differences:
+ *   - Elements are 32-bit, bfloat16 or 16-bit floats (biq_type).  Arithmetic is in 32 bits or more whatever the type, and a
+ *     result is rounded once, to the output's type.
+ *   - Infinities and NaN are values like others: they show in the results of the rows that depend on them, and in no others.
+ *   - Rows of a tensor have strides of their own (biq_rows).  Elements of one head are adjacent.  Any alignment of the
+ *     element's size is accepted; 16-byte aligned rows are faster.
+ *   - What device memory says of lengths, pages and positions is not known to the host, and so is not refused: it is bounded
+ *     on the device instead, as each operation describes.  No value of it leads outside the buffers described here.
+ */
+typedef enum { BIQ_F32 = 0, BIQ_BF16 = 1, BIQ_F16 = 2 } biq_type;
+
+/* Rows of heads: element d of head h of row r at data[r * row_stride + h * head_stride + d] (strides in elements). */
+typedef struct {
+    void* data;
+    int64_t row_stride, head_stride;
+} biq_rows;
+
+/*
+ * Rotary positions: pairs of elements of a head are turned by an angle that grows with the token's position,
+ *     (a, b) -> (a c - b s, a s + b c),  c = cos(position * f_i), s = sin(position * f_i).
+ * angles: device float [positions][rot / 2][2], c and s of every position and pair (biq_rotary_table makes it).  rot: how many
+ * elements of a head are turned, its first ones (even, at most head_dim); the others are left as they are.  interleaved: pair i
+ * is elements 2i and 2i + 1, otherwise elements i and i + rot / 2.
+ * The products and the sum of a pair are each rounded to 32 bits (no fused multiply-add).
+ */
+typedef struct {
+    const float* angles;
+    int positions, rot, interleaved;
+} biq_rotation;
+
+/* How the frequencies f_i = base^(-2i / rot) are stretched for contexts longer than trained on. */
+typedef enum {
+    BIQ_ROTARY_PLAIN = 0,
+    BIQ_ROTARY_LINEAR = 1,   /* f_i / factor: positions interpolated                                                     */
+    BIQ_ROTARY_BASE = 2,     /* base * factor^(rot / (rot - 2)): the lowest frequency is divided by factor, the highest kept */
+    BIQ_ROTARY_BY_PARTS = 3  /* f_i / factor where a pair turns less than `slow` times in `trained` tokens, f_i where it
+                                turns more than `fast` times, linear in the turns between them                           */
+} biq_rotary_scaling;
+
+/* HOST: turns[i] = f_i / (2 pi), i < rot / 2, for biq_rotary_table.  factor, trained, slow, fast: see biq_rotary_scaling (the
+ * last three for BIQ_ROTARY_BY_PARTS only).  BIQ_EINVAL: rot odd, below 2 (4 for BIQ_ROTARY_BASE), base <= 1 or not finite,
+ * factor < 1, trained < 1, slow >= fast. */
+biq_status biq_rotary_frequencies(double* turns, int rot, double base, int scaling, double factor, int trained, double slow,
+                                  double fast);
+
+/* angles[p][i] = amplitude * (cos, sin)(2 pi (first + p) turns[i]), p < positions, i < rot / 2; turns device double, angles
+ * device float.  The angle is reduced in 64 bits: exact to 32 bits for every position.  amplitude scales what is turned
+ * (1 for none). */
+biq_status biq_rotary_table(const double* turns, float* angles, int rot, int first, int positions, double amplitude,
+                            void* stream);
+
+/*
+ * y = x turned by the angles of positions[row]; inverse: by the opposite angles, which is the gradient (x, y then hold the
+ * gradients of y and x).  y may be x (same data and strides); otherwise they must not overlap.  A position outside
+ * [0, rotation.positions) makes the turned elements of its row NaN.
+ */
+typedef struct {
+    biq_rows x, y;
+    const int32_t* positions;   /* [rows] */
+    biq_rotation rotation;
+    int type, rows, heads, head_dim, inverse;
+} biq_rotary_args;
+biq_status biq_rotary(const biq_rotary_args* args, void* stream);
+
+/*
+ * A cache of keys and values in 8 bits with one 32-bit scale for each block of BIQ_CACHE_BLOCK tokens and head, for keys and
+ * values apart: a code stands for code * scale.  A block is what the matrix cores take from one lane, so that its scale is one
+ * multiplication of a lane's sums, and small enough that a large token costs few others their precision.
+ *
+ * Tokens lie in pages; page table[s][t / page_tokens] holds token t of sequence s.  With T = page_tokens, H = heads,
+ * D = head_dim, a page of biq_cache_page_bytes() bytes holds
+ *     keys    [H][T / 16][16][D]   codes, token by token
+ *     values  [H][T / 16][D][16]   codes, the 16 tokens of a block adjacent
+ *     scales  float [2][H][T / 16] keys, values
+ * and nothing outside it, so a page is copied by copying its bytes.
+ *
+ * format BIQ_CACHE_INT8: integers in [-127, 127], scale = (largest magnitude of the block) / 127, codes rounded to nearest, ties
+ * to even.  BIQ_CACHE_FP8: 8-bit floats with 4 exponent and 3 fraction bits (OCP E4M3), scale = the least power of two that
+ * makes every magnitude at most 448; rounded to nearest, ties to even.  Integers have the smaller mean error (0.9 % of the
+ * standard deviation for normal values, floats 2.5 %), floats keep small channels beside large ones.
+ *
+ * Tokens of a block that came earlier are written anew where a later one needs a larger scale (a block's scale never falls
+ * until its first token is written again): codes become rn(code * (old scale / new scale)).  Blocks whose largest magnitude is
+ * below 2^-100 are held as zeros.  A block that gets an infinity or a NaN stands for NaN altogether (scale NaN), until its
+ * first token is written again.
+ *
+ * lens[s]: tokens of sequence s, those of the call included; taken as at least 0 and at most table_stride * page_tokens.  A
+ * sequence is cut back by lowering its length.  A page number outside [0, num_pages) has no tokens: nothing is written to it,
+ * and attention does not see them.  No page may hold tokens of two sequences that are written in one call.
+ * page_tokens: a multiple of 16 up to 256; head_dim: a multiple of 16 up to 256; else BIQ_EUNSUPPORTED.
+ */
+#define BIQ_CACHE_BLOCK 16
+typedef enum { BIQ_CACHE_INT8 = 0, BIQ_CACHE_FP8 = 1 } biq_cache_format;
+typedef struct {
+    void* store;            /* uint8 [num_pages][biq_cache_page_bytes()], 16-byte aligned */
+    const int32_t* table;   /* [seqs][table_stride] page numbers */
+    const int32_t* lens;    /* [seqs] */
+    int num_pages, page_tokens, table_stride, seqs, heads, head_dim, format;
+} biq_cache;
+
+/* Bytes of a page, a multiple of 128 (0 on invalid arguments). */
+size_t biq_cache_page_bytes(int page_tokens, int heads, int head_dim);
+
+/*
+ * Rows of a call that belong to sequences: sequence s has rows starts[s] .. starts[s + 1] (device, seqs + 1 numbers that do not
+ * fall, bounded to [0, rows] on the device), or rows s * max_rows .. (s + 1) * max_rows where starts is NULL (then rows must be
+ * seqs * max_rows).  max_rows bounds the rows of a sequence (rows beyond it are not served; `rows` is always enough).  The n
+ * rows of sequence s are its last n tokens: row i is token lens[s] - n + i.
+ */
+typedef struct {
+    const int32_t* starts;
+    int rows, max_rows;
+} biq_ragged;
+
+/* Writes the rows of k and v ([rows][heads][head_dim]) into the cache.  rotation.angles not NULL: keys are turned by the angles
+ * of their tokens on the way (a token outside [0, rotation.positions) is a NaN); the tokens need the length with the new rows
+ * in lens.  Rows before token 0 are dropped.  A call with the same arguments again leaves the cache as it is. */
+typedef struct {
+    biq_cache cache;
+    biq_rows k, v;
+    biq_ragged ragged;
+    biq_rotation rotation;
+    int type;
+} biq_cache_append_args;
+biq_status biq_cache_append(const biq_cache_append_args* args, void* stream);
+
+/* The values that the cache holds, in k and v ([rows][heads][head_dim]): row i of n of sequence s is its token lens[s] - n + i; zeros
+ * before token 0 and for pages that do not exist. */
+typedef struct {
+    biq_cache cache;
+    biq_rows k, v;
+    biq_ragged ragged;
+    int type;
+} biq_cache_read_args;
+biq_status biq_cache_read(const biq_cache_read_args* args, void* stream);
+
+/*
+ * Attention of the rows of q over the cache: out = sum_t softmax_t(scale * q . k_t) v_t over the tokens t that the row at token
+ * position p sees: t < lens[s]; t <= p if causal; t > p - window if window > 0.  q_heads is a multiple of cache.heads; head h
+ * reads the cache's head h / (q_heads / cache.heads).  A row that sees nothing gives zeros.  lse (NULL, or float
+ * [rows][q_heads]): log of the sum of exp(scale * q . k_t), -infinity for a row that sees nothing; with it, parts of a
+ * context computed apart can be joined.
+ *
+ * Codes enter the matrix cores as bf16 values, which hold them exactly; a 32-bit q and its probabilities as three bf16 terms
+ * each (24 bits), a 16-bit q as two, a bf16 q as it is and its probabilities rounded to bf16.  Sums, maxima and the softmax
+ * are in 32 bits.  Deterministic.
+ * max_len: about the largest of lens (0: table_stride * page_tokens).  It only sets how the tokens are split over workgroups:
+ * results are right whatever it is.  workspace: biq_attention_workspace_bytes(), 16-byte aligned (may be 0).
+ */
+typedef struct {
+    biq_cache cache;
+    biq_rows q, out;
+    float* lse;
+    biq_ragged ragged;
+    int type, q_heads, max_len, causal, window;
+    float scale;
+} biq_attention_args;
+size_t biq_attention_workspace_bytes(const biq_attention_args* args);
+biq_status biq_attention(const biq_attention_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, by given random numbers: the answer's tokens are
+ * distributed as the target's, whatever the draft.  Per sequence: draft i (in order) is accepted if
+ *     uniform[i] * q_i(token) < p_i(token)    (32 bits);
+ * the first one that is not, j, is replaced by a token drawn from max(0, p_j - q_j); after all drafts one more is drawn from
+ * p_drafts.  q NULL: the draft was certain of its tokens (q_i is 1 at its token, 0 elsewhere).  drafts = 0: a token is drawn.
+ * Drawn: weights w = floor(2^40 min(1, max(0, p - q))) (0 for NaN), the first token whose running sum of w exceeds
+ * floor(floor(2^31 uniform[drafts]) * (sum of all w) / 2^31).  Integers, so the token depends on no order of additions.  If all w
+ * are 0, p_j alone is drawn from; if it is 0 as well, the token is -1.  uniform in [0, 1) (bounded to it; NaN: 0, and no draft
+ * is accepted).
+ * draft_lens (NULL: all of them): sequence s has draft_lens[s] of the drafts, bounded to [0, drafts].  A token outside
+ * [0, vocab) is not accepted.
+ * tokens [seqs][drafts + 1]: the accepted drafts, the drawn token, then -1.  accepted [seqs]: how many drafts were.
+ * p [seqs][drafts + 1][vocab] and q [seqs][drafts][vocab] with strides in elements between sequences and positions.
+ * drafts <= 63, vocab <= 2^22: BIQ_EUNSUPPORTED beyond.  workspace: biq_verify_workspace_bytes(), 16-byte aligned (may be 0).
+ */
+typedef struct {
+    const void* p;
+    const void* q;
+    int64_t p_seq_stride, p_stride, q_seq_stride, q_stride;
+    const int32_t* draft_tokens;   /* [seqs][drafts] */
+    const int32_t* draft_lens;     /* [seqs] or NULL */
+    const float* uniform;          /* [seqs][drafts + 1] */
+    int32_t* tokens;
+    int32_t* accepted;
+    int type, seqs, drafts, vocab;
+} biq_verify_args;
+size_t biq_verify_workspace_bytes(int seqs, int vocab);
+biq_status biq_verify_drafts(const biq_verify_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

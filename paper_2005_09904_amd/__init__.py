@@ -9,3 +9,8 @@ from .binding import (  # noqa: F401
     biq_num_chunks, biq_pack, biq_packed_bytes, biq_plan_check, biq_plan_get, biq_plan_get_lut, biq_plan_get_mfma, biq_plan_workspace_bytes, biq_quantize, biq_query,
     biq_unpack_keys, biq_unpack_keys16, biq_workspace_bytes, load_library, status_str,
 )
+from .serving import (  # noqa: F401
+    KvCache, PreparedAppend, PreparedAttention, PreparedRead, PreparedRotary, PreparedVerify, biq_attention,
+    biq_attention_workspace_bytes, biq_cache_append, biq_cache_page_bytes, biq_cache_read, biq_rotary, biq_rotary_frequencies,
+    biq_rotary_table, biq_verify_drafts, biq_verify_workspace_bytes,
+)

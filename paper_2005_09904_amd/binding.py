@@ -22,6 +22,9 @@ EXPORTS = [
     "biq_kernel_name", "biq_pack", "biq_unpack_keys", "biq_build_lut", "biq_query", "biq_gemm",
     "biq_gemm_ex", "biq_quantize", "biq_unpack_keys16", "biq_init", "biq_noalloc_scratch_bytes",
     "biq_gemm_noalloc", "biq_gemm_grouped", "biq_lstm_cell",
+    # (serving.py)
+    "biq_rotary_frequencies", "biq_rotary_table", "biq_rotary", "biq_cache_page_bytes", "biq_cache_append", "biq_cache_read",
+    "biq_attention_workspace_bytes", "biq_attention", "biq_verify_workspace_bytes", "biq_verify_drafts",
 ]
 
 
@@ -99,7 +102,20 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "biq_gemm_grouped": (I, [ctypes.POINTER(BiqProblem), I, I, P]),
         "biq_lstm_cell": (I, [P, P, P, P, P, P, P, I, I, I, I, I, P]),
     }
-    for name, (res, args) in sig.items():
+    D = ctypes.c_double
+    serving = {
+        "biq_rotary_frequencies": (I, [P, I, D, I, D, I, D, D]),
+        "biq_rotary_table": (I, [P, P, I, I, I, D, P]),
+        "biq_rotary": (I, [P, P]),
+        "biq_cache_page_bytes": (Z, [I, I, I]),
+        "biq_cache_append": (I, [P, P]),
+        "biq_cache_read": (I, [P, P]),
+        "biq_attention_workspace_bytes": (Z, [P]),
+        "biq_attention": (I, [P, P, Z, P]),
+        "biq_verify_workspace_bytes": (Z, [I, I]),
+        "biq_verify_drafts": (I, [P, P, Z, P]),
+    }
+    for name, (res, args) in [*sig.items(), *serving.items()]:
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args

@@ -1,0 +1,26 @@
+// Internal interface between the checks of the decoder-step operators (serve_api.hip) and the translation units that
+// instantiate and launch their kernels.  Not part of the ABI.
+#pragma once
+
+#include "biq_attention.h"
+#include "biq_rotary.h"
+#include "biq_verify.h"
+
+namespace biq {
+
+// What the planner chooses for attention: tiles of 16 rows per wave.
+struct AttendShape { int nt, waves; };
+
+hipError_t launch_attend_f32(int fmt, int chunks, AttendShape shape, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_bf16(int fmt, int chunks, AttendShape shape, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_f16(int fmt, int chunks, AttendShape shape, const AttendParams& p, hipStream_t s);
+
+// (chunks: 64 elements of a head each)
+hipError_t launch_append(int type, int fmt, int chunks, const AppendParams& p, hipStream_t s);
+hipError_t launch_read(int type, int fmt, int chunks, const ReadParams& p, hipStream_t s);
+hipError_t launch_rotary(int type, const RotaryParams& p, hipStream_t s);
+hipError_t launch_rotary_table(const double* turns, float* angles, int pairs, int first, int positions, double amplitude,
+                               hipStream_t s);
+hipError_t launch_verify(int type, const VerifyParams& p, hipStream_t s);
+
+}  // namespace biq

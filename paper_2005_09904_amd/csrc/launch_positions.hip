@@ -1,0 +1,65 @@
+// Rotary positions and their table; verification of drafted tokens.
+#include "biq_serve_launch.h"
+
+namespace biq {
+namespace {
+
+// The product is reduced to a part of a turn in 64 bits (2^-53 of the turns in all), then to 32 bits.
+__global__ __launch_bounds__(256) void rotary_table_kernel(const double* turns, float* angles, int pairs, int first, int positions,
+                                                           double amplitude) {
+    const long long at = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    if (at >= static_cast<long long>(positions) * pairs) return;
+    const long long row = at / pairs;
+    double t = static_cast<double>(first + row) * turns[at - row * pairs];
+    t -= rint(t);
+    double s, c;
+    sincospi(2.0 * t, &s, &c);
+    angles[2 * at] = static_cast<float>(amplitude * c);
+    angles[2 * at + 1] = static_cast<float>(amplitude * s);
+}
+
+template <int TYPE>
+hipError_t rotary_t(const RotaryParams& p, hipStream_t s) {
+    const int items = p.rotation.rot / 2 + (p.copy ? p.dim - p.rotation.rot : 0);
+    const long long threads = static_cast<long long>(p.rows) * p.heads * items;
+    hipLaunchKernelGGL(rotary_kernel<TYPE>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t verify_t(const VerifyParams& p, hipStream_t s) {
+    hipLaunchKernelGGL(verify_sums_kernel<TYPE>, dim3(static_cast<unsigned>(p.seqs) * p.parts), dim3(kVerifyThreads), 0, s, p);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL(verify_draw_kernel<TYPE>, dim3(p.seqs), dim3(kVerifyThreads), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotary(int type, const RotaryParams& p, hipStream_t s) {
+    switch (type) {
+        case BIQ_F32: return rotary_t<BIQ_F32>(p, s);
+        case BIQ_BF16: return rotary_t<BIQ_BF16>(p, s);
+        case BIQ_F16: return rotary_t<BIQ_F16>(p, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_rotary_table(const double* turns, float* angles, int pairs, int first, int positions, double amplitude,
+                               hipStream_t s) {
+    const long long threads = static_cast<long long>(positions) * pairs;
+    hipLaunchKernelGGL(rotary_table_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, turns, angles, pairs,
+                       first, positions, amplitude);
+    return hipGetLastError();
+}
+
+hipError_t launch_verify(int type, const VerifyParams& p, hipStream_t s) {
+    switch (type) {
+        case BIQ_F32: return verify_t<BIQ_F32>(p, s);
+        case BIQ_BF16: return verify_t<BIQ_BF16>(p, s);
+        case BIQ_F16: return verify_t<BIQ_F16>(p, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace biq

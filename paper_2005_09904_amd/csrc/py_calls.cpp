@@ -237,6 +237,64 @@ void calls_dealloc(PyObject* self) {
     Py_TYPE(self)->tp_free(self);
 }
 
+// ---- an operation whose arguments are one descriptor: Operation(address, name, descriptor, workspace, check, stream) ----
+// descriptor: address of the C struct, which the caller keeps; workspace: None, or (address, bytes) where the C function
+// takes one; stream: its handle.
+struct Operation {
+    PyObject_HEAD
+    void* fn;
+    void* descriptor;
+    void* workspace;
+    size_t workspace_bytes;
+    bool takes_workspace;
+    void* stream;
+    PyObject *name, *check;
+};
+
+PyObject* operation_new(PyTypeObject* type, PyObject* args, PyObject*) {
+    unsigned long long fn, descriptor, address = 0, bytes = 0, stream;
+    PyObject *name, *workspace, *check;
+    if (!PyArg_ParseTuple(args, "KUKOOK", &fn, &name, &descriptor, &workspace, &check, &stream)) return nullptr;
+    if (workspace != Py_None && !PyArg_ParseTuple(workspace, "KK", &address, &bytes)) return nullptr;
+    Operation* o = reinterpret_cast<Operation*>(type->tp_alloc(type, 0));
+    if (!o) return nullptr;
+    o->fn = reinterpret_cast<void*>(static_cast<uintptr_t>(fn));
+    o->descriptor = reinterpret_cast<void*>(static_cast<uintptr_t>(descriptor));
+    o->workspace = reinterpret_cast<void*>(static_cast<uintptr_t>(address));
+    o->workspace_bytes = static_cast<size_t>(bytes);
+    o->takes_workspace = workspace != Py_None;
+    o->stream = reinterpret_cast<void*>(static_cast<uintptr_t>(stream));
+    Py_INCREF(name); Py_INCREF(check);
+    o->name = name; o->check = check;
+    return reinterpret_cast<PyObject*>(o);
+}
+
+PyObject* operation_call(PyObject* self, PyObject* args, PyObject* kwargs) {
+    if (PyTuple_GET_SIZE(args) != 0 || (kwargs && PyDict_GET_SIZE(kwargs) != 0)) {
+        PyErr_SetString(PyExc_TypeError, "a prepared call takes no arguments");
+        return nullptr;
+    }
+    const Operation* o = reinterpret_cast<Operation*>(self);
+    biq_status s;
+    Py_BEGIN_ALLOW_THREADS
+    if (o->takes_workspace)
+        s = reinterpret_cast<biq_status (*)(const void*, void*, size_t, void*)>(o->fn)(o->descriptor, o->workspace, o->workspace_bytes,
+                                                                                    o->stream);
+    else
+        s = reinterpret_cast<biq_status (*)(const void*, void*)>(o->fn)(o->descriptor, o->stream);
+    Py_END_ALLOW_THREADS
+    if (s == BIQ_OK) Py_RETURN_NONE;
+    return PyObject_CallFunction(o->check, "iO", static_cast<int>(s), o->name);
+}
+
+void operation_dealloc(PyObject* self) {
+    Operation* o = reinterpret_cast<Operation*>(self);
+    Py_XDECREF(o->name); Py_XDECREF(o->check);
+    Py_TYPE(self)->tp_free(self);
+}
+
+PyTypeObject operation_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
 #define BIQ_METHOD(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef calls_methods[] = {
     BIQ_METHOD("gemm", call<GEMM>), BIQ_METHOD("query", call<QUERY>), BIQ_METHOD("gemm_noalloc", call<GEMM_NOALLOC>),
@@ -263,13 +321,21 @@ PyMODINIT_FUNC PyInit__calls() {
     calls_type.tp_dealloc = calls_dealloc;
     calls_type.tp_new = calls_new;
     calls_type.tp_methods = calls_methods;
-    if (PyType_Ready(&prepared_type) < 0 || PyType_Ready(&calls_type) < 0) return nullptr;
+    operation_type.tp_name = "paper_2005_09904_amd._calls.Operation";
+    operation_type.tp_basicsize = sizeof(Operation);
+    operation_type.tp_flags = Py_TPFLAGS_DEFAULT;
+    operation_type.tp_dealloc = operation_dealloc;
+    operation_type.tp_new = operation_new;
+    operation_type.tp_call = operation_call;
+    if (PyType_Ready(&operation_type) < 0 || PyType_Ready(&prepared_type) < 0 || PyType_Ready(&calls_type) < 0) return nullptr;
     str_data_ptr = PyUnicode_InternFromString("data_ptr");
     str_numel = PyUnicode_InternFromString("numel");
     str_element_size = PyUnicode_InternFromString("element_size");
     str_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     PyObject* m = PyModule_Create(&module_def);
     if (!m) return nullptr;
+    Py_INCREF(&operation_type);
+    if (PyModule_AddObject(m, "Operation", reinterpret_cast<PyObject*>(&operation_type)) < 0) return nullptr;
     Py_INCREF(&calls_type);
     if (PyModule_AddObject(m, "Calls", reinterpret_cast<PyObject*>(&calls_type)) < 0) return nullptr;
     return m;

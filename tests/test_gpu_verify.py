@@ -1,0 +1,131 @@
+"""Verification of drafted tokens against Python's integers: every token equal."""
+import numpy as np
+import pytest
+import torch
+
+import serving_util as su
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def biq():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2005_09904_amd as biq
+
+    biq.load_library()
+    return biq
+
+
+def case(seqs, drafts, vocab, typ, seed, near=0.5):
+    rng = np.random.default_rng(seed)
+    z = rng.standard_normal((seqs, drafts + 1, vocab)) * 2
+    y = z[:, :drafts] + near * rng.standard_normal((seqs, drafts, vocab))
+    p = np.exp(z) / np.exp(z).sum(axis=2, keepdims=True)
+    q = np.exp(y) / np.exp(y).sum(axis=2, keepdims=True)
+    tokens = np.array([[rng.choice(vocab, p=q[s, i]) for i in range(drafts)] for s in range(seqs)], np.int32).reshape(seqs, drafts)
+    u = (rng.integers(0, 1 << 24, size=(seqs, drafts + 1)) * 2.0 ** -24).astype(np.float32)
+    to = lambda a: torch.from_numpy(a).float().to(su.TYPES[typ])
+    return to(p), to(q), torch.from_numpy(tokens), torch.from_numpy(u)
+
+
+def check(biq, p, q, drafts, u, lens=None):
+    dev = lambda t: None if t is None else t.to("cuda:0")
+    seqs, k = drafts.shape
+    tokens = torch.full((seqs, k + 1), 77, dtype=torch.int32, device="cuda:0")
+    accepted = torch.full((seqs,), 77, dtype=torch.int32, device="cuda:0")
+    ws = torch.full((max(16, biq.biq_verify_workspace_bytes(seqs, p.shape[2])),), 0xff, dtype=torch.uint8, device="cuda:0")
+    biq.biq_verify_drafts(dev(p), dev(q), dev(drafts), dev(u), tokens, accepted, draft_lens=dev(lens), workspace=ws)
+    want = su.verify(p.float().numpy(), None if q is None else q.float().numpy(), drafts.numpy(), None if lens is None else lens.numpy(), u.numpy())
+    assert np.array_equal(accepted.cpu().numpy(), want[1])
+    assert np.array_equal(tokens.cpu().numpy(), want[0])
+    return want
+
+
+@pytest.mark.parametrize("typ", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("seqs,drafts,vocab", [(1, 1, 1), (3, 2, 2), (5, 4, 63), (7, 3, 64), (40, 5, 301), (2, 63, 37), (3, 4, 4095), (3, 4, 4096),
+                                               (3, 4, 4097), (2, 3, 20003), (1, 7, 70000)])
+@pytest.mark.parametrize("certain", [False, True])
+def test_tokens(biq, typ, seqs, drafts, vocab, certain):
+    p, q, t, u = case(seqs, drafts, vocab, typ, seqs + vocab)
+    check(biq, p, None if certain else q, t, u)
+
+
+def test_no_drafts_draws_a_token(biq):
+    p, _, _, u = case(20, 0, 999, "fp32", 1)
+    want = check(biq, p, None, torch.zeros((20, 0), dtype=torch.int32), u)
+    assert len(set(want[0][:, 0])) > 5
+
+
+def test_ragged_drafts_and_tokens_out_of_range(biq):
+    p, q, t, u = case(8, 4, 500, "fp32", 2, near=0.0)          # p = q: every draft is accepted
+    lens = torch.tensor([0, 1, 2, 3, 4, 5, -3, 4], dtype=torch.int32)
+    want = check(biq, p, q, t, u, lens)
+    assert list(want[1]) == [0, 1, 2, 3, 4, 4, 0, 4]
+    t[7, 2] = 500
+    t[4, 0] = -1
+    t[3, 1] = 1 << 30
+    want = check(biq, p, q, t, u, lens)
+    assert want[1][7] == 2 and want[1][4] == 0 and want[1][3] == 1
+    check(biq, p, None, t, u, lens)
+
+
+def test_uniform_at_its_ends_and_outside(biq):
+    p, q, t, u = case(8, 3, 200, "fp32", 3)
+    for value in (0.0, 2.0 ** -24, 1 - 2.0 ** -24, 1.0, 1.5, -0.25, float("nan"), 1e-40):
+        check(biq, p, q, t, torch.full_like(u, value))
+        v = u.clone()
+        v[:, 3] = value
+        check(biq, p, q, t, v)
+
+
+def test_nothing_left_and_rows_of_zeros(biq):
+    """p - q has no weight: p alone; p has none either: no token.  Infinities and NaN weigh 1 and 0."""
+    p, q, t, u = case(6, 2, 9000, "fp32", 4)
+    u[:, :2] = 1.5                                              # nothing is accepted
+    q[0, 0] = p[0, 0]
+    q[1, 0] = 1.0
+    p[2, 0] = 0.0
+    p[3, 0, 5000:] = float("nan")
+    p[4, 0, 8000] = float("inf")
+    q[5, 0, 100:8999] = float("nan")
+    want = check(biq, p, q, t, u)
+    assert want[0][2, 0] == -1 and want[0][0, 0] >= 0
+    p, _, _, u = case(3, 0, 5000, "fp32", 5)
+    p[1] = 0.0
+    p[2, 0, :4999] = 0.0
+    want = check(biq, p, None, torch.zeros((3, 0), dtype=torch.int32), u)
+    assert want[0][1, 0] == -1 and want[0][2, 0] == 4999
+
+
+def test_strides(biq):
+    p, q, t, u = case(4, 3, 1001, "fp32", 6)
+    tokens, accepted = torch.empty((4, 4), dtype=torch.int32, device="cuda:0"), torch.empty(4, dtype=torch.int32, device="cuda:0")
+    ws = torch.empty(biq.biq_verify_workspace_bytes(4, 1001), dtype=torch.uint8, device="cuda:0")
+    want = su.verify(p.numpy(), q.numpy(), t.numpy(), None, u.numpy())
+    for lead, width in ((0, 1004), (0, 1001), (1, 1003), (3, 1008)):
+        a, b = (torch.full((4 * 5 * width + 8,), float("nan"), device="cuda:0") for _ in range(2))
+        pv = a[lead:lead + 4 * 5 * width].view(4, 5, width)[:, 1:, :1001]
+        qv = b[lead:lead + 4 * 3 * width].view(3, 4, width).transpose(0, 1)[..., :1001]
+        pv.copy_(p)
+        qv.copy_(q)
+        biq.biq_verify_drafts(pv, qv, t.to("cuda:0"), u.to("cuda:0"), tokens, accepted, workspace=ws)
+        assert np.array_equal(tokens.cpu().numpy(), want[0]) and np.array_equal(accepted.cpu().numpy(), want[1])
+
+
+def test_the_tokens_are_distributed_as_the_targets(biq):
+    """20000 sequences with the same two distributions: counts of the first token within 5 standard deviations of p's."""
+    n, vocab = 20000, 6
+    g = torch.Generator().manual_seed(5)
+    p = torch.tensor([0.4, 0.05, 0.25, 0.1, 0.15, 0.05])
+    q = torch.tensor([0.1, 0.3, 0.25, 0.05, 0.05, 0.25])
+    drafts = torch.multinomial(q.expand(n, vocab), 1, generator=g).int()
+    u = torch.rand((n, 2), generator=g)
+    dev = "cuda:0"
+    tokens, accepted = torch.empty((n, 2), dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev)
+    ws = torch.empty(biq.biq_verify_workspace_bytes(n, vocab), dtype=torch.uint8, device=dev)
+    biq.biq_verify_drafts(p.to(dev).expand(n, 2, vocab), q.to(dev).expand(n, 1, vocab), drafts.to(dev), u.to(dev), tokens, accepted, workspace=ws)
+    counts = torch.bincount(tokens[:, 0].long().cpu(), minlength=vocab).double()
+    assert ((counts - n * p.double()).abs() <= 5 * (n * p.double() * (1 - p.double())).sqrt()).all()
+    rate = torch.minimum(p, q).sum().item()
+    assert abs(accepted.float().mean().item() - rate) < 5 * (rate * (1 - rate) / n) ** 0.5
