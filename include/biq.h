@@ -494,11 +494,11 @@ biq_status biq_cache_read(const biq_cache_read_args* args, void* stream);
  * [rows][q_heads]): log of the sum of exp(scale * q . k_t), -infinity for a row that sees nothing; with it, parts of a
  * context computed apart can be joined.
  *
- * Codes enter the matrix cores as bf16 values, which hold them exactly; a 32-bit q and its probabilities as three bf16 terms
- * each (24 bits), a 16-bit q as two, a bf16 q as it is and its probabilities rounded to bf16.  Sums, maxima and the softmax
- * are in 32 bits.  Deterministic.
+ * Codes enter the matrix cores as 16-bit floats, which hold them exactly; a 32-bit q as two of them (22 bits, below 2^-24
+ * of the row's largest element fewer), and so do the weights of 32-bit and 16-bit outputs; those of a bf16 output are one (11
+ * bits).  Sums, maxima and the softmax are in 32 bits.  Deterministic.
  * max_len: about the largest of lens (0: table_stride * page_tokens).  It only sets how the tokens are split over workgroups:
- * results are right whatever it is.  workspace: biq_attention_workspace_bytes(), 16-byte aligned (may be 0).
+ * results are right whatever it is (splits differ in the order of additions).  workspace: biq_attention_workspace_bytes(), 16-byte aligned (may be 0).
  */
 typedef struct {
     biq_cache cache;

@@ -22,53 +22,123 @@ struct AttendParams {
     Ragged ragged;
     Rows q, out;
     float* lse;
-    float* part;             // splits > 1: [row * q_heads + head][split][dim] sums, then [..][split][2] maximum and sum
-    long long part_stats;    // floats before the maxima
+    float* part;             // pieces of units, [slot][row of the tile][dim] sums, ..
+    float* stats;            // .. and [slot][row of the tile][2] references and sums of weights
+    int* owners;             // [unit][2] first and last share with steps of the unit
     int q_heads, group, causal, window;
-    int units;               // seqs * heads * splits
-    int splits, split_tokens, row_tiles;
-    float scale;             // scale * log2(e)
+    int seqs, row_tiles;     // row_tiles: the most that a sequence's rows make
+    int shares;              // > 0: workgroups that share all steps equally; 0: a workgroup per unit
+    int negative;            // the scale is below 0: q is negated
+    float scale;             // |scale| * log2(e)
 };
 
-// Tokens that a tile of rows sees, in whole steps of 64: [base, end).
-struct TokenSpan { int base, end; };
-__device__ __forceinline__ TokenSpan token_span(const AttendParams& p, int len, int pos_first, int pos_last) {
-    TokenSpan t;
-    int lo = p.window > 0 ? pos_first - p.window + 1 : 0;
+// What a workgroup spends on a unit beside its steps (rows, first keys, joining its waves, results), in steps.
+constexpr int kUnitCost = 5;
+
+// A unit is a tile of rows of a sequence and head; its work is steps of 64 tokens, [base, base + 64 steps), the same for all
+// units of a sequence (every token that one of its rows sees).
+struct SeqWork {
+    int2 range;              // first row, rows
+    int len, base, steps;    // steps of a unit: one at least, as a row that sees nothing has a result too
+    int tiles;               // units per head
+    __device__ __forceinline__ int cost() const { return steps + kUnitCost; }
+    __device__ __forceinline__ int total(int heads) const { return cost() * tiles * heads; }
+};
+template <int ROWS>
+__device__ __forceinline__ SeqWork seq_work(const AttendParams& p, int seq) {
+    SeqWork w;
+    w.range = p.ragged.range(seq);
+    w.len = p.cache.length(seq);
+    int lo = p.window > 0 ? w.len - w.range.y - p.window + 1 : 0;
     lo = lo < 0 ? 0 : lo;
-    t.base = lo & ~63;
-    t.end = p.causal ? pos_last + 1 : len;
-    t.end = t.end < t.base ? t.base : t.end;
-    return t;
-}
-// Splits of that span that have tokens (one at least).  The last split takes what is left, whatever the length.
-__device__ __forceinline__ int active_splits(const AttendParams& p, TokenSpan t) {
-    const int n = (t.end - t.base + p.split_tokens - 1) / p.split_tokens;
-    return n < 1 ? 1 : n > p.splits ? p.splits : n;
+    w.base = lo & ~63;
+    w.steps = (w.len - w.base + 63) >> 6;
+    w.steps = w.steps < 1 ? 1 : w.steps;
+    w.tiles = (w.range.y * p.group + ROWS - 1) / ROWS;
+    return w;
 }
 
-// Terms of 8 floats as bf16, each the upper half of what is left (the last one rounded): 8 bits of significand a term.
-template <int TERMS>
-__device__ __forceinline__ void bf16_terms(const float (&x)[8], bf16x8 (&out)[TERMS]) {
-    float r[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r[j] = x[j];
-#pragma unroll
-    for (int t = 0; t < TERMS; ++t) {
-        union { bf16x8 v; uint32_t w[4]; } o;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (t == TERMS - 1) {
-                union { bf16x2 v; uint32_t w; } c;
-                c.v = __builtin_convertvector((f32x2){r[2 * j], r[2 * j + 1]}, bf16x2);
-                o.w[j] = c.w;
-            } else {
-                o.w[j] = __builtin_amdgcn_perm(__float_as_uint(r[2 * j + 1]), __float_as_uint(r[2 * j]), 0x07060302);
-                r[2 * j] -= __uint_as_float(__float_as_uint(r[2 * j]) & 0xffff0000u);
-                r[2 * j + 1] -= __uint_as_float(__float_as_uint(r[2 * j + 1]) & 0xffff0000u);
-            }
+// All units of a call in a row, sequence by sequence, in it heads slowest, each taking kUnitCost places and one for each of
+// its steps.  Every workgroup has an equal share of the places, whatever the lengths are.  Every wave finds its place by
+// itself: a lane per sequence, 64 at a time.
+template <int ROWS>
+struct Shares {
+    const AttendParams& p;
+    int lane, upto, total;   // upto: running sum over the first 64 sequences
+    int count;               // shares: none without a place
+    __device__ __forceinline__ Shares(const AttendParams& params, int l, bool used = true) : p(params), lane(l), upto(0), total(0), count(0) {
+        if (!used) return;
+        for (int s = 0; s < p.seqs; s += 64) {
+            const int x = running(s);
+            if (s == 0) upto = x;
+            total += __builtin_amdgcn_readlane(x, 63);
         }
-        out[t] = o.v;
+        count = p.shares < total ? p.shares : total;
+    }
+    __device__ __forceinline__ int running(int s0) const {
+        const int s = s0 + lane;
+        int x = s < p.seqs ? seq_work<ROWS>(p, s).total(p.cache.heads) : 0;
+        // running sum: in rows of 16 lanes, then the rows' ends
+        x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // row_shr:1, 2, 4, 8
+        x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row_bcast:15 to rows 1 and 3
+        x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);     // row_bcast:31 to rows 2 and 3
+        return x;
+    }
+    // First place of share w.
+    __device__ __forceinline__ int begin(int w) const {
+        return static_cast<int>(static_cast<unsigned long long>(static_cast<unsigned>(total)) * static_cast<unsigned>(w) / static_cast<unsigned>(count));
+    }
+    // Share that place x belongs to.
+    __device__ __forceinline__ int owner(int x) const {
+        return static_cast<int>((static_cast<unsigned long long>(x + 1) * static_cast<unsigned>(count) - 1) / static_cast<unsigned>(total));
+    }
+    // Sequence of place x (x < total), which becomes the place's number in the sequence.
+    __device__ __forceinline__ int find(int& x) const {
+        for (int s = 0;; s += 64) {
+            const int sums = s == 0 ? upto : running(s);
+            const unsigned long long above = __ballot(sums > x);
+            if (above) {
+                const int l = __ffsll(above) - 1;
+                if (l > 0) x -= __builtin_amdgcn_readlane(sums, l - 1);
+                return s + l;
+            }
+            x -= __builtin_amdgcn_readlane(sums, 63);
+        }
+    }
+};
+
+__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// log(2^ref total): the exponent of total is taken off first, as ref and log2(total) mostly cancel.
+__device__ __forceinline__ float log_sum(float ref, float total) {
+    if (total == 0.f) return -INFINITY;
+    const float m = __builtin_amdgcn_frexp_mantf(total);
+    return ((ref + static_cast<float>(__builtin_amdgcn_frexp_expf(total))) + __builtin_amdgcn_logf(m)) * 0.69314718055994531f;
+}
+
+constexpr float kNoRef = -3.402823466e38f;            // reference of a row that has seen nothing
+
+// The matrix cores multiply 16-bit floats: both code formats fit them exactly, and a 32-bit number is two of them to 22 bits
+// once it is scaled into their range.  Terms of q: two for 32-bit elements, one otherwise (bf16 values have 8 bits).
+template <int TYPE> struct RowTerms { static constexpr int value = TYPE == BIQ_F32 ? 2 : 1; };
+// Terms of the weights: one (11 bits) where the output has 8 bits, two otherwise.
+template <int TYPE> struct WeightTerms { static constexpr int value = TYPE == BIQ_BF16 ? 1 : 2; };
+
+template <int TERMS>
+__device__ __forceinline__ void f16_terms(const float (&x)[8], f16x8 (&out)[TERMS]) {
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        const f16x2 hi = __builtin_convertvector((f32x2){x[j], x[j + 1]}, f16x2);
+        out[0][j] = hi[0];
+        out[0][j + 1] = hi[1];
+        if constexpr (TERMS == 2) {
+            const f16x2 lo = __builtin_convertvector((f32x2){x[j] - static_cast<float>(hi[0]), x[j + 1] - static_cast<float>(hi[1])}, f16x2);
+            out[1][j] = lo[0];
+            out[1][j + 1] = lo[1];
+        }
     }
 }
 
@@ -84,330 +154,441 @@ __device__ __forceinline__ void load_q8(const Rows& q, long long at, float (&x)[
     }
 }
 
-template <int TYPE> struct AttendTerms { static constexpr int value = TYPE == BIQ_F32 ? 3 : TYPE == BIQ_F16 ? 2 : 1; };
+template <int TYPE>
+__device__ __forceinline__ void store_row4(const Rows& out, long long at, f32x4 x) {
+    if (out.quads) store_elem4<TYPE>(out.data, at, x);
+    else
+#pragma unroll
+        for (int j = 0; j < 4; ++j) store_elem<TYPE>(out.data, at + j, x[j]);
+}
 
-__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
+// Row tiles, their place in the tensors and what they see.
+struct RowPlace {
+    long long row;           // -1: none
+    int head, lo, hi;
+};
+__device__ __forceinline__ RowPlace row_place(const AttendParams& p, int2 range, int len, int head, int rr, int rows_all) {
+    RowPlace r;
+    const int i = rr / p.group, pos = len - range.y + i;
+    r.row = rr < rows_all ? range.x + i : -1;
+    r.head = head * p.group + (rr - i * p.group);
+    r.hi = p.causal ? pos : len - 1;
+    r.lo = p.window > 0 ? pos - p.window + 1 : 0;
+    return r;
+}
+
+// Elements of the row of a lane's column: part (c, h) holds elements 64 c + 16 (lane / 16) + 8 h ..
+template <int TYPE, int CH>
+__device__ __forceinline__ void load_row(const AttendParams& p, const RowPlace& r, int dim, int grp, float (&x)[CH][2][8]) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[c][h][j] = 0.f;
+            const int d = c * 64 + grp * 16 + h * 8;
+            if (r.row >= 0 && d < dim) load_q8<TYPE>(p.q, r.row * p.q.row_stride + r.head * p.q.head_stride + d, x[c][h]);
+        }
+}
+
+// The same as right operands.  Rows of 32-bit or bf16 elements are scaled by a power of two, their largest magnitude to
+// [2^14, 2^15); returned is what undoes it.
+template <int TYPE, int CH>
+__device__ __forceinline__ float row_terms(bool negative, float (&x)[CH][2][8], f16x8 (&q)[CH][2][RowTerms<TYPE>::value]) {
+    float up = 1.f, down = 1.f;
+    if constexpr (TYPE != BIQ_F16) {
+        float most = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[c][h][j]));
+        most = max_over_groups(most);
+        int e = static_cast<int>(__float_as_uint(most) >> 23);          // biased exponent
+        e = most == 0.f ? 127 + 14 : e < 27 ? 27 : e;
+        up = __uint_as_float(static_cast<uint32_t>(127 + 14 + 127 - e) << 23);
+        down = __uint_as_float(static_cast<uint32_t>(e - 14) << 23);
+    }
+    if (negative) up = -up;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[c][h][j] *= up;
+            f16_terms<RowTerms<TYPE>::value>(x[c][h], q[c][h]);
+        }
+    return down;
+}
+
+// A lane's 16 scores of one row against the tokens first .. first + 15 of a block -> weights times the block's value scale v,
+//     y = 2^(score kscale - ref) v,  sum += sum of 2^(score kscale - ref),
+// as PT 16-bit terms per 8 tokens.
+//
+// y has to stay in the range of 16-bit floats whatever v is, so ref follows the running maximum of score + log2 v (v taken as
+// 2^-100 at least: the sums themselves have 32 bits' range), 6 below it, and only where y would pass 2^14: then `grown` is
+// set (for the whole wave), and what was summed is to be multiplied by `keep`.  A y below 2^-25 (2^-39 of the largest one) is
+// lost.
+// With one term v is added to the exponent as its logarithm, and divided out of the sum once.
+struct Sight { int lo, hi, first, valid; };           // tokens seen: lo .. hi, and the block's first `valid`
+template <int PT>
+__device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v, bool whole, Sight see, float& ref, float& sum, bool& grown,
+                                      float& keep, f16x8 (&out)[2][PT]) {
+    float x[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = s[j >> 2][j & 3];
+    if (!whole) {                                     // (scaled first: a block that is hidden may have any scale)
+        const int lo = see.lo - see.first, hi = see.hi - see.first < see.valid - 1 ? see.hi - see.first : see.valid - 1;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = j < lo || j > hi ? -INFINITY : x[j] * kscale;
+        kscale = 1.f;
+        v = lo > 15 || hi < 0 || hi < lo ? 1.f : v;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) top = fmaxf(top, x[j]);
+    const float lv = fmaxf(__builtin_amdgcn_logf(v), -100.f);
+    top = __builtin_fmaf(top, kscale, lv);            // (kscale >= 0, or NaN)
+    grown = __any(top > ref + 14.f);
+    keep = 1.f;
+    if (grown) {
+        const float most = max_over_groups(top);
+        const float next = most > ref + 14.f ? most - 6.f : ref;       // (a row's bits do not depend on its neighbours)
+        keep = exp2_raw(ref - next);
+        ref = next;
+    }
+    float part = 0.f;
+    if (PT == 1 && __all(v > 0.f && v < INFINITY)) {
+        const float c = lv - ref;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const f32x2 y = {exp2_raw(__builtin_fmaf(x[8 * h + j], kscale, c)), exp2_raw(__builtin_fmaf(x[8 * h + j + 1], kscale, c))};
+                const f16x2 w = __builtin_convertvector(y, f16x2);
+                out[h][0][j] = w[0];
+                out[h][0][j + 1] = w[1];
+                part += y[0] + y[1];
+            }
+        part *= exp2_raw(-lv);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float e = exp2_raw(__builtin_fmaf(x[8 * h + j], kscale, -ref));
+                part += e;
+                y[j] = e * v;
+            }
+            f16_terms<PT>(y, out[h]);
+        }
+    }
+    sum = __builtin_fmaf(sum, keep, part);
+}
+
+// The four blocks of a step of 64 tokens.  The step is the same for all lanes, so the pages are looked up with scalar loads:
+// a vector load would wait its turn behind all codes that were requested before it.
+struct StepPages {
+    long long offset[4], scale[4];       // bytes of the block's keys and of their scale (of page 0 where there is no page)
+    int valid[4];                        // tokens of the block
+    template <typename T>
+    static __device__ __forceinline__ T of(const T (&x)[4], int block) {
+        const T a = block & 1 ? x[1] : x[0], b = block & 1 ? x[3] : x[2];
+        return block & 2 ? b : a;
+    }
+};
+__device__ __forceinline__ StepPages step_pages(const Cache& c, int dim, int seq, int head, int t0, int len) {
+    typedef const __attribute__((address_space(4))) int* ScalarInts;
+    const ScalarInts table = (ScalarInts)(c.table + static_cast<long long>(seq) * c.table_stride);
+    const long long codes = static_cast<long long>(c.heads) * c.page_blocks * kCacheBlock * dim;
+    StepPages s;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int b = (t0 >> 4) + j, i = c.page_index(b);
+        const int n = table[i < c.table_stride ? i : 0];
+        const bool there = i < c.table_stride && static_cast<uint32_t>(n) < static_cast<uint32_t>(c.num_pages);
+        const long long page = (there ? n : 0) * c.page_bytes;
+        const int block = c.block_in_page(b, head);
+        const int left = there ? len - b * kCacheBlock : 0;
+        s.valid[j] = left < 0 ? 0 : left > kCacheBlock ? kCacheBlock : left;
+        s.offset[j] = page + static_cast<long long>(block) * (kCacheBlock * dim);
+        s.scale[j] = page + 2 * codes + 4ll * block;
+    }
+    return s;
+}
+
+// Codes of tokens that the sequence does not have may be anything: zeros.
+__device__ __forceinline__ u32x4 first_codes(u32x4 w, int valid) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int left = valid - 4 * i;
+        w[i] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+    }
+    return w;
+}
 
 // Few rows of a sequence and head (one token with its heads, drafted tokens).  The waves of a workgroup hold the same rows and take
-// steps of 64 tokens in turn, straight from memory to registers: every code is used by one wave only.  The waves' sums are
-// joined through LDS.  CH: 64 elements of a head each; NT: tiles of 16 rows.
-template <int TYPE, int FMT, int CH, int NT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void attend_rows_kernel(const AttendParams p) {
-    constexpr int TERMS = AttendTerms<TYPE>::value;
+// steps of 64 tokens in turn, straight from memory to registers: every code is used by one wave only.  Keys are requested a
+// step ahead, values before the scores.  The waves' sums are joined through LDS.
+// CH: 64 elements of a head each; FULL: the head has all of them; NT: tiles of 16 rows.
+template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1) void attend_rows_kernel(const AttendParams p) {
+    constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE>::value;
     constexpr int ROWS = 16 * NT;
     extern __shared__ float lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, grp = lane >> 4;
-    // row tiles of a unit follow each other on one XCD: they read the same tokens
-    const int xcd = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
-    const int unit = at / p.row_tiles * kXcds + xcd, tile = at % p.row_tiles;
-    if (unit >= p.units) return;
-    const int split = unit % p.splits, head = unit / p.splits % p.cache.heads, seq = unit / p.splits / p.cache.heads;
-    const int2 range = p.ragged.range(seq);
-    const int len = p.cache.length(seq);
-    const int rows_here = range.y * p.group - tile * ROWS;      // (token, head of the group), heads fastest
-    if (rows_here <= 0) return;
-    const int i_first = tile * ROWS / p.group;
-    const int i_last = (tile * ROWS + (rows_here < ROWS ? rows_here : ROWS) - 1) / p.group;
-    const int pos0 = len - range.y;                             // token of row 0 (negative: before the first token)
-    const TokenSpan span = token_span(p, len, pos0 + i_first, pos0 + i_last);
-    const int splits_here = active_splits(p, span);
-    if (split >= splits_here) return;
-    const int begin = span.base + split * p.split_tokens;
-    const int end = split == splits_here - 1 ? span.end : begin + p.split_tokens;
+    const int dim = FULL ? 64 * CH : p.cache.dim;
+    const long long codes = static_cast<long long>(p.cache.heads) * p.cache.page_blocks * kCacheBlock * dim;
+    const int kblock = col >> 2;                                // block of this lane's key rows, 0 .. 3
 
-    const int dim = p.cache.dim;
-    // rows of this lane's columns, and what they see
-    long long row_of[NT];
-    int head_of[NT], lo[NT], hi[NT];
-    bf16x8 q[NT][CH][2][TERMS];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int rr = tile * ROWS + n * 16 + col;
-        const bool there = n * 16 + col < rows_here;
-        const int i = rr / p.group;
-        row_of[n] = there ? range.x + i : -1;
-        head_of[n] = head * p.group + (rr - i * p.group);
-        hi[n] = p.causal ? pos0 + i : len - 1;
-        lo[n] = p.window > 0 ? pos0 + i - p.window + 1 : 0;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                const int d = c * 64 + grp * 16 + h * 8;
-                if (there && d < dim) load_q8<TYPE>(p.q, row_of[n] * p.q.row_stride + head_of[n] * p.q.head_stride + d, x);
-                bf16_terms<TERMS>(x, q[n][c][h]);
-            }
+    // steps of this workgroup: a share of all, or all of one unit
+    const Shares<ROWS> shares(p, lane, p.shares > 0);
+    int from = 0, upto = 1;
+    if (p.shares > 0) {
+        if (static_cast<int>(blockIdx.x) >= shares.count) return;
+        from = shares.begin(blockIdx.x);
+        upto = shares.begin(blockIdx.x + 1);
     }
-    // tokens that every row of the tile sees
-    const int all_lo = p.window > 0 ? pos0 + i_last - p.window + 1 : 0;
-    const int all_hi = p.causal ? pos0 + i_first : len - 1;
+    for (bool again = false; from < upto;) {
+    int seq, unit, step = 0, stop;                              // (unit of the sequence: head * tiles + tile)
+    if (p.shares > 0) {
+        stop = from;
+        seq = __builtin_amdgcn_readfirstlane(shares.find(stop));
+    } else {
+        seq = blockIdx.x / (p.cache.heads * p.row_tiles);
+    }
+    const SeqWork work = seq_work<ROWS>(p, seq);
+    if (p.shares > 0) {
+        unit = stop / work.cost();
+        const int place = stop - unit * work.cost(), left = upto - from;
+        step = place > kUnitCost ? place - kUnitCost : 0;
+        stop = place + left < work.cost() ? place + left - kUnitCost : work.steps;
+        from += left < work.cost() - place ? left : work.cost() - place;
+        if (stop <= step) continue;                             // no step in this share
+    } else {
+        const int r = blockIdx.x - seq * (p.cache.heads * p.row_tiles), t = r % p.row_tiles;
+        if (t >= work.tiles) return;
+        unit = r / p.row_tiles * work.tiles + t;
+        stop = work.steps;
+        from = upto;
+    }
+    const int head = unit / work.tiles, tile = unit - head * work.tiles;
+    // a piece that ends before its unit does: the share's second slot if it begins it, else the first
+    const int slot = stop - step == work.steps ? -1 : 2 * static_cast<int>(blockIdx.x) + (step == 0 ? 1 : 0);
+    if (p.shares > 0 && step == 0 && threadIdx.x == 0) {
+        const int id = (seq * p.cache.heads + head) * p.row_tiles + tile;
+        p.owners[2 * id] = blockIdx.x;
+        p.owners[2 * id + 1] = stop == work.steps ? blockIdx.x : shares.owner(from - 1 - stop + work.steps);
+    }
+    const int2 range = work.range;
+    const int len = work.len;
+    const int rows_all = range.y * p.group, row0 = tile * ROWS;     // (token, head of the group), heads fastest
+    const int pos0 = len - range.y;                             // token of row 0 (negative: before the first token)
+    const int pos_first = pos0 + row0 / p.group;
+    const int pos_last = pos0 + ((row0 + ROWS < rows_all ? row0 + ROWS : rows_all) - 1) / p.group;
+    const int begin = work.base + step * 64, end = work.base + stop * 64;
 
-    f32x4 o[NT][CH * 4];
-    float m[NT], l[NT];
+    // the rows are requested first: they are needed first
+    RowPlace place[NT];
+    float x[NT][CH][2][8];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        m[n] = -INFINITY;
+        place[n] = row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
+        load_row<TYPE, CH>(p, place[n], dim, grp, x[n]);
+    }
+    u32x4 kc[4][CH];                                            // token 4 t + col % 4 of that block
+    float ks = 0.f, vs = 0.f;
+    const uint8_t* vbase = p.cache.store;
+    int valid = 0;
+    auto request_keys = [&](int t0) {
+        const StepPages at = step_pages(p.cache, dim, seq, head, t0, len);
+        const uint8_t* kbase = p.cache.store + at.of(at.offset, kblock);
+        vbase = p.cache.store + codes + at.of(at.offset, grp);
+        const uint8_t* scales = p.cache.store + at.of(at.scale, grp);
+        valid = at.of(at.valid, grp);
+        // (scales of blocks that do not exist are not used, whatever they are)
+        ks = *reinterpret_cast<const float*>(scales);
+        vs = reinterpret_cast<const float*>(scales)[p.cache.heads * p.cache.page_blocks];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                int d = c * 64 + grp * 16;
+                d = FULL || d < dim ? d : 0;                    // (against zeros of q)
+                kc[t][c] = *reinterpret_cast<const u32x4*>(kbase + (4 * t + (col & 3)) * dim + d);
+            }
+    };
+    int t0 = begin + __builtin_amdgcn_readfirstlane(wave) * 64;
+    if (t0 < end) request_keys(t0);
+
+    f16x8 q[NT][CH][2][QT];
+    float unit_of[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) unit_of[n] = row_terms<TYPE, CH>(p.negative, x[n], q[n]) * p.scale;
+
+    // tokens that every row of the tile sees
+    const int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0;
+    const int all_hi = p.causal ? pos_first : len - 1;
+    f32x4 o[NT][CH * 4];
+    float ref[NT], l[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        ref[n] = kNoRef;
         l[n] = 0.f;
 #pragma unroll
         for (int t = 0; t < CH * 4; ++t) o[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
-
-    const long long codes = p.cache.codes_bytes();
-    const int kblock = col >> 2;                                // block of this lane's key rows, 0 .. 3
-    // key rows of the lane in tile t: token 4 t + col % 4 of its block
-    u32x4 kc[4][CH];
-    float ks = 0.f, vs = 0.f;
-    const uint8_t* vbase = p.cache.store;
-    int valid = 0;
-
-    auto locate_and_load_keys = [&](int t0) {
-        const int kb = (t0 >> 4) + kblock, vb = (t0 >> 4) + grp;
-        const int kp = p.cache.page_number(seq, kb), vp = p.cache.page_number(seq, vb);
-        // (without a page: codes of page 0, hidden below)
-        const uint8_t* kbase = p.cache.page(kp < 0 ? 0 : kp) + static_cast<long long>(p.cache.block_in_page(kb, head)) * (kCacheBlock * dim);
-        const uint8_t* page = p.cache.page(vp < 0 ? 0 : vp);
-        const int vblock = p.cache.block_in_page(vb, head);
-        vbase = page + codes + static_cast<long long>(vblock) * (kCacheBlock * dim);
-        const float* scales = reinterpret_cast<const float*>(page + 2 * codes) + vblock;
-        valid = vp < 0 ? 0 : len - vb * kCacheBlock;
-        valid = valid < 0 ? 0 : valid > kCacheBlock ? kCacheBlock : valid;
-        ks = valid ? scales[0] : 0.f;
-        vs = valid ? scales[p.cache.heads * p.cache.page_blocks] : 0.f;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            int d = c * 64 + grp * 16;
-            d = d < dim ? d : 0;                                // (against zeros of q)
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                kc[t][c] = *reinterpret_cast<const u32x4*>(kbase + (4 * t + (col & 3)) * dim + d);
-        }
-    };
-
-    int t0 = begin + wave * 64;
-    if (t0 < end) locate_and_load_keys(t0);
     for (; t0 < end; t0 += 64 * WAVES) {
-        // values of this step
         u32x4 vc[CH * 4];
 #pragma unroll
         for (int t = 0; t < CH * 4; ++t) {
-            const int d = t * 16 < dim ? t * 16 + col : col;    // (beyond the head: sums that are not stored)
+            const int d = FULL || t * 16 < dim ? t * 16 + col : col;    // (beyond the head: sums that are not stored)
             vc[t] = *reinterpret_cast<const u32x4*>(vbase + d * kCacheBlock);
         }
-        const float kscale = ks * p.scale, vscale = vs;
+        const float kscale = ks, vscale = vs;
         const int nvalid = valid;
-        // scores
+        __builtin_amdgcn_sched_barrier(0);                      // (the requests stay ahead of the products)
         f32x4 s[NT][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) s[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < 4; ++t) s[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bf16x8 k = codes_bf16<FMT>(kc[t][c][2 * h], kc[t][c][2 * h + 1]);
+            for (int h = 0; h < 2; ++h) {
+                f16x8 k[4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                for (int t = 0; t < 4; ++t) k[t] = codes_f16<FMT>(kc[t][c][2 * h], kc[t][c][2 * h + 1]);
 #pragma unroll
-                        for (int e = 0; e < TERMS; ++e)
-                            s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[n][c][h][e], s[n][t], 0, 0, 0);
-                }
-        }
-        // keys of the next step
-        const int tn = t0 + 64 * WAVES;
-        if (tn < end) locate_and_load_keys(tn);
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < QT; ++e)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k[t], q[n][c][h][e], s[n][t], 0, 0, 0);
+            }
+        // (always, the last ones again: loads under a condition would all be waited for before the values' products)
+        __builtin_amdgcn_sched_barrier(0);
+        request_keys(t0 + 64 * WAVES < end ? t0 + 64 * WAVES : t0);
+        __builtin_amdgcn_sched_barrier(0);
 
         const bool whole = t0 + 63 <= all_hi && t0 >= all_lo && __all(nvalid == kCacheBlock);
         if (!whole) {
-            // codes of tokens that the sequence does not have may be anything
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int left = nvalid - 4 * w;                // tokens of this dword
-                const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-#pragma unroll
-                for (int t = 0; t < CH * 4; ++t) vc[t][w] &= mask;
-            }
+            for (int t = 0; t < CH * 4; ++t) vc[t] = first_codes(vc[t], nvalid);
         }
+        f16x8 w[NT][2][PT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int first = t0 + grp * kCacheBlock;           // token of the lane's sum 0
-            float x[16];
-            float top = -INFINITY;
+            bool grown;
+            float keep;
+            const Sight see = {place[n].lo, place[n].hi, t0 + grp * kCacheBlock, nvalid};
+            weigh<PT>(s[n], kscale * unit_of[n], vscale, whole, see, ref[n], l[n], grown, keep, w[n]);
+            if (grown) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                x[j] = s[n][j >> 2][j & 3] * kscale;
-                if (!whole && (first + j < lo[n] || first + j > hi[n] || j >= nvalid)) x[j] = -INFINITY;
-                top = fmaxf(top, x[j]);
-            }
-            const float now = fmaxf(m[n], max_over_groups(top));
-            const float ref = now == -INFINITY ? 0.f : now;     // (nothing seen yet)
-            const float keep = exp2_raw(m[n] - ref);
-            m[n] = now;
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const bool seen = whole || x[j] != -INFINITY;
-                const float e = exp2_raw(x[j] - ref);
-                sum += e;
-                x[j] = seen ? e * vscale : 0.f;                 // (a hidden token's scale may be NaN)
-            }
-            l[n] = l[n] * keep + sum;
-#pragma unroll
-            for (int t = 0; t < CH * 4; ++t) o[n][t] *= keep;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float y[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = x[8 * h + j];
-                bf16x8 pt[TERMS];
-                bf16_terms<TERMS>(y, pt);
-#pragma unroll
-                for (int t = 0; t < CH * 4; ++t) {
-                    const bf16x8 v = codes_bf16<FMT>(vc[t][2 * h], vc[t][2 * h + 1]);
-#pragma unroll
-                    for (int e = 0; e < TERMS; ++e)
-                        o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pt[e], o[n][t], 0, 0, 0);
-                }
+                for (int t = 0; t < CH * 4; ++t) o[n][t] *= keep;
             }
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < CH * 4; ++t) {
+                const f16x8 v = codes_f16<FMT>(vc[t][2 * h], vc[t][2 * h + 1]);
+#pragma unroll
+                for (int e = 0; e < PT; ++e)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[n][h][e], o[n][t], 0, 0, 0);
+            }
     }
 
-    // ---- the waves' sums, joined -------------------------------------------------------------------
-    float top[NT], total[NT];
+    // ---- the waves' sums, joined: every wave's go to LDS, then every thread adds 4 elements of a row ------------------
+    // Sums (tile i of 16 elements, lane) lie at 16-byte place 64 i + 16 grp + (col + 4 i + grp) % 16: neither the lanes that
+    // write a tile nor those that read a row meet on a bank.
+    float* stats = lds;                                         // [wave][ROWS][2]
+    f32x4* sums = reinterpret_cast<f32x4*>(lds + WAVES * ROWS * 2);     // [wave][NT][CH * 4][64]
+    if (again) __syncthreads();                                 // (the unit before is read)
+    again = true;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        total[n] = sum_over_groups(l[n]);
-        top[n] = m[n];
-    }
-    if constexpr (WAVES > 1) {
-        float* stats = lds;                                     // [wave][ROWS][2]
-        float* slots = lds + WAVES * ROWS * 2;                  // [WAVES / 2][NT * CH * 4][64][4]
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-            if (grp == 0) {
-                stats[(wave * ROWS + n * 16 + col) * 2] = m[n];
-                stats[(wave * ROWS + n * 16 + col) * 2 + 1] = total[n];
-            }
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float t = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) t = fmaxf(t, stats[(w * ROWS + n * 16 + col) * 2]);
-            const float ref = t == -INFINITY ? 0.f : t;
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w)
-                sum += stats[(w * ROWS + n * 16 + col) * 2 + 1] * exp2_raw(stats[(w * ROWS + n * 16 + col) * 2] - ref);
-            const float f = exp2_raw(m[n] - ref);
-            top[n] = t;
-            total[n] = sum;
-#pragma unroll
-            for (int i = 0; i < CH * 4; ++i) o[n][i] *= f;
-        }
-        // halves of the waves are added, over and over
-        for (int half = WAVES / 2; half > 0; half /= 2) {
-            if (half < WAVES / 2) __syncthreads();
-            if (wave >= half && wave < 2 * half) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < CH * 4; ++i)
-                        *reinterpret_cast<f32x4*>(slots + (((wave - half) * NT + n) * (CH * 4) + i) * 256 + lane * 4) = o[n][i];
-            }
-            __syncthreads();
-            if (wave < half) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < CH * 4; ++i)
-                        o[n][i] += *reinterpret_cast<const f32x4*>(slots + ((wave * NT + n) * (CH * 4) + i) * 256 + lane * 4);
-            }
-        }
-        if (wave != 0) return;
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (row_of[n] < 0) continue;
-        const long long rh = row_of[n] * p.q_heads + head_of[n];
-        if (p.splits > 1) {
-            float* part = p.part + (rh * p.splits + split) * dim;
-#pragma unroll
-            for (int i = 0; i < CH * 4; ++i)
-                if (i * 16 < dim) *reinterpret_cast<f32x4*>(part + i * 16 + grp * 4) = o[n][i];
-            if (grp == 0) {
-                float* st = p.part + p.part_stats + (rh * p.splits + split) * 2;
-                st[0] = top[n];
-                st[1] = total[n];
-            }
-            continue;
-        }
-        const float inv = total[n] == 0.f ? 0.f : 1.f / total[n];
-        const long long to = row_of[n] * p.out.row_stride + head_of[n] * p.out.head_stride + grp * 4;
+        const float total = sum_over_groups(l[n]);
+        if (grp == 0) *reinterpret_cast<f32x2*>(stats + (wave * ROWS + n * 16 + col) * 2) = (f32x2){ref[n], total};
 #pragma unroll
         for (int i = 0; i < CH * 4; ++i)
-            if (i * 16 < dim) {
-                const f32x4 r = o[n][i] * inv;
-                if (p.out.quads) store_elem4<TYPE>(p.out.data, to + i * 16, r);
-                else
+            sums[((wave * NT + n) * (CH * 4) + i) * 64 + grp * 16 + ((col + 4 * i + grp) & 15)] = o[n][i];
+    }
+    __syncthreads();
+    const int quads = dim / 4, rows_here = rows_all - row0 < ROWS ? rows_all - row0 : ROWS;
+    for (int at = threadIdx.x; at < rows_here * quads; at += 64 * WAVES) {
+        const int rr = at / quads, d = at - rr * quads;         // row of the tile, its elements 4 d ..
+        f32x2 st[WAVES];
+        float now = kNoRef, total = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) store_elem<TYPE>(p.out.data, to + i * 16 + j, r[j]);
-            }
-        if (p.lse && grp == 0) p.lse[rh] = total[n] == 0.f ? -INFINITY : (top[n] + __log2f(total[n])) * 0.69314718055994531f;
+        for (int w = 0; w < WAVES; ++w) {
+            st[w] = *reinterpret_cast<const f32x2*>(stats + (w * ROWS + rr) * 2);
+            now = fmaxf(now, st[w][0]);
+        }
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = exp2_raw(st[w][0] - now);
+            total += st[w][1] * f;
+            acc += sums[((w * NT + rr / 16) * (CH * 4) + d / 4) * 64 + (d & 3) * 16 + ((rr + d) & 15)] * f;
+        }
+        if (slot >= 0) {
+            const long long to = static_cast<long long>(slot) * ROWS + rr;
+            *reinterpret_cast<f32x4*>(p.part + to * dim + 4 * d) = acc;
+            if (d == 0) *reinterpret_cast<f32x2*>(p.stats + to * 2) = (f32x2){now, total};
+            continue;
+        }
+        const RowPlace r = row_place(p, range, len, head, row0 + rr, rows_all);
+        store_row4<TYPE>(p.out, r.row * p.out.row_stride + r.head * p.out.head_stride + 4 * d, acc * (total == 0.f ? 0.f : 1.f / total));
+        if (p.lse && d == 0) p.lse[r.row * p.q_heads + r.head] = log_sum(now, total);
+    }
     }
 }
 
-// The splits of a row's tokens, joined: 16 lanes a row and head, elements 4 lane, 4 lane + 64, ..
-template <int TYPE>
+// Units whose steps went to several workgroups, joined: a workgroup per row of a unit.  LANES lanes hold 4 elements each of one
+// piece, so 256 / LANES pieces are read at once.
+template <int TYPE, int ROWS, int LANES>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendParams p, int tile_rows) {
-    const long long rh = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) >> 4;
-    const int lane = threadIdx.x & 15;
-    if (rh >= static_cast<long long>(p.ragged.rows) * p.q_heads) return;
-    const int row = static_cast<int>(rh / p.q_heads), head = static_cast<int>(rh - static_cast<long long>(row) * p.q_heads);
-    // the row's sequence
-    const int seqs = p.units / (p.cache.heads * p.splits);
-    int seq;
-    if (!p.ragged.starts) {
-        seq = row / p.ragged.max_rows;
-    } else {
-        int a = 0, e = seqs;                                    // last sequence that starts at or before the row
-        while (e - a > 1) {
-            const int mid = (a + e) / 2;
-            if (p.ragged.starts[mid] <= row) a = mid; else e = mid;
-        }
-        seq = a;
-    }
-    const int2 range = p.ragged.range(seq);
-    const int i = row - range.x;
-    if (i < 0 || i >= range.y) return;                          // a row of no sequence
-    const int len = p.cache.length(seq), pos0 = len - range.y;
-    // the tile of rows that it was computed in
-    const int tile = (i * p.group + head % p.group) / tile_rows;
-    const int last = (tile + 1) * tile_rows < range.y * p.group ? (tile + 1) * tile_rows : range.y * p.group;
-    const TokenSpan span = token_span(p, len, pos0 + tile * tile_rows / p.group, pos0 + (last - 1) / p.group);
-    const int n = active_splits(p, span);
-    const float* st = p.part + p.part_stats + rh * p.splits * 2;
-    float top = -INFINITY;
-    for (int k = 0; k < n; ++k) top = fmaxf(top, st[2 * k]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float total = 0.f;
-    for (int k = 0; k < n; ++k) total += st[2 * k + 1] * exp2_raw(st[2 * k] - ref);
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    const float* part = p.part + rh * p.splits * p.cache.dim;
-    for (int d = lane * 4; d < p.cache.dim; d += 64) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < n; ++k)
-            acc += *reinterpret_cast<const f32x4*>(part + static_cast<long long>(k) * p.cache.dim + d) * exp2_raw(st[2 * k] - ref);
-        acc *= inv;
-        const long long to = row * p.out.row_stride + head * p.out.head_stride + d;
-        if (p.out.quads) store_elem4<TYPE>(p.out.data, to, acc);
-        else
+    constexpr int GROUPS = 256 / LANES;
+    __shared__ f32x4 sums[256];
+    const int unit = blockIdx.x / tile_rows, rr = blockIdx.x - unit * tile_rows;
+    const int tile = unit % p.row_tiles, head = unit / p.row_tiles % p.cache.heads, seq = unit / p.row_tiles / p.cache.heads;
+    const SeqWork work = seq_work<ROWS>(p, seq);
+    const int rows_all = work.range.y * p.group;
+    if (tile * ROWS + rr >= rows_all) return;
+    // pieces: the second slot of share w0, then the first ones of w0 + 1 .. w1
+    const int w0 = p.owners[2 * unit], n = p.owners[2 * unit + 1] - w0 + 1;
+    if (n == 1) return;                                         // in one piece: the output is there
+    auto at = [&](int k) { return static_cast<long long>(k == 0 ? 2 * w0 + 1 : 2 * (w0 + k)) * ROWS + rr; };
+    const f32x2* stats = reinterpret_cast<const f32x2*>(p.stats);
+    const int lane = threadIdx.x & 63, dim = p.cache.dim;
+    float ref = kNoRef;
+    for (int k = lane; k < n; k += 64) ref = fmaxf(ref, stats[at(k)][0]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) store_elem<TYPE>(p.out.data, to + j, acc[j]);
-    }
-    if (p.lse && lane == 0) p.lse[rh] = total == 0.f ? -INFINITY : (top + __log2f(total)) * 0.69314718055994531f;
+    for (int d = 32; d > 0; d /= 2) ref = fmaxf(ref, __shfl_xor(ref, d));
+    float total = 0.f;
+    for (int k = lane; k < n; k += 64) total += stats[at(k)][1] * exp2_raw(stats[at(k)][0] - ref);
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) total += __shfl_xor(total, d);
+    const int g = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (d < dim)
+#pragma unroll 4
+        for (int k = g; k < n; k += GROUPS) acc += *reinterpret_cast<const f32x4*>(p.part + at(k) * dim + d) * exp2_raw(stats[at(k)][0] - ref);
+    sums[threadIdx.x] = acc;
+    __syncthreads();
+    if (g != 0 || d >= dim) return;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) acc += sums[k * LANES + threadIdx.x];
+    const RowPlace place = row_place(p, work.range, work.len, head, tile * ROWS + rr, rows_all);
+    store_row4<TYPE>(p.out, place.row * p.out.row_stride + place.head * p.out.head_stride + d, acc * (total == 0.f ? 0.f : 1.f / total));
+    if (p.lse && threadIdx.x == 0) p.lse[place.row * p.q_heads + place.head] = log_sum(ref, total);
 }
 
 }  // namespace biq

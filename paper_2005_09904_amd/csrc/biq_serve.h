@@ -13,8 +13,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kCacheBlock = BIQ_CACHE_BLOCK;
 
@@ -114,22 +114,24 @@ __device__ __forceinline__ float code_value(uint32_t w) {
         return __builtin_amdgcn_cvt_f32_fp8(w, I);
 }
 
-// 8 codes as 8 bf16 values: both formats fit bf16's 8 bits of significand.
+// 8 codes as 8 16-bit floats (exact).
 template <int FMT>
-__device__ __forceinline__ bf16x8 codes_bf16(uint32_t a, uint32_t b) {
-    union { bf16x8 v; uint32_t w[4]; } r;
+__device__ __forceinline__ f16x8 codes_f16(uint32_t a, uint32_t b) {
+    union { f16x8 v; f16x2 p[4]; uint32_t w[4]; } r;
     if constexpr (FMT == BIQ_CACHE_INT8) {
-        // the upper halves of two floats (exact: integers below 2^8)
-        r.w[0] = __builtin_amdgcn_perm(__float_as_uint(code_value<FMT, 1>(a)), __float_as_uint(code_value<FMT, 0>(a)), 0x07060302);
-        r.w[1] = __builtin_amdgcn_perm(__float_as_uint(code_value<FMT, 3>(a)), __float_as_uint(code_value<FMT, 2>(a)), 0x07060302);
-        r.w[2] = __builtin_amdgcn_perm(__float_as_uint(code_value<FMT, 1>(b)), __float_as_uint(code_value<FMT, 0>(b)), 0x07060302);
-        r.w[3] = __builtin_amdgcn_perm(__float_as_uint(code_value<FMT, 3>(b)), __float_as_uint(code_value<FMT, 2>(b)), 0x07060302);
+        // 0x6400 + u is 1024 + u: of the code + 128 as an unsigned byte
+        const uint32_t ua = a ^ 0x80808080u, ub = b ^ 0x80808080u;
+        r.w[0] = __builtin_amdgcn_perm(0x64646464u, ua, 0x04010400u);
+        r.w[1] = __builtin_amdgcn_perm(0x64646464u, ua, 0x04030402u);
+        r.w[2] = __builtin_amdgcn_perm(0x64646464u, ub, 0x04010400u);
+        r.w[3] = __builtin_amdgcn_perm(0x64646464u, ub, 0x04030402u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.p[i] -= (f16x2){1152.0f16, 1152.0f16};
     } else {
-        union { bf16x2 v; uint32_t w; } t;
-        t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false); r.w[0] = t.w;
-        t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);  r.w[1] = t.w;
-        t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false); r.w[2] = t.w;
-        t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);  r.w[3] = t.w;
+        r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
+        r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
+        r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false);
+        r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
     }
     return r.v;
 }

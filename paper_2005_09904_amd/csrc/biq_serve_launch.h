@@ -8,12 +8,10 @@
 
 namespace biq {
 
-// What the planner chooses for attention: tiles of 16 rows per wave.
-struct AttendShape { int nt, waves; };
-
-hipError_t launch_attend_f32(int fmt, int chunks, AttendShape shape, const AttendParams& p, hipStream_t s);
-hipError_t launch_attend_bf16(int fmt, int chunks, AttendShape shape, const AttendParams& p, hipStream_t s);
-hipError_t launch_attend_f16(int fmt, int chunks, AttendShape shape, const AttendParams& p, hipStream_t s);
+// (nt: tiles of 16 rows per wave)
+hipError_t launch_attend_f32(int fmt, int nt, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_bf16(int fmt, int nt, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_f16(int fmt, int nt, const AttendParams& p, hipStream_t s);
 
 // (chunks: 64 elements of a head each)
 hipError_t launch_append(int type, int fmt, int chunks, const AppendParams& p, hipStream_t s);

@@ -68,8 +68,9 @@ int chunks_of(int head_dim) { return (head_dim + 63) / 64; }
 // ---- attention: how a call is mapped ----------------------------------------------------------------------
 
 struct AttendPlan {
-    AttendShape shape;
-    int row_tiles, splits, split_tokens;
+    int nt;                  // tiles of 16 rows per wave
+    long long row_tiles;
+    int shares;              // workgroups that share all steps; 0: a workgroup per unit
     size_t workspace;
 };
 
@@ -85,23 +86,23 @@ biq_status attend_check(const biq_attention_args* a) {
 AttendPlan attend_plan(const biq_attention_args& a) {
     AttendPlan pl{};
     const biq_cache& c = a.cache;
-    const int group = a.q_heads / c.heads, waves = chunks_of(c.head_dim) <= 2 ? 8 : 4;
-    pl.shape = {1, waves};
-    pl.row_tiles = static_cast<int>((static_cast<long long>(a.ragged.max_rows) * group + 15) / 16);
-    long long span = static_cast<long long>(c.table_stride) * c.page_tokens;
-    if (a.max_len > 0 && a.max_len < span) span = a.max_len;
+    const long long rows = static_cast<long long>(a.ragged.max_rows) * (a.q_heads / c.heads);      // of a sequence and head
+    pl.nt = rows <= 16 || chunks_of(c.head_dim) > 2 ? 1 : 2;
+    const int tile = 16 * pl.nt;
+    pl.row_tiles = (rows + tile - 1) / tile;
+    const long long room = static_cast<long long>(c.table_stride) * c.page_tokens;
+    long long span = a.max_len > 0 ? a.max_len : room;
     if (a.window > 0 && static_cast<long long>(a.window) + a.ragged.max_rows + 64 < span) span = static_cast<long long>(a.window) + a.ragged.max_rows + 64;
-    // one workgroup per CU at least, no split below one step of its waves
     const long long units = static_cast<long long>(c.seqs) * c.heads * pl.row_tiles;
-    const int step = 64 * waves;
-    long long splits = (kCus + units - 1) / units;
-    const long long most = (span + step - 1) / step;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    pl.split_tokens = static_cast<int>((span + splits * step - 1) / (splits * step) * step);
-    pl.splits = static_cast<int>((span + pl.split_tokens - 1) / pl.split_tokens);
-    if (pl.splits > 1)
-        pl.workspace = static_cast<size_t>(a.ragged.rows) * a.q_heads * pl.splits * (c.head_dim + 2) * 4;
+    // Lengths are not known here, so a unit per workgroup is only taken where a unit is short: up to 8 steps (77 tokens, 8 units: 6.6 us
+    // instead of 10.2: the join is a launch of its own), or 32 where there is a unit for every CU.  Beyond, one workgroup per
+    // CU shares the steps (32 sequences of 410 .. 4096 tokens, 8 heads: 43 us instead of 46).
+    // Two per CU are slower (58) as there are more pieces.
+    const long long steps = (span + 63) / 64;
+    if (steps > (units >= kCus ? 32 : 8) && units < 16 * kCus && units * (room / 64 + 1 + kUnitCost) < kMaxInt) {
+        pl.shares = units * steps < kCus ? static_cast<int>(units * steps) : kCus;
+        pl.workspace = static_cast<size_t>(pl.shares) * 2 * tile * (c.head_dim + 2) * 4 + static_cast<size_t>(units) * 8;
+    }
     return pl;
 }
 
@@ -224,21 +225,20 @@ biq_status biq_attention(const biq_attention_args* a, void* workspace, size_t wo
     p.group = a->q_heads / a->cache.heads;
     p.causal = a->causal != 0;
     p.window = a->window;
-    p.splits = pl.splits;
-    p.split_tokens = pl.split_tokens;
-    p.row_tiles = pl.row_tiles;
-    p.scale = a->scale * 1.4426950408889634f;
+    p.seqs = a->cache.seqs;
+    p.shares = pl.shares;
+    p.negative = a->scale < 0.f;
+    p.scale = fabsf(a->scale) * 1.4426950408889634f;
     p.part = static_cast<float*>(workspace);
-    p.part_stats = static_cast<long long>(a->ragged.rows) * a->q_heads * pl.splits * a->cache.head_dim;
-    const long long units = static_cast<long long>(a->cache.seqs) * a->cache.heads * pl.splits;
-    if (units > kMaxInt - 8 || (units + 8) * pl.row_tiles > kMaxInt) return BIQ_EUNSUPPORTED;
-    p.units = static_cast<int>(units);
-    const int chunks = chunks_of(a->cache.head_dim);
+    p.stats = p.part + static_cast<size_t>(pl.shares) * 2 * 16 * pl.nt * a->cache.head_dim;
+    p.owners = reinterpret_cast<int*>(p.stats + static_cast<size_t>(pl.shares) * 2 * 16 * pl.nt * 2);
+    if (static_cast<long long>(a->cache.seqs) * a->cache.heads * pl.row_tiles > kMaxInt) return BIQ_EUNSUPPORTED;
+    p.row_tiles = static_cast<int>(pl.row_tiles);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     switch (a->type) {
-        case BIQ_F32: return status(launch_attend_f32(a->cache.format, chunks, pl.shape, p, s));
-        case BIQ_BF16: return status(launch_attend_bf16(a->cache.format, chunks, pl.shape, p, s));
-        default: return status(launch_attend_f16(a->cache.format, chunks, pl.shape, p, s));
+        case BIQ_F32: return status(launch_attend_f32(a->cache.format, pl.nt, p, s));
+        case BIQ_BF16: return status(launch_attend_bf16(a->cache.format, pl.nt, p, s));
+        default: return status(launch_attend_f16(a->cache.format, pl.nt, p, s));
     }
 }
 

@@ -234,3 +234,17 @@ def test_offsets_beyond_32_bits(biq):
     for rows in (1, 40):
         q = torch.randn((rows, 16, dim), device="cuda:0")
         assert torch.equal(call(biq, cache, q, max_len=1024)[0], call(biq, pages.on(biq), q, max_len=1024)[0])
+
+
+@pytest.mark.parametrize("seqs,new", [(70, 1), (130, 1), (66, 9)])
+def test_many_sequences_share_the_work(biq, seqs, new):
+    """More sequences than lanes, lengths from none to many: places, pieces and their joining."""
+    rng = np.random.default_rng(seqs)
+    lens = [int(n) for n in rng.choice([0, 1, 30, 64, 65, 200, 640, 1500], size=seqs)]
+    counts = [0 if s % 11 == 5 else int(rng.integers(1, new + 1)) for s in range(seqs)]
+    check(biq, su.filled(lens, 1, 32, 64, "int8", seqs), counts, "fp32", 2, seqs, max_len=1500)
+
+
+def test_one_long_sequence_is_shared(biq):
+    check(biq, su.filled([9000], 1, 32, 256, "int8", 1), [1], "fp32", 3, 1, uniform=True)
+    check(biq, su.filled([9000, 0, 17], 1, 32, 256, "fp8", 1), [6, 1, 2], "bf16", 3, 1, window=5000)
