@@ -288,34 +288,62 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v
     sum = __builtin_fmaf(sum, keep, part);
 }
 
-// The four blocks of a step of 64 tokens.  The step is the same for all lanes, so the pages are looked up with scalar loads:
-// a vector load would wait its turn behind all codes that were requested before it.
-struct StepPages {
-    long long offset[4], scale[4];       // bytes of the block's keys and of their scale (of page 0 where there is no page)
-    int valid[4];                        // tokens of the block
-    template <typename T>
-    static __device__ __forceinline__ T of(const T (&x)[4], int block) {
-        const T a = block & 1 ? x[1] : x[0], b = block & 1 ? x[3] : x[2];
-        return block & 2 ? b : a;
-    }
+// Where a lane finds the codes of a step of 64 tokens (4 blocks): keys of block kblock, values and scales of block vblock.  The
+// step is the same for all lanes, so pages are looked up with scalar loads: a vector load would wait its turn behind all
+// codes that were requested before it.  Blocks without a page point to page 0, and have no valid tokens.
+struct StepPlace {
+    const uint8_t* keys;
+    const uint8_t* values;
+    const float* scales;     // of the keys; of the values: heads * page_blocks further
+    int valid;               // tokens of vblock that the sequence has
+    bool all;                // the sequence has all 64
 };
-__device__ __forceinline__ StepPages step_pages(const Cache& c, int dim, int seq, int head, int t0, int len) {
+__device__ __forceinline__ StepPlace step_place(const Cache& c, int dim, int seq, int head, int t0, int len, int kblock, int vblock) {
     typedef const __attribute__((address_space(4))) int* ScalarInts;
     const ScalarInts table = (ScalarInts)(c.table + static_cast<long long>(seq) * c.table_stride);
-    const long long codes = static_cast<long long>(c.heads) * c.page_blocks * kCacheBlock * dim;
-    StepPages s;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int b = (t0 >> 4) + j, i = c.page_index(b);
+    const int block_bytes = kCacheBlock * dim, b0 = t0 >> 4;
+    const long long codes = static_cast<long long>(c.heads) * c.page_blocks * block_bytes;
+    auto lookup = [&](int i) {
         const int n = table[i < c.table_stride ? i : 0];
-        const bool there = i < c.table_stride && static_cast<uint32_t>(n) < static_cast<uint32_t>(c.num_pages);
-        const long long page = (there ? n : 0) * c.page_bytes;
-        const int block = c.block_in_page(b, head);
-        const int left = there ? len - b * kCacheBlock : 0;
-        s.valid[j] = left < 0 ? 0 : left > kCacheBlock ? kCacheBlock : left;
-        s.offset[j] = page + static_cast<long long>(block) * (kCacheBlock * dim);
-        s.scale[j] = page + 2 * codes + 4ll * block;
+        return i < c.table_stride && static_cast<uint32_t>(n) < static_cast<uint32_t>(c.num_pages) ? n : -1;
+    };
+    StepPlace s;
+    int left;
+    if ((c.page_blocks & 3) == 0) {                             // one page
+        const int i = c.page_index(b0), n = lookup(i);
+        const int block = head * c.page_blocks + (b0 - i * c.page_blocks);
+        const uint8_t* page = c.store + (n < 0 ? 0 : n) * c.page_bytes;
+        const uint8_t* first = page + static_cast<long long>(block) * block_bytes;
+        s.keys = first + static_cast<uint32_t>(kblock * block_bytes);
+        s.values = first + codes + static_cast<uint32_t>(vblock * block_bytes);
+        s.scales = reinterpret_cast<const float*>(page + 2 * codes + 4ll * block) + static_cast<uint32_t>(vblock);
+        s.all = n >= 0 && len - t0 >= 64;
+        left = n < 0 ? 0 : len - t0 - vblock * kCacheBlock;
+    } else {
+        long long code_at[4], scale_at[4];
+        int end[4];
+        s.all = len - t0 >= 64;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = c.page_index(b0 + j), n = lookup(i);
+            const int block = head * c.page_blocks + (b0 + j - i * c.page_blocks);
+            const long long page = (n < 0 ? 0 : n) * c.page_bytes;
+            code_at[j] = page + static_cast<long long>(block) * block_bytes;
+            scale_at[j] = page + 2 * codes + 4ll * block;
+            end[j] = n < 0 ? 0 : len - (b0 + j) * kCacheBlock;
+            s.all = s.all && n >= 0;
+        }
+        // (by value: a choice between elements of an array would put the array into memory)
+        auto of = [](auto x0, auto x1, auto x2, auto x3, int block) {
+            const auto a = block & 1 ? x1 : x0, b = block & 1 ? x3 : x2;
+            return block & 2 ? b : a;
+        };
+        s.keys = c.store + of(code_at[0], code_at[1], code_at[2], code_at[3], kblock);
+        s.values = c.store + codes + of(code_at[0], code_at[1], code_at[2], code_at[3], vblock);
+        s.scales = reinterpret_cast<const float*>(c.store + of(scale_at[0], scale_at[1], scale_at[2], scale_at[3], vblock));
+        left = of(end[0], end[1], end[2], end[3], vblock);
     }
+    s.valid = left < 0 ? 0 : left > kCacheBlock ? kCacheBlock : left;
     return s;
 }
 
@@ -403,22 +431,22 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     float ks = 0.f, vs = 0.f;
     const uint8_t* vbase = p.cache.store;
     int valid = 0;
+    bool all_valid = false;
     auto request_keys = [&](int t0) {
-        const StepPages at = step_pages(p.cache, dim, seq, head, t0, len);
-        const uint8_t* kbase = p.cache.store + at.of(at.offset, kblock);
-        vbase = p.cache.store + codes + at.of(at.offset, grp);
-        const uint8_t* scales = p.cache.store + at.of(at.scale, grp);
-        valid = at.of(at.valid, grp);
+        const StepPlace at = step_place(p.cache, dim, seq, head, t0, len, kblock, grp);
+        vbase = at.values;
+        valid = at.valid;
+        all_valid = at.all;
         // (scales of blocks that do not exist are not used, whatever they are)
-        ks = *reinterpret_cast<const float*>(scales);
-        vs = reinterpret_cast<const float*>(scales)[p.cache.heads * p.cache.page_blocks];
+        ks = at.scales[0];
+        vs = at.scales[p.cache.heads * p.cache.page_blocks];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 int d = c * 64 + grp * 16;
                 d = FULL || d < dim ? d : 0;                    // (against zeros of q)
-                kc[t][c] = *reinterpret_cast<const u32x4*>(kbase + (4 * t + (col & 3)) * dim + d);
+                kc[t][c] = *reinterpret_cast<const u32x4*>(at.keys + (4 * t + (col & 3)) * dim + d);
             }
     };
     int t0 = begin + __builtin_amdgcn_readfirstlane(wave) * 64;
@@ -450,6 +478,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         }
         const float kscale = ks, vscale = vs;
         const int nvalid = valid;
+        const bool step_valid = all_valid;
         __builtin_amdgcn_sched_barrier(0);                      // (the requests stay ahead of the products)
         f32x4 s[NT][4];
 #pragma unroll
@@ -475,7 +504,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         request_keys(t0 + 64 * WAVES < end ? t0 + 64 * WAVES : t0);
         __builtin_amdgcn_sched_barrier(0);
 
-        const bool whole = t0 + 63 <= all_hi && t0 >= all_lo && __all(nvalid == kCacheBlock);
+        const bool whole = step_valid && t0 + 63 <= all_hi && t0 >= all_lo;
         if (!whole) {
 #pragma unroll
             for (int t = 0; t < CH * 4; ++t) vc[t] = first_codes(vc[t], nvalid);
@@ -548,6 +577,197 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         store_row4<TYPE>(p.out, r.row * p.out.row_stride + r.head * p.out.head_stride + 4 * d, acc * (total == 0.f ? 0.f : 1.f / total));
         if (p.lse && d == 0) p.lse[r.row * p.q_heads + r.head] = log_sum(now, total);
     }
+    }
+}
+
+// Order of READS operands from LDS and the EACH products of every one of them: four reads ahead.  (Left alone, the compiler
+// reads each operand right before its products and waits for it.)
+template <int READS, int EACH>
+__device__ __forceinline__ void read_ahead() {
+    constexpr int kReads = 0x100, kProducts = 0x8;
+    __builtin_amdgcn_sched_group_barrier(kReads, 4, 0);
+#pragma unroll
+    for (int i = 0; i < READS - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kProducts, EACH, 0);
+        __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kProducts, 4 * EACH, 0);
+}
+
+// Many rows of a sequence and head (prompts).  The waves of a workgroup hold different rows, NT tiles of 16 each, and share the
+// tokens: a step's 64 are requested a step ahead, each code by one wave, and laid down in LDS as the 16-bit operands that all
+// waves read, in the order of the lanes that read them (lane after lane: no bank is met twice).  Two buffers, one barrier
+// a step.
+template <int TYPE, int FMT, int CH, bool FULL, int NT>
+__global__ __launch_bounds__(256, CH <= 2 ? 2 : 1) void attend_tile_kernel(const AttendParams p) {
+    constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE>::value;
+    constexpr int WAVES = 4, ROWS = 16 * NT * WAVES;
+    constexpr int HALF = 8 * CH * 64;                           // operands of the keys; as many of the values
+    extern __shared__ float lds[];
+    f16x8* buffers = reinterpret_cast<f16x8*>(lds);             // [2][keys [4][CH][2], values [CH * 4][2]][64]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, grp = lane >> 4;
+    const int dim = FULL ? 64 * CH : p.cache.dim;
+    const long long codes = static_cast<long long>(p.cache.heads) * p.cache.page_blocks * kCacheBlock * dim;
+    // Later rows see more tokens and come first.  Where the sequences and heads can be dealt to the XCDs evenly, each keeps to
+    // its own, whose tokens then stay in its L2.
+    const int pairs = p.seqs * p.cache.heads;
+    int pair, tile;
+    if (pairs % kXcds == 0) {
+        const int at = blockIdx.x / kXcds;
+        pair = at / p.row_tiles * kXcds + blockIdx.x % kXcds;
+        tile = p.row_tiles - 1 - at % p.row_tiles;
+    } else {
+        pair = blockIdx.x % pairs;
+        tile = p.row_tiles - 1 - blockIdx.x / pairs;
+    }
+    const int seq = pair / p.cache.heads, head = pair - seq * p.cache.heads;
+    const int2 range = p.ragged.range(seq);
+    const int len = p.cache.length(seq);
+    const int rows_all = range.y * p.group, row0 = tile * ROWS;
+    if (row0 >= rows_all) return;
+    const int pos0 = len - range.y;
+    const int last_row = (row0 + ROWS < rows_all ? row0 + ROWS : rows_all) - 1;
+    int begin = p.window > 0 ? pos0 + row0 / p.group - p.window + 1 : 0;
+    begin = begin < 0 ? 0 : begin & ~63;
+    const int end = p.causal ? pos0 + last_row / p.group + 1 : len;
+
+    // this wave's rows
+    RowPlace place[NT];
+    f16x8 q[NT][CH][2][QT];
+    float unit_of[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        place[n] = row_place(p, range, len, head, row0 + (wave * NT + n) * 16 + col, rows_all);
+        float x[CH][2][8];
+        load_row<TYPE, CH>(p, place[n], dim, grp, x);
+        unit_of[n] = row_terms<TYPE, CH>(p.negative, x, q[n]) * p.scale;
+    }
+    // what all and what some of them see
+    const int wave_row = row0 + wave * NT * 16;
+    const int wave_last = wave_row + NT * 16 < rows_all ? wave_row + NT * 16 - 1 : rows_all - 1;
+    const int pos_first = pos0 + wave_row / p.group, pos_last = pos0 + wave_last / p.group;
+    const int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0, all_hi = p.causal ? pos_first : len - 1;
+    const int any_lo = p.window > 0 ? pos_first - p.window + 1 : 0, any_hi = wave_row < rows_all ? p.causal ? pos_last : len - 1 : -1;
+
+    // this wave's part of a step: key rows of tile `wave`, values of CH tiles of 16 elements
+    u32x4 kc[CH], vc[CH];
+    float ks, vs;
+    int valid;
+    bool all_valid;
+    auto request = [&](int t0) {
+        const StepPlace at = step_place(p.cache, dim, seq, head, t0, len, col >> 2, grp);
+        valid = at.valid;
+        all_valid = at.all;
+        ks = at.scales[0];
+        vs = at.scales[p.cache.heads * p.cache.page_blocks];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int kd = c * 64 + grp * 16, vd = (wave * CH + c) * 16;
+            kc[c] = *reinterpret_cast<const u32x4*>(at.keys + (4 * wave + (col & 3)) * dim + (FULL || kd < dim ? kd : 0));
+            vc[c] = *reinterpret_cast<const u32x4*>(at.values + ((FULL || vd < dim ? vd : 0) + col) * kCacheBlock);
+        }
+    };
+    auto lay_down = [&](f16x8* to) {
+        if (!all_valid) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) vc[c] = first_codes(vc[c], valid);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                to[((wave * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(kc[c][2 * h], kc[c][2 * h + 1]);
+                to[HALF + ((wave * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(vc[c][2 * h], vc[c][2 * h + 1]);
+            }
+    };
+
+    f32x4 o[NT][CH * 4];
+    float ref[NT], l[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        ref[n] = kNoRef;
+        l[n] = 0.f;
+#pragma unroll
+        for (int t = 0; t < CH * 4; ++t) o[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    if (begin < end) {
+        request(begin);
+        lay_down(buffers);
+        __syncthreads();
+    }
+    int parity = 0;
+    for (int t0 = begin; t0 < end; t0 += 64) {
+        const float kscale = ks, vscale = vs;
+        const int nvalid = valid;
+        const bool step_valid = all_valid;
+        const f16x8* from = buffers + parity * 2 * HALF;
+        parity ^= 1;
+        request(t0 + 64 < end ? t0 + 64 : t0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t0 <= any_hi && t0 + 63 >= any_lo) {
+            f32x4 s[NT][4];
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const f16x8 k = from[((t * CH + c) * 2 + h) * 64 + lane];
+#pragma unroll
+                        for (int e = 0; e < QT; ++e)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[n][c][h][e], s[n][t], 0, 0, 0);
+                    }
+            }
+            read_ahead<8 * CH, QT * NT>();
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool whole = step_valid && t0 + 63 <= all_hi && t0 >= all_lo;
+            f16x8 w[NT][2][PT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                bool grown;
+                float keep;
+                const Sight see = {place[n].lo, place[n].hi, t0 + grp * kCacheBlock, nvalid};
+                weigh<PT>(s[n], kscale * unit_of[n], vscale, whole, see, ref[n], l[n], grown, keep, w[n]);
+                if (grown) {
+#pragma unroll
+                    for (int t = 0; t < CH * 4; ++t) o[n][t] *= keep;
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int t = 0; t < CH * 4; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f16x8 v = from[HALF + (t * 2 + h) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < PT; ++e)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[n][h][e], o[n][t], 0, 0, 0);
+                }
+            read_ahead<8 * CH, PT * NT>();
+            __builtin_amdgcn_s_setprio(0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        lay_down(buffers + parity * 2 * HALF);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const float total = sum_over_groups(l[n]);
+        if (place[n].row < 0) continue;
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const long long to = place[n].row * p.out.row_stride + place[n].head * p.out.head_stride + grp * 4;
+#pragma unroll
+        for (int i = 0; i < CH * 4; ++i)
+            if (FULL || i * 16 < dim) store_row4<TYPE>(p.out, to + i * 16, o[n][i] * inv);
+        if (p.lse && grp == 0) p.lse[place[n].row * p.q_heads + place[n].head] = log_sum(ref[n], total);
     }
 }
 

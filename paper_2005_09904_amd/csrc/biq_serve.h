@@ -58,11 +58,12 @@ struct Cache {
     long long page_bytes;
     int num_pages, table_stride, heads, dim;
     int page_blocks;         // blocks per page, 1 .. 16
-    uint32_t page_magic;     // floor(2^32 / page_blocks) + 1 (page_blocks > 1)
+    uint32_t page_magic;     // floor(2^32 / page_blocks) + 1, its low 32 bits ..
+    uint32_t page_ones;      // .. and all ones where there is a 33rd (page_blocks = 1)
 
     // b / page_blocks for b < 2^27: the product is off by less than 2^27 * 16 < 2^32
     __device__ __forceinline__ int page_index(int b) const {
-        return page_blocks == 1 ? b : static_cast<int>(__umulhi(static_cast<uint32_t>(b), page_magic));
+        return static_cast<int>(__umulhi(static_cast<uint32_t>(b), page_magic) + (static_cast<uint32_t>(b) & page_ones));
     }
     __device__ __forceinline__ int length(int s) const {
         const long long most = static_cast<long long>(table_stride) * page_blocks * kCacheBlock;

@@ -47,7 +47,8 @@ Cache cache_of(const biq_cache& c) {
     d.heads = c.heads;
     d.dim = c.head_dim;
     d.page_blocks = c.page_tokens / kCacheBlock;
-    d.page_magic = d.page_blocks > 1 ? static_cast<uint32_t>((1ull << 32) / d.page_blocks + 1) : 0;
+    d.page_magic = static_cast<uint32_t>((1ull << 32) / d.page_blocks + 1);
+    d.page_ones = d.page_blocks == 1 ? ~0u : 0u;
     return d;
 }
 
@@ -68,6 +69,7 @@ int chunks_of(int head_dim) { return (head_dim + 63) / 64; }
 // ---- attention: how a call is mapped ----------------------------------------------------------------------
 
 struct AttendPlan {
+    bool tiles;              // the kernel for many rows
     int nt;                  // tiles of 16 rows per wave
     long long row_tiles;
     int shares;              // workgroups that share all steps; 0: a workgroup per unit
@@ -87,18 +89,35 @@ AttendPlan attend_plan(const biq_attention_args& a) {
     AttendPlan pl{};
     const biq_cache& c = a.cache;
     const long long rows = static_cast<long long>(a.ragged.max_rows) * (a.q_heads / c.heads);      // of a sequence and head
-    pl.nt = rows <= 16 || chunks_of(c.head_dim) > 2 ? 1 : 2;
-    const int tile = 16 * pl.nt;
-    pl.row_tiles = (rows + tile - 1) / tile;
     const long long room = static_cast<long long>(c.table_stride) * c.page_tokens;
     long long span = a.max_len > 0 ? a.max_len : room;
     if (a.window > 0 && static_cast<long long>(a.window) + a.ragged.max_rows + 64 < span) span = static_cast<long long>(a.window) + a.ragged.max_rows + 64;
-    const long long units = static_cast<long long>(c.seqs) * c.heads * pl.row_tiles;
+    const long long steps = (span + 63) / 64, pairs = static_cast<long long>(c.seqs) * c.heads;
+
+    // Few rows or many: by the time of a step of 64 tokens (bf16, us; heads of 64, 128, 192, 256).  For few rows the CUs share the
+    // steps of all units: kRows each.  For many a workgroup walks through its steps alone: kAlone each, kShared where two of
+    // them are on a CU (one for heads above 128).  Measured for 8 heads of 4, 1 .. 16 sequences of 4 .. 512 rows over 1024 and
+    // 8192 tokens: 64 rows of 16 sequences and 8192 tokens 90 us by rows, 217 by tiles, 512 rows 660 and 318.
+    static const double kRows[4] = {0.46, 0.64, 0.95, 1.19}, kAlone[4] = {1.25, 1.64, 2.0, 2.27}, kShared[4] = {1.7, 2.4, 2.0, 2.27};
+    const int ch = chunks_of(c.head_dim) - 1;
+    const int few = rows <= 16 || ch > 1 ? 16 : 32, many = ch <= 1 ? 128 : 64;
+    const long long tiles = pairs * ((rows + many - 1) / many), slots = ch <= 1 ? 2 * kCus : kCus;
+    const double by_rows = static_cast<double>(pairs * ((rows + few - 1) / few)) / kCus * kRows[ch];
+    const double by_tiles = tiles <= kCus ? kAlone[ch] : kShared[ch] * static_cast<double>((tiles + slots - 1) / slots);
+    if (rows > 16 && by_tiles < by_rows) {
+        pl.tiles = true;
+        pl.nt = many / 64;
+        pl.row_tiles = (rows + many - 1) / many;
+        return pl;
+    }
+    pl.nt = few / 16;
+    const int tile = few;
+    pl.row_tiles = (rows + tile - 1) / tile;
+    const long long units = pairs * pl.row_tiles;
     // Lengths are not known here, so a unit per workgroup is only taken where a unit is short: up to 8 steps (77 tokens, 8 units: 6.6 us
     // instead of 10.2: the join is a launch of its own), or 32 where there is a unit for every CU.  Beyond, one workgroup per
     // CU shares the steps (32 sequences of 410 .. 4096 tokens, 8 heads: 43 us instead of 46).
     // Two per CU are slower (58) as there are more pieces.
-    const long long steps = (span + 63) / 64;
     if (steps > (units >= kCus ? 32 : 8) && units < 16 * kCus && units * (room / 64 + 1 + kUnitCost) < kMaxInt) {
         pl.shares = units * steps < kCus ? static_cast<int>(units * steps) : kCus;
         pl.workspace = static_cast<size_t>(pl.shares) * 2 * tile * (c.head_dim + 2) * 4 + static_cast<size_t>(units) * 8;
@@ -236,9 +255,9 @@ biq_status biq_attention(const biq_attention_args* a, void* workspace, size_t wo
     p.row_tiles = static_cast<int>(pl.row_tiles);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     switch (a->type) {
-        case BIQ_F32: return status(launch_attend_f32(a->cache.format, pl.nt, p, s));
-        case BIQ_BF16: return status(launch_attend_bf16(a->cache.format, pl.nt, p, s));
-        default: return status(launch_attend_f16(a->cache.format, pl.nt, p, s));
+        case BIQ_F32: return status(launch_attend_f32(a->cache.format, pl.tiles, pl.nt, p, s));
+        case BIQ_BF16: return status(launch_attend_bf16(a->cache.format, pl.tiles, pl.nt, p, s));
+        default: return status(launch_attend_f16(a->cache.format, pl.tiles, pl.nt, p, s));
     }
 }
 
