@@ -356,7 +356,7 @@ biq_status biq_gemm_noalloc(const uint8_t* K, const float* alpha, const float* X
  *     result is rounded once, to the output's type.
  *   - Infinities and NaN are values like others: they show in the results of the rows that depend on them, and in no others.
  *   - Rows of a tensor have strides of their own (biq_rows).  Elements of one head are adjacent.  Any alignment of the
- *     element's size is accepted; 16-byte aligned rows are faster.
+ *     element's size is accepted; rows at multiples of 4 bytes are faster (16 for biq_rotary).
  *   - What device memory says of lengths, pages and positions is not known to the host, and so is not refused: it is bounded
  *     on the device instead, as each operation describes.  No value of it leads outside the buffers described here.
  */

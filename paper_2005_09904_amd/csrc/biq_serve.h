@@ -31,19 +31,20 @@ __device__ __forceinline__ void store_elem(void* base, long long i, float x) {
     static_cast<typename Elem<TYPE>::T*>(base)[i] = static_cast<typename Elem<TYPE>::T>(x);
 }
 
-// 4 adjacent elements at an address aligned to all of them.
+// 4 adjacent elements at a multiple of 4 bytes (wide accesses to memory need no more).
 template <int TYPE>
 __device__ __forceinline__ f32x4 load_elem4(const void* base, long long i) {
-    typedef typename Elem<TYPE>::T V __attribute__((ext_vector_type(4)));
+    typedef typename Elem<TYPE>::T V __attribute__((ext_vector_type(4), aligned(4)));
     return __builtin_convertvector(*reinterpret_cast<const V*>(static_cast<const typename Elem<TYPE>::T*>(base) + i), f32x4);
 }
 template <int TYPE>
 __device__ __forceinline__ void store_elem4(void* base, long long i, f32x4 x) {
     typedef typename Elem<TYPE>::T V __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<V*>(static_cast<typename Elem<TYPE>::T*>(base) + i) = __builtin_convertvector(x, V);
+    typedef typename Elem<TYPE>::T Loose __attribute__((ext_vector_type(4), aligned(4)));
+    *reinterpret_cast<Loose*>(static_cast<typename Elem<TYPE>::T*>(base) + i) = __builtin_convertvector(x, V);
 }
 
-// biq_rows, with what the host has checked: quads = groups of 4 elements are aligned to their size.
+// biq_rows, with what the host has checked: quads = every 4th element lies at a multiple of 4 bytes.
 struct Rows {
     void* data;
     long long row_stride, head_stride;

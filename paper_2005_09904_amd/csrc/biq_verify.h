@@ -1,7 +1,7 @@
 // Verification of drafted tokens (biq_verify_drafts).
 //
-// The drawn token needs the sum of a row's weights before it needs their order, so a row of probabilities is read once in
-// parts for their sums, and the part where the goal lies once more.  Weights are integers (40 bits below the point), so that
+// The drawn token needs the sum of a row's weights before it needs their order, so a row of probabilities is read once, a
+// wave per span of 1024 tokens, for the spans' sums, and the span where the goal lies once more.  Weights are integers (40 bits below the point), so that
 // every order of additions gives the same sums and the same token.
 #pragma once
 
@@ -9,8 +9,8 @@
 
 namespace biq {
 
-constexpr int kVerifyThreads = 1024;
-constexpr int kVerifyPart = 4 * kVerifyThreads;      // tokens whose weights are summed into one number
+constexpr int kVerifySpan = 1024;                    // tokens whose weights are summed into one number
+constexpr int kVerifyThreads = 1024;                 // of the kernel that draws: 4 spans each, as 2^22 tokens have 4096
 
 struct VerifyParams {
     const void* p;
@@ -21,8 +21,9 @@ struct VerifyParams {
     const float* uniform;
     int* tokens;
     int* accepted;
-    unsigned long long* sums;    // [seqs][parts]
-    int seqs, drafts, vocab, parts;
+    unsigned long long* sums;    // [seqs][spans]
+    int* verdicts;               // [seqs][4] accepted drafts, the refused one's token, whether none was refused
+    int seqs, drafts, vocab, spans;
     int p_quads, q_quads;
 };
 
@@ -117,107 +118,127 @@ __device__ __forceinline__ unsigned long long sum_over_wave(unsigned long long x
     return x;
 }
 
-// Sum over the workgroup, in every thread.
-__device__ __forceinline__ unsigned long long sum_over_group(unsigned long long x, unsigned long long* lds) {
-    x = sum_over_wave(x);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    unsigned long long total = 0;
+__device__ __forceinline__ unsigned long long running_sum(unsigned long long x, int lane) {
 #pragma unroll
-    for (int w = 0; w < kVerifyThreads / 64; ++w) total += lds[w];
-    return total;
+    for (int d = 1; d < 64; d *= 2) {
+        const unsigned long long y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
 }
 
-// Sum of one part's weights: workgroup (sequence, part).
+// Sums of spans of weights, one per wave (workgroups of 4).  Every wave judges the drafts itself: it needs to know the row.
 template <int TYPE>
-__global__ __launch_bounds__(kVerifyThreads) void verify_sums_kernel(const VerifyParams p) {
-    __shared__ unsigned long long lds[kVerifyThreads / 64];
-    const int seq = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
-    const Verdict v = judge<TYPE>(p, seq, threadIdx.x & 63);
+__global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyParams p) {
+    const int lane = threadIdx.x & 63, groups = (p.spans + 3) / 4;
+    const int seq = blockIdx.x / groups, span = (blockIdx.x - seq * groups) * 4 + (threadIdx.x >> 6);
+    if (span >= p.spans) return;
+    const Verdict v = judge<TYPE>(p, seq, lane);
     const Source s = source_of(p, seq, v);
-    unsigned long long w[4];
-    weights4<TYPE>(p, s, part * kVerifyPart + 4 * static_cast<int>(threadIdx.x), w);
-    const unsigned long long total = sum_over_group(w[0] + w[1] + w[2] + w[3], lds);
-    if (threadIdx.x == 0) p.sums[static_cast<long long>(seq) * p.parts + part] = total;
+    if (span == 0 && lane == 0) {
+        p.verdicts[4 * seq] = v.accepted;
+        p.verdicts[4 * seq + 1] = v.token;
+        p.verdicts[4 * seq + 2] = v.all;
+    }
+    unsigned long long total = 0, w[4];
+#pragma unroll
+    for (int i = 0; i < kVerifySpan / 256; ++i) {
+        weights4<TYPE>(p, s, span * kVerifySpan + i * 256 + 4 * lane, w);
+        total += (w[0] + w[1]) + (w[2] + w[3]);
+    }
+    total = sum_over_wave(total);
+    if (lane == 0) p.sums[static_cast<long long>(seq) * p.spans + span] = total;
 }
 
-// The token: a workgroup per sequence.
+// Running sum over the workgroup up to and with this thread's x; all: over everything.
+__device__ __forceinline__ unsigned long long running_over_group(unsigned long long x, unsigned long long* lds, unsigned long long& all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const unsigned long long mine = running_sum(x, lane);
+    __syncthreads();                                            // (the sums before are read)
+    if (lane == 63) lds[wave] = mine;
+    __syncthreads();
+    unsigned long long before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kVerifyThreads / 64; ++w) {
+        if (w < wave) before += lds[w];
+        all += lds[w];
+    }
+    return before + mine;
+}
+
+// The token: a workgroup per sequence finds the span where the running sum passes the goal, then the token in it.
 template <int TYPE>
 __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(const VerifyParams p) {
     __shared__ unsigned long long lds[kVerifyThreads / 64];
+    __shared__ unsigned long long rest;                         // the goal less the sums before the span
     __shared__ int found;
-    const int seq = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Verdict v = judge<TYPE>(p, seq, lane);
+    const int seq = blockIdx.x, me = threadIdx.x;
+    const unsigned long long* sums = p.sums + static_cast<long long>(seq) * p.spans;
+    const Verdict v = {p.verdicts[4 * seq], p.verdicts[4 * seq + 1], p.verdicts[4 * seq + 2] != 0};
     Source s = source_of(p, seq, v);
-    const unsigned long long* sums = p.sums + static_cast<long long>(seq) * p.parts;
-    unsigned long long total = 0;
-    for (int i = 0; i < p.parts; ++i) total += sums[i];
-    bool own = true;                                            // the parts' sums are those of s
+    unsigned long long x[4], total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = 4 * me + i < p.spans ? sums[4 * me + i] : 0;
+    const float u = p.uniform[static_cast<long long>(seq) * (p.drafts + 1) + p.drafts];
+    unsigned long long upto = running_over_group((x[0] + x[1]) + (x[2] + x[3]), lds, total);
     if (total == 0 && !v.all) {                                 // nothing left of p - q: p alone
         s.minus = false;
         s.gone = -1;
-        own = false;
-        unsigned long long mine = 0, w[4];
-        for (int t = 4 * threadIdx.x; t < p.vocab; t += kVerifyPart) {
-            weights4<TYPE>(p, s, t, w);
-            mine += w[0] + w[1] + w[2] + w[3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = 0;
+            if (4 * me + i >= p.spans) continue;
+            for (int t = 0; t < kVerifySpan; t += 4) {
+                unsigned long long w[4];
+                weights4<TYPE>(p, s, (4 * me + i) * kVerifySpan + t, w);
+                x[i] += (w[0] + w[1]) + (w[2] + w[3]);
+            }
         }
-        total = sum_over_group(mine, lds);
+        upto = running_over_group((x[0] + x[1]) + (x[2] + x[3]), lds, total);
     }
-    const float u = p.uniform[static_cast<long long>(seq) * (p.drafts + 1) + p.drafts];
-    float scaled = u > 0.f ? u * 0x1p31f : 0.f;
+    const float scaled = u > 0.f ? u * 0x1p31f : 0.f;
     const unsigned long long u31 = scaled < 0x1p31f ? static_cast<unsigned long long>(scaled) : 0x7fffffffull;
     // floor(u31 total / 2^31), total < 2^63
-    unsigned long long goal = u31 * (total >> 32) * 2 + (u31 * (total & 0xffffffffull) >> 31);
-    if (threadIdx.x == 0) found = -1;
+    const unsigned long long goal = u31 * (total >> 32) * 2 + (u31 * (total & 0xffffffffull) >> 31);
+    if (me == 0) found = -1;
     __syncthreads();
-    if (total > 0) {
-        int part = 0;
-        if (own)
-            for (; part < p.parts - 1 && sums[part] <= goal; ++part) goal -= sums[part];
-        for (; part < p.parts; ++part) {
-            unsigned long long w[4];
-            const int t = part * kVerifyPart + 4 * static_cast<int>(threadIdx.x);
-            weights4<TYPE>(p, s, t, w);
-            const unsigned long long mine = w[0] + w[1] + w[2] + w[3];
-            unsigned long long upto = mine;                     // running sum over the wave
+    unsigned long long run = upto - ((x[0] + x[1]) + (x[2] + x[3]));
+    if (run <= goal && upto > goal) {                           // one thread, as the sums rise; none where all is 0
+        int i = 0;
 #pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const unsigned long long y = __shfl_up(upto, d);
-                if (lane >= d) upto += y;
+        for (int e = 0; e < 3; ++e)
+            if (run + x[e] <= goal && i == e) {
+                run += x[e];
+                ++i;
             }
-            __syncthreads();
-            if (lane == 63) lds[wave] = upto;
-            __syncthreads();
-            unsigned long long before = 0, all = 0;
+        found = 4 * me + i;
+        rest = goal - run;
+    }
+    __syncthreads();
+    const int span = found;
+    if (span >= 0) {
+        const unsigned long long left = rest;
+        unsigned long long w[4] = {0, 0, 0, 0}, all;
+        const int t = span * kVerifySpan + 4 * me;
+        if (me < kVerifySpan / 4) weights4<TYPE>(p, s, t, w);
+        const unsigned long long mine = (w[0] + w[1]) + (w[2] + w[3]);
+        unsigned long long at = running_over_group(mine, lds, all) - mine;
+        if (at <= left && at + mine > left) {
+            int i = 0;
 #pragma unroll
-            for (int i = 0; i < kVerifyThreads / 64; ++i) {
-                if (i < wave) before += lds[i];
-                all += lds[i];
+            for (int e = 0; e < 3; ++e) {
+                at += w[e];
+                i += at <= left;                                // (sums rise: the tokens before the first above the goal)
             }
-            if (all > goal) {
-                unsigned long long run = before + upto - mine;
-                if (run <= goal && run + mine > goal) {
-                    int i = 0;
-#pragma unroll
-                    for (int e = 0; e < 3; ++e) {
-                        run += w[e];
-                        i += run <= goal;                       // (sums rise: the tokens before the first above the goal)
-                    }
-                    found = t + i;
-                }
-                break;
-            }
-            goal -= all;
+            found = t + i;
         }
         __syncthreads();
     }
-    if (wave == 0 && lane <= p.drafts) {
-        const int token = lane < v.accepted ? p.draft_tokens[static_cast<long long>(seq) * p.drafts + lane]
-                                            : lane == v.accepted ? found : -1;
-        p.tokens[static_cast<long long>(seq) * (p.drafts + 1) + lane] = token;
-        if (lane == 0) p.accepted[seq] = v.accepted;
+    if (me <= p.drafts) {
+        const int token = me < v.accepted ? p.draft_tokens[static_cast<long long>(seq) * p.drafts + me] : me == v.accepted ? found : -1;
+        p.tokens[static_cast<long long>(seq) * (p.drafts + 1) + me] = token;
+        if (me == 0) p.accepted[seq] = v.accepted;
     }
 }
 

@@ -28,10 +28,10 @@ hipError_t read_t(int chunks, const ReadParams& p, dim3 grid, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Workgroups of four waves, a wave per block, head and kind.
+// Workgroups of four waves, a wave per head, kind (keys, values) and block.
 template <typename P>
 dim3 block_grid(const P& p) {
-    return dim3(static_cast<unsigned>((static_cast<long long>(p.seqs) * p.blocks * 2 * p.cache.heads + 3) / 4));
+    return dim3(static_cast<unsigned>(p.seqs) * p.blocks * ((2 * p.cache.heads + 3) / 4));
 }
 
 }  // namespace

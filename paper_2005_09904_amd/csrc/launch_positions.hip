@@ -20,7 +20,29 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(const double* turns, 
 
 template <int TYPE>
 hipError_t rotary_t(const RotaryParams& p, hipStream_t s) {
-    const int items = p.rotation.rot / 2 + (p.copy ? p.dim - p.rotation.rot : 0);
+    constexpr int V = TYPE == BIQ_F32 ? 4 : 8;
+    const int rot = p.rotation.rot, part = p.rotation.interleaved ? rot : rot / 2, rest = p.dim - rot;
+    auto wide = [](const Rows& r) {
+        return (reinterpret_cast<uintptr_t>(r.data) & 15) == 0 && r.row_stride % V == 0 && r.head_stride % V == 0;
+    };
+    if (part % V == 0 && (!p.copy || rest % V == 0) && wide(p.x) && wide(p.y)) {
+        // a thread per access and head while all of them are on the GPU at once, then one for kRotaryHeads heads
+        const long long items = part / V + (p.copy ? rest / V : 0);
+        const long long all = items * p.heads * p.rows;
+        const int groups = all < 1024 * 256 ? p.heads : (p.heads + kRotaryHeads - 1) / kRotaryHeads;
+        const long long threads = items * groups * p.rows;
+        if (threads < 0x7fffff00) {
+            const dim3 grid(static_cast<unsigned>((threads + 255) / 256));
+            if (p.rotation.interleaved)
+                hipLaunchKernelGGL((rotary_wide_kernel<TYPE, true>), grid, dim3(256), 0, s, p, static_cast<uint32_t>(items),
+                                   static_cast<uint32_t>(groups), static_cast<uint32_t>(threads));
+            else
+                hipLaunchKernelGGL((rotary_wide_kernel<TYPE, false>), grid, dim3(256), 0, s, p, static_cast<uint32_t>(items),
+                                   static_cast<uint32_t>(groups), static_cast<uint32_t>(threads));
+            return hipGetLastError();
+        }
+    }
+    const int items = rot / 2 + (p.copy ? rest : 0);
     const long long threads = static_cast<long long>(p.rows) * p.heads * items;
     hipLaunchKernelGGL(rotary_kernel<TYPE>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
     return hipGetLastError();
@@ -28,7 +50,7 @@ hipError_t rotary_t(const RotaryParams& p, hipStream_t s) {
 
 template <int TYPE>
 hipError_t verify_t(const VerifyParams& p, hipStream_t s) {
-    hipLaunchKernelGGL(verify_sums_kernel<TYPE>, dim3(static_cast<unsigned>(p.seqs) * p.parts), dim3(kVerifyThreads), 0, s, p);
+    hipLaunchKernelGGL(verify_sums_kernel<TYPE>, dim3(static_cast<unsigned>(p.seqs) * ((p.spans + 3) / 4)), dim3(256), 0, s, p);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(verify_draw_kernel<TYPE>, dim3(p.seqs), dim3(kVerifyThreads), 0, s, p);
     return hipGetLastError();

@@ -24,7 +24,8 @@ bool rows_ok(const biq_rows& r, int type) {
 }
 Rows rows_of(const biq_rows& r, int type) {
     Rows out{r.data, r.row_stride, r.head_stride, 0};
-    out.quads = aligned(r.data, 4 * type_bytes(type)) && r.row_stride % 4 == 0 && r.head_stride % 4 == 0;
+    const int most = static_cast<int>(4 / type_bytes(type));    // elements in 4 bytes
+    out.quads = aligned(r.data, 4) && r.row_stride % most == 0 && r.head_stride % most == 0;
     return out;
 }
 
@@ -263,7 +264,7 @@ biq_status biq_attention(const biq_attention_args* a, void* workspace, size_t wo
 
 size_t biq_verify_workspace_bytes(int seqs, int vocab) {
     if (seqs < 1 || vocab < 1 || vocab > (1 << 22)) return 0;
-    return static_cast<size_t>(seqs) * ((vocab + kVerifyPart - 1) / kVerifyPart) * 8;
+    return static_cast<size_t>(seqs) * (static_cast<size_t>((vocab + kVerifySpan - 1) / kVerifySpan) * 8 + 16);
 }
 
 biq_status biq_verify_drafts(const biq_verify_args* a, void* workspace, size_t workspace_bytes, void* stream) {
@@ -297,9 +298,11 @@ biq_status biq_verify_drafts(const biq_verify_args* a, void* workspace, size_t w
     p.seqs = a->seqs;
     p.drafts = a->drafts;
     p.vocab = a->vocab;
-    p.parts = (a->vocab + kVerifyPart - 1) / kVerifyPart;
-    p.p_quads = aligned(a->p, 4 * size) && a->p_seq_stride % 4 == 0 && a->p_stride % 4 == 0;
-    p.q_quads = aligned(a->q, 4 * size) && a->q_seq_stride % 4 == 0 && a->q_stride % 4 == 0;
+    p.spans = (a->vocab + kVerifySpan - 1) / kVerifySpan;
+    p.verdicts = reinterpret_cast<int*>(p.sums + static_cast<size_t>(a->seqs) * p.spans);
+    const long long words = static_cast<long long>(4 / size);       // elements in 4 bytes
+    p.p_quads = aligned(a->p, 4) && a->p_seq_stride % words == 0 && a->p_stride % words == 0;
+    p.q_quads = aligned(a->q, 4) && a->q_seq_stride % words == 0 && a->q_stride % words == 0;
     return status(launch_verify(a->type, p, static_cast<hipStream_t>(stream)));
 }
 
