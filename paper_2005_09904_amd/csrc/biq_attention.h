@@ -595,16 +595,16 @@ __device__ __forceinline__ void read_ahead() {
 }
 
 // Many rows of a sequence and head (prompts).  The waves of a workgroup hold different rows, NT tiles of 16 each, and share the
-// tokens: a step's 64 are requested a step ahead, each code by one wave, and laid down in LDS as the 16-bit operands that all
-// waves read, in the order of the lanes that read them (lane after lane: no bank is met twice).  Two buffers, one barrier
-// a step.
-template <int TYPE, int FMT, int CH, bool FULL, int NT>
-__global__ __launch_bounds__(256, CH <= 2 ? 2 : 1) void attend_tile_kernel(const AttendParams p) {
+// tokens: a stage of WAVES / 4 steps of 64 is requested a stage ahead, each code by one wave, and laid down in LDS as the 16-bit
+// operands that all waves read, in the order of the lanes that read them (lane after lane: no bank is met twice).  Two
+// buffers, one barrier a stage.
+template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kernel(const AttendParams p) {
     constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE>::value;
-    constexpr int WAVES = 4, ROWS = 16 * NT * WAVES;
-    constexpr int HALF = 8 * CH * 64;                           // operands of the keys; as many of the values
+    constexpr int STEPS = WAVES / 4, ROWS = 16 * NT * WAVES;
+    constexpr int HALF = 8 * CH * 64;                           // operands of a step's keys; as many of its values
     extern __shared__ float lds[];
-    f16x8* buffers = reinterpret_cast<f16x8*>(lds);             // [2][keys [4][CH][2], values [CH * 4][2]][64]
+    f16x8* buffers = reinterpret_cast<f16x8*>(lds);             // [2][STEPS][keys [4][CH][2], values [CH * 4][2]][64]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
     const int dim = FULL ? 64 * CH : p.cache.dim;
@@ -650,35 +650,43 @@ __global__ __launch_bounds__(256, CH <= 2 ? 2 : 1) void attend_tile_kernel(const
     const int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0, all_hi = p.causal ? pos_first : len - 1;
     const int any_lo = p.window > 0 ? pos_first - p.window + 1 : 0, any_hi = wave_row < rows_all ? p.causal ? pos_last : len - 1 : -1;
 
-    // this wave's part of a step: key rows of tile `wave`, values of CH tiles of 16 elements
+    // this wave's part of a stage: of step wave / 4 the key rows of tile wave % 4 and the values of CH tiles of 16 elements
+    const int my_step = wave >> 2, my_part = wave & 3;
     u32x4 kc[CH], vc[CH];
-    float ks, vs;
-    int valid;
-    bool all_valid;
+    float ks[STEPS], vs[STEPS];
+    int valid[STEPS];
+    bool all_valid[STEPS];
     auto request = [&](int t0) {
-        const StepPlace at = step_place(p.cache, dim, seq, head, t0, len, col >> 2, grp);
-        valid = at.valid;
-        all_valid = at.all;
-        ks = at.scales[0];
-        vs = at.scales[p.cache.heads * p.cache.page_blocks];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int kd = c * 64 + grp * 16, vd = (wave * CH + c) * 16;
-            kc[c] = *reinterpret_cast<const u32x4*>(at.keys + (4 * wave + (col & 3)) * dim + (FULL || kd < dim ? kd : 0));
-            vc[c] = *reinterpret_cast<const u32x4*>(at.values + ((FULL || vd < dim ? vd : 0) + col) * kCacheBlock);
+        for (int i = 0; i < STEPS; ++i) {
+            const StepPlace at = step_place(p.cache, dim, seq, head, t0 + 64 * i, len, col >> 2, grp);
+            valid[i] = at.valid;
+            all_valid[i] = at.all;
+            ks[i] = at.scales[0];
+            vs[i] = at.scales[p.cache.heads * p.cache.page_blocks];
+            if (i != my_step) continue;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int kd = c * 64 + grp * 16, vd = (my_part * CH + c) * 16;
+                kc[c] = *reinterpret_cast<const u32x4*>(at.keys + (4 * my_part + (col & 3)) * dim + (FULL || kd < dim ? kd : 0));
+                vc[c] = *reinterpret_cast<const u32x4*>(at.values + ((FULL || vd < dim ? vd : 0) + col) * kCacheBlock);
+            }
         }
     };
     auto lay_down = [&](f16x8* to) {
-        if (!all_valid) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) vc[c] = first_codes(vc[c], valid);
-        }
+        for (int i = 0; i < STEPS; ++i)
+            if (i == my_step && !all_valid[i]) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c) vc[c] = first_codes(vc[c], valid[i]);
+            }
+        to += my_step * 2 * HALF;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                to[((wave * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(kc[c][2 * h], kc[c][2 * h + 1]);
-                to[HALF + ((wave * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(vc[c][2 * h], vc[c][2 * h + 1]);
+                to[((my_part * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(kc[c][2 * h], kc[c][2 * h + 1]);
+                to[HALF + ((my_part * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(vc[c][2 * h], vc[c][2 * h + 1]);
             }
     };
 
@@ -697,17 +705,25 @@ __global__ __launch_bounds__(256, CH <= 2 ? 2 : 1) void attend_tile_kernel(const
         __syncthreads();
     }
     int parity = 0;
-    for (int t0 = begin; t0 < end; t0 += 64) {
-        const float kscale = ks, vscale = vs;
-        const int nvalid = valid;
-        const bool step_valid = all_valid;
-        const f16x8* from = buffers + parity * 2 * HALF;
-        parity ^= 1;
-        request(t0 + 64 < end ? t0 + 64 : t0);
+    for (int stage = begin; stage < end; stage += 64 * STEPS) {
+        float kscale[STEPS], vscale[STEPS];
+        int nvalid[STEPS];
+        bool step_valid[STEPS];
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            kscale[i] = ks[i];
+            vscale[i] = vs[i];
+            nvalid[i] = valid[i];
+            step_valid[i] = all_valid[i];
+        }
+        request(stage + 64 * STEPS < end ? stage + 64 * STEPS : stage);
         __builtin_amdgcn_sched_barrier(0);
-        if (t0 <= any_hi && t0 + 63 >= any_lo) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int t0 = stage + 64 * i;
+            const f16x8* from = buffers + (parity * STEPS + i) * 2 * HALF;
+            if (t0 >= end || t0 > any_hi || t0 + 63 < any_lo) continue;
             f32x4 s[NT][4];
-            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
 #pragma unroll
@@ -724,23 +740,21 @@ __global__ __launch_bounds__(256, CH <= 2 ? 2 : 1) void attend_tile_kernel(const
                     }
             }
             read_ahead<8 * CH, QT * NT>();
-            __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
-            const bool whole = step_valid && t0 + 63 <= all_hi && t0 >= all_lo;
+            const bool whole = step_valid[i] && t0 + 63 <= all_hi && t0 >= all_lo;
             f16x8 w[NT][2][PT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 bool grown;
                 float keep;
-                const Sight see = {place[n].lo, place[n].hi, t0 + grp * kCacheBlock, nvalid};
-                weigh<PT>(s[n], kscale * unit_of[n], vscale, whole, see, ref[n], l[n], grown, keep, w[n]);
+                const Sight see = {place[n].lo, place[n].hi, t0 + grp * kCacheBlock, nvalid[i]};
+                weigh<PT>(s[n], kscale[i] * unit_of[n], vscale[i], whole, see, ref[n], l[n], grown, keep, w[n]);
                 if (grown) {
 #pragma unroll
                     for (int t = 0; t < CH * 4; ++t) o[n][t] *= keep;
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int t = 0; t < CH * 4; ++t)
 #pragma unroll
@@ -752,10 +766,10 @@ __global__ __launch_bounds__(256, CH <= 2 ? 2 : 1) void attend_tile_kernel(const
                         for (int n = 0; n < NT; ++n) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[n][h][e], o[n][t], 0, 0, 0);
                 }
             read_ahead<8 * CH, PT * NT>();
-            __builtin_amdgcn_s_setprio(0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        lay_down(buffers + parity * 2 * HALF);
+        parity ^= 1;
+        lay_down(buffers + parity * STEPS * 2 * HALF);
         __syncthreads();
     }
 #pragma unroll

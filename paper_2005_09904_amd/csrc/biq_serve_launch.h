@@ -8,10 +8,10 @@
 
 namespace biq {
 
-// (tiles: the kernel for many rows; nt: tiles of 16 rows per wave)
-hipError_t launch_attend_f32(int fmt, bool tiles, int nt, const AttendParams& p, hipStream_t s);
-hipError_t launch_attend_bf16(int fmt, bool tiles, int nt, const AttendParams& p, hipStream_t s);
-hipError_t launch_attend_f16(int fmt, bool tiles, int nt, const AttendParams& p, hipStream_t s);
+// (tiles: the kernel for many rows; nt: tiles of 16 rows per wave; waves: per workgroup)
+hipError_t launch_attend_f32(int fmt, bool tiles, int nt, int waves, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_bf16(int fmt, bool tiles, int nt, int waves, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_f16(int fmt, bool tiles, int nt, int waves, const AttendParams& p, hipStream_t s);
 
 // (chunks: 64 elements of a head each)
 hipError_t launch_append(int type, int fmt, int chunks, const AppendParams& p, hipStream_t s);

@@ -248,3 +248,29 @@ def test_many_sequences_share_the_work(biq, seqs, new):
 def test_one_long_sequence_is_shared(biq):
     check(biq, su.filled([9000], 1, 32, 256, "int8", 1), [1], "fp32", 3, 1, uniform=True)
     check(biq, su.filled([9000, 0, 17], 1, 32, 256, "fp8", 1), [6, 1, 2], "bf16", 3, 1, window=5000)
+
+
+@pytest.mark.parametrize("dim,typ,window", [(64, "bf16", 0), (80, "fp32", 300), (128, "fp16", 0)])
+def test_prompts_that_fill_the_gpu(biq, dim, typ, window):
+    """Rows enough for the widest workgroups (ragged, the last of them partly filled); a sample of them is checked."""
+    lens, counts = [1100, 700, 1500], [1100, 650, 1300]
+    heads, qh = 16, 96
+    pages = su.filled(lens, heads, dim, 64, "int8", dim)
+    rng = np.random.default_rng(1)
+    q = torch.from_numpy(rng.standard_normal((sum(counts), qh, dim)).astype(np.float32)).to(su.TYPES[typ])
+    starts = torch.tensor([0, *np.cumsum(counts)], dtype=torch.int32, device="cuda:0")
+    out, lse = call(biq, pages.on(biq), q.to("cuda:0"), starts=starts, max_rows=max(counts), max_len=1500, window=window)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    at = 0
+    for s, n in enumerate(counts):
+        k, v = pages.values(s)
+        for r in sorted({0, 1, n // 3, n - 43, n - 1}):
+            for h in (0, 5, 47, 95):
+                g = h // 6
+                want, want_lse, size, vmax = su.attention(q[at + r:at + r + 1, h:h + 1].double().numpy(), k[:, g:g + 1], v[:, g:g + 1], dim ** -0.5,
+                                                          np.array([lens[s] - n + r]), True, window)
+                tol, tol_lse = su.attention_bounds(typ, want, size, vmax)
+                assert np.all(np.abs(out[at + r, h] - want[0, 0]) <= tol[0, 0]), (s, r, h)
+                assert abs(lse[at + r, h] - want_lse[0, 0]) <= tol_lse, (s, r, h)
+        at += n
