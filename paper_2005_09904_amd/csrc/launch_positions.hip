@@ -50,6 +50,10 @@ hipError_t rotary_t(const RotaryParams& p, hipStream_t s) {
 
 template <int TYPE>
 hipError_t verify_t(const VerifyParams& p, hipStream_t s) {
+    if (p.spans <= kVerifyOneSpans) {
+        hipLaunchKernelGGL(verify_one_kernel<TYPE>, dim3(p.seqs), dim3(kVerifyThreads), 0, s, p);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(verify_sums_kernel<TYPE>, dim3(static_cast<unsigned>(p.seqs) * ((p.spans + 3) / 4)), dim3(256), 0, s, p);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(verify_draw_kernel<TYPE>, dim3(p.seqs), dim3(kVerifyThreads), 0, s, p);

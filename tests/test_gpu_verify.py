@@ -44,7 +44,7 @@ def check(biq, p, q, drafts, u, lens=None):
 
 @pytest.mark.parametrize("typ", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("seqs,drafts,vocab", [(1, 1, 1), (3, 2, 2), (5, 4, 63), (7, 3, 64), (40, 5, 301), (2, 63, 37), (3, 4, 4095), (3, 4, 4096),
-                                               (3, 4, 4097), (2, 3, 20003), (1, 7, 70000)])
+                                               (3, 4, 4097), (3, 2, 16384), (3, 2, 16385), (2, 3, 20003), (1, 7, 70000)])
 @pytest.mark.parametrize("certain", [False, True])
 def test_tokens(biq, typ, seqs, drafts, vocab, certain):
     p, q, t, u = case(seqs, drafts, vocab, typ, seqs + vocab)
