@@ -3,6 +3,10 @@
 // A wave has one block of 16 tokens of one head, keys or values.  Its lanes hold what they write: of the keys 16 adjacent
 // elements of a token, of the values the 16 tokens at one element, 16 bytes of codes either way, so the codes that are there
 // already come with one load to the lanes that may have to round them anew.
+//
+// The writer waits for loads that depend on each other (lengths, rows, page, angles; a wave lives 8 us): 10300 tokens of 8 heads of
+// 128 (bf16 to fp8, 63 MB) take 25 us, 2.5 TB/s, one token of 64 sequences 7 us.  The reader is bound by its writes: 105 MB (to
+// fp32) take 20.5 us, 5.1 TB/s.
 #pragma once
 
 #include "biq_serve.h"

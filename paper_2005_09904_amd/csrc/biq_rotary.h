@@ -40,7 +40,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p) {
 
 // Memory bounds it: 16 bytes a lane and access, and a row's angles are read once for kHeads heads.  V elements are one access;
 // a thread has one access of pairs (interleaved), two that form pairs (halves), or one that is copied, of the heads first,
-// first + groups, ..  For parts of a head that are multiples of V on 16-byte aligned rows.
+// first + groups, ..  For parts of a head that are multiples of V on 16-byte aligned rows.  16384 rows of 40 heads of 128 in
+// bf16 (336 MB): 62 us, 5.4 TB/s (a thread per pair: 165).
 constexpr int kRotaryHeads = 4;
 template <int TYPE, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotary_wide_kernel(const RotaryParams p, uint32_t items, uint32_t groups, uint32_t threads) {

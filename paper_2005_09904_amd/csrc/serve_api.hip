@@ -58,6 +58,11 @@ bool ragged_ok(const biq_ragged& r, int seqs) {
     return r.starts || static_cast<long long>(seqs) * r.max_rows == r.rows;
 }
 
+// Token numbers, counted from the first row (which may lie before token 0), stay within 32 bits.
+bool tokens_fit(const biq_ragged& r, const biq_cache& c) {
+    return static_cast<long long>(r.max_rows) + static_cast<long long>(c.table_stride) * c.page_tokens <= kMaxInt - 4096;
+}
+
 bool rotation_ok(const biq_rotation& r, int head_dim) {
     return aligned(r.angles, 8) && r.positions >= 1 && r.rot >= 2 && r.rot % 2 == 0 && r.rot <= head_dim;
 }
@@ -82,6 +87,7 @@ biq_status attend_check(const biq_attention_args* a) {
     if (biq_status s = cache_check(a->cache); s != BIQ_OK) return s;
     if (!type_ok(a->type) || a->q_heads < 1 || a->max_len < 0 || a->window < 0 || !ragged_ok(a->ragged, a->cache.seqs)) return BIQ_EINVAL;
     if (a->q_heads % a->cache.heads) return BIQ_EINVAL;
+    if (!tokens_fit(a->ragged, a->cache)) return BIQ_EUNSUPPORTED;
     if (a->q_heads > 65536 || static_cast<long long>(a->ragged.rows) * a->q_heads > kMaxInt) return BIQ_EUNSUPPORTED;
     return BIQ_OK;
 }
@@ -211,7 +217,7 @@ biq_status biq_cache_append(const biq_cache_append_args* a, void* stream) {
     if (a->rotation.angles) p.rotation = {a->rotation.angles, a->rotation.positions, a->rotation.rot, a->rotation.interleaved != 0};
     p.seqs = a->cache.seqs;
     p.blocks = blocks_touched(a->ragged.max_rows);
-    if (static_cast<long long>(p.seqs) * p.blocks > kMaxInt / (2 * a->cache.heads)) return BIQ_EUNSUPPORTED;
+    if (!tokens_fit(a->ragged, a->cache) || static_cast<long long>(p.seqs) * p.blocks > kMaxInt / (2 * a->cache.heads)) return BIQ_EUNSUPPORTED;
     return status(launch_append(a->type, a->cache.format, chunks_of(a->cache.head_dim), p, static_cast<hipStream_t>(stream)));
 }
 
@@ -226,7 +232,7 @@ biq_status biq_cache_read(const biq_cache_read_args* a, void* stream) {
     p.v = rows_of(a->v, a->type);
     p.seqs = a->cache.seqs;
     p.blocks = blocks_touched(a->ragged.max_rows);
-    if (static_cast<long long>(p.seqs) * p.blocks > kMaxInt / (2 * a->cache.heads)) return BIQ_EUNSUPPORTED;
+    if (!tokens_fit(a->ragged, a->cache) || static_cast<long long>(p.seqs) * p.blocks > kMaxInt / (2 * a->cache.heads)) return BIQ_EUNSUPPORTED;
     return status(launch_read(a->type, a->cache.format, chunks_of(a->cache.head_dim), p, static_cast<hipStream_t>(stream)));
 }
 
@@ -249,7 +255,8 @@ biq_status biq_attention(const biq_attention_args* a, void* workspace, size_t wo
     p.q_heads = a->q_heads;
     p.group = a->q_heads / a->cache.heads;
     p.causal = a->causal != 0;
-    p.window = a->window;
+    // (a window that no token is outside of is none)
+    p.window = a->window < static_cast<long long>(a->cache.table_stride) * a->cache.page_tokens ? a->window : 0;
     p.seqs = a->cache.seqs;
     p.shares = pl.shares;
     p.negative = a->scale < 0.f;

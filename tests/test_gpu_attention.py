@@ -274,3 +274,10 @@ def test_prompts_that_fill_the_gpu(biq, dim, typ, window):
                 assert np.all(np.abs(out[at + r, h] - want[0, 0]) <= tol[0, 0]), (s, r, h)
                 assert abs(lse[at + r, h] - want_lse[0, 0]) <= tol_lse, (s, r, h)
         at += n
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_a_window_as_large_as_can_be(biq, new):
+    pages = su.filled([300, 50], 1, 64, 64, "int8", 3)
+    for window in (299, 300, 301, 384, 385, 2**31 - 1):
+        check(biq, pages, [new, 70], "fp32", 2, 5, window=window)

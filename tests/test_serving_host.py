@@ -257,3 +257,16 @@ def test_statuses_come_back_through_the_prepared_call(biq):
         assert e.value.status == EINVAL
     with pytest.raises(TypeError):
         call._call(1)
+
+
+def test_token_numbers_beyond_32_bits_are_refused(biq):
+    from paper_2005_09904_amd import serving
+
+    lib = biq.load_library()
+    big = cache(table_stride=(1 << 26) - 1000)                  # 2^31 tokens but 32000
+    a = attention(cache=big, ragged=ragged(A, 40000, 40000))
+    assert lib.biq_attention(ctypes.addressof(a), A, 1 << 40, None) == EUNSUPPORTED
+    b = serving._AppendArgs(cache=big, k=rows(), v=rows(), ragged=ragged(A, 40000, 40000), rotation=serving._Rotation(None, 0, 0, 0), type=0)
+    assert lib.biq_cache_append(ctypes.addressof(b), None) == EUNSUPPORTED
+    c = serving._ReadArgs(cache=big, k=rows(), v=rows(), ragged=ragged(A, 40000, 40000), type=0)
+    assert lib.biq_cache_read(ctypes.addressof(c), None) == EUNSUPPORTED
