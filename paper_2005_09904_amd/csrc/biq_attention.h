@@ -32,8 +32,9 @@ struct AttendParams {
     float scale;             // |scale| * log2(e)
 };
 
-// What a workgroup spends on a unit beside its steps (rows, first keys, joining its waves, results), in steps.
-constexpr int kUnitCost = 5;
+// What a workgroup spends on a unit beside its steps (rows, first keys, joining its waves, results), in steps: 32 sequences of 410 ..
+// 4096 tokens take 44.7, 41.7, 39.9, 40.8 us with 2, 5, 10, 14.
+constexpr int kUnitCost = 10;
 
 // A unit is a tile of rows of a sequence and head; its work is steps of 64 tokens, [base, base + 64 steps), the same for all
 // units of a sequence (every token that one of its rows sees).
@@ -362,9 +363,9 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 w, int valid) {
 // step ahead, values before the scores.  The waves' sums are joined through LDS.
 //
 // Memory bounds it where units are long: one token of 32 heads over 131071 tokens (269 MB, fp8, bf16) takes 50.5 us, 5.3 TB/s.
-// Where a workgroup has several shorter units, what it does beside their steps shows (5 steps' worth each), and with 32-bit rows
+// Where a workgroup has several shorter units, what it does beside their steps shows (10 steps' worth each), and with 32-bit rows
 // the instructions of a step (4 waves of a CU issue 5000 cycles each: 320 of 520 vector instructions turn codes into 16-bit
-// floats): 32 sequences of 410 .. 4096 tokens (140 MB, int8, fp32) take 36.5 us, 3.8 TB/s, 5 rows of 16 sequences 43 us.
+// floats): 32 sequences of 410 .. 4096 tokens (140 MB, int8, fp32) take 35 us, 4 TB/s, 5 rows of 16 sequences 42 us.
 // CH: 64 elements of a head each; FULL: the head has all of them; NT: tiles of 16 rows.
 template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1) void attend_rows_kernel(const AttendParams p) {

@@ -128,8 +128,8 @@ AttendPlan attend_plan(const biq_attention_args& a) {
     const long long units = pairs * pl.row_tiles;
     // Lengths are not known here, so a unit per workgroup is only taken where a unit is short: up to 8 steps (77 tokens, 8 units: 6.6 us
     // instead of 10.2: the join is a launch of its own), or 32 where there is a unit for every CU.  Beyond, one workgroup per
-    // CU shares the steps (32 sequences of 410 .. 4096 tokens, 8 heads: 43 us instead of 46).
-    // Two per CU are slower (58) as there are more pieces.
+    // CU shares the steps (32 sequences of 410 .. 4096 tokens, 8 heads: 40 us instead of 46).
+    // Two per CU are slower (41.6) as there are more pieces.
     if (steps > (units >= kCus ? 32 : 8) && units < 16 * kCus && units * (room / 64 + 1 + kUnitCost) < kMaxInt) {
         pl.shares = units * steps < kCus ? static_cast<int>(units * steps) : kCus;
         pl.workspace = static_cast<size_t>(pl.shares) * 2 * tile * (c.head_dim + 2) * 4 + static_cast<size_t>(units) * 8;
