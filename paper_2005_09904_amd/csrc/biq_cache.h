@@ -4,9 +4,9 @@
 // elements of a token, of the values the 16 tokens at one element, 16 bytes of codes either way, so the codes that are there
 // already come with one load to the lanes that may have to round them anew.
 //
-// The writer waits for loads that depend on each other (lengths, rows, page, angles; a wave lives 8 us): 10300 tokens of 8 heads of
-// 128 (bf16 to fp8, 63 MB) take 25 us, 2.5 TB/s, one token of 64 sequences 7 us.  The reader is bound by its writes: 105 MB (to
-// fp32) take 20.5 us, 5.1 TB/s.
+// The writer waits for loads that depend on each other (lengths, page; then rows, angles and codes, all requested before the first
+// is used: 19.7 us instead of 25): 10300 tokens of 8 heads of 128 (bf16 to fp8, 63 MB) take 19.7 us, 3.2 TB/s, one token of 64
+// sequences 6.8 us.  The reader is bound by its writes: 105 MB (to fp32) take 20.5 us, 5.1 TB/s.
 #pragma once
 
 #include "biq_serve.h"
@@ -61,18 +61,28 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t bits, float old) {
     return r;
 }
 
+// Largest of a wave's numbers: within rows of 16 lanes, then over the rows' ends; lane 63 has it.
 __device__ __forceinline__ uint32_t max_over_wave(uint32_t x) {
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-        const uint32_t y = __shfl_xor(x, d);
-        x = x > y ? x : y;
-    }
-    return x;
+    auto with = [&](int y) { x = x > static_cast<uint32_t>(y) ? x : static_cast<uint32_t>(y); };
+    with(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x111, 0xf, 0xf, true));       // row_shr:1, 2, 4, 8
+    with(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x112, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x114, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x118, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x142, 0xa, 0xf, false));      // row_bcast:15 to rows 1 and 3
+    with(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0x143, 0xc, 0xf, false));      // row_bcast:31 to rows 2 and 3
+    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), 63));
 }
 
-// 16 values and 16 old codes -> 16 codes.  fresh: which are new; the others before `old` tokens are kept.
+// The bytes of 16 codes whose bit is set; zeros for the others.
+__device__ __forceinline__ u32x4 chosen_codes(u32x4 codes, uint32_t bits) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) codes[w] &= ((bits >> (4 * w) & 15u) * 0x00204081u & 0x01010101u) * 255u;
+    return codes;
+}
+
+// 16 values and 16 codes -> 16 codes.  fresh: the values that count; the others are +0, as are the codes of these.
 template <int FMT>
-__device__ __forceinline__ u32x4 encode16(const float (&x)[16], u32x4 codes, uint32_t fresh, uint32_t old, BlockScale s) {
+__device__ __forceinline__ u32x4 encode16(const float (&x)[16], u32x4 codes, uint32_t fresh, BlockScale s) {
     u32x4 out;
     float y[4];
 #pragma unroll
@@ -82,64 +92,74 @@ __device__ __forceinline__ u32x4 encode16(const float (&x)[16], u32x4 codes, uin
         y[2] = code_value<FMT, 2>(codes[w]);
         y[3] = code_value<FMT, 3>(codes[w]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t bit = 1u << (4 * w + i);
-            y[i] = (fresh & bit) ? x[4 * w + i] * s.fresh : (old & bit) ? y[i] * s.kept : 0.f;
-        }
+        for (int i = 0; i < 4; ++i)
+            y[i] = __uint_as_float(__float_as_uint(y[i]) | __float_as_uint(x[4 * w + i])) * ((fresh >> (4 * w + i) & 1u) ? s.fresh : s.kept);
         out[w] = s.scale != s.scale ? 0u : encode4<FMT>(y[0], y[1], y[2], y[3]);
     }
     return out;
 }
 
-// 16 and 2 adjacent elements of a row.
-template <int TYPE>
-__device__ __forceinline__ void load16(const Rows& src, long long at, float (&x)[16]) {
-#pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-        if (src.quads) {
-            const f32x4 q = load_elem4<TYPE>(src.data, at + e);
-#pragma unroll
-            for (int f = 0; f < 4; ++f) x[e + f] = q[f];
+// N adjacent elements of a row as they are.  They become floats once everything that a block needs is requested: a conversion
+// right behind a load, or in a branch with it, waits for it.  QUADS: Rows.quads.
+template <int TYPE, int N>
+struct Elems {
+    typedef typename Elem<TYPE>::T T;
+    typedef T V __attribute__((ext_vector_type(N)));
+    V v;
+    template <bool QUADS>
+    __device__ __forceinline__ void request(const T* row, uint32_t d) {
+        typedef T Loose __attribute__((ext_vector_type(N), aligned(4)));
+        const T* from = row + d;
+        if (QUADS) {
+            v = *reinterpret_cast<const Loose*>(from);
         } else {
 #pragma unroll
-            for (int f = 0; f < 4; ++f) x[e + f] = load_elem<TYPE>(src.data, at + e + f);
+            for (int e = 0; e < N; ++e) v[e] = from[e];
         }
     }
-}
-template <int TYPE>
-__device__ __forceinline__ f32x2 load2(const Rows& src, long long at) {
-    typedef typename Elem<TYPE>::T V __attribute__((ext_vector_type(2), aligned(4)));
-    if (src.quads) return __builtin_convertvector(*reinterpret_cast<const V*>(static_cast<const typename Elem<TYPE>::T*>(src.data) + at), f32x2);
-    return (f32x2){load_elem<TYPE>(src.data, at), load_elem<TYPE>(src.data, at + 1)};
-}
+    __device__ __forceinline__ void get(float (&x)[N], bool used) const {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = used ? static_cast<float>(v[e]) : 0.f;
+    }
+};
 
-// Elements d0 .. d0 + 15 of a key turned by the angles of its position (row `at` of src).
-template <int TYPE>
-__device__ __forceinline__ void turn16(const Rows& src, long long at, const Rotation& r, int pos, int d0, float (&x)[16]) {
+// Elements d0 .. d0 + 15 of a key (raw; row `at` of src) turned by the angles of its position.
+template <int TYPE, bool QUADS>
+__device__ __forceinline__ void turn16(const Rows& src, long long at, const Rotation& r, int pos, int d0, bool used, const Elems<TYPE, 16>& raw, float (&x)[16]) {
     const int rot = r.rot, half = rot / 2;
-    if (d0 >= rot) return;
+    if (!r.angles || d0 >= rot || !used) {
+        raw.get(x, used);
+        return;
+    }
     const bool known = pos < r.positions;
     const float* angles = r.angles + static_cast<long long>(known ? pos : 0) * rot;
     if (r.interleaved) {
+        f32x2 cs[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) cs[e / 2] = *reinterpret_cast<const f32x2*>(angles + (d0 + e < rot ? d0 + e : d0));
+        raw.get(x, true);
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
             if (d0 + e >= rot) continue;
-            const f32x2 cs = *reinterpret_cast<const f32x2*>(angles + d0 + e);
             const float a = x[e], b = x[e + 1];
-            x[e] = turned(a, b, cs[0], cs[1], false);
-            x[e + 1] = turned(b, a, cs[0], cs[1], true);
+            x[e] = turned(a, b, cs[e / 2][0], cs[e / 2][1], false);
+            x[e + 1] = turned(b, a, cs[e / 2][0], cs[e / 2][1], true);
         }
     } else if (half % 16 == 0) {                                // partners are 16 adjacent elements as well
         const bool second = d0 >= half;
         const int p0 = second ? d0 - half : d0;
-        float y[16];
-        load16<TYPE>(src, at + (second ? p0 : d0 + half), y);
+        Elems<TYPE, 16> partners;
+        partners.template request<QUADS>(static_cast<const typename Elem<TYPE>::T*>(src.data) + at, second ? p0 : d0 + half);
+        f32x2 cs[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const f32x2 cs = *reinterpret_cast<const f32x2*>(angles + 2 * (p0 + e));
-            x[e] = turned(x[e], y[e], cs[0], cs[1], second);
-        }
+        for (int e = 0; e < 16; ++e) cs[e] = *reinterpret_cast<const f32x2*>(angles + 2 * (p0 + e));
+        raw.get(x, true);
+        float y[16];
+        partners.get(y, true);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = turned(x[e], y[e], cs[e][0], cs[e][1], second);
     } else {
+        raw.get(x, true);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int d = d0 + e;
@@ -164,8 +184,8 @@ __device__ __forceinline__ uint32_t most_bits(const float (&x)[16], uint32_t bit
     return bits;
 }
 
-// A block of a sequence: tokens [0, old) are there, [old, end) are new.  find() looks up where it lies (codes stays NULL where
-// there is no page); the new rows are requested before.
+// A block of a sequence: tokens [0, old) are there, [old, end) are new.  find() looks up where it lies (scalar loads), if it has a
+// page; then codes, rows and angles are requested together.
 struct BlockPlace {
     const Cache& cache;
     int seq, b, head;
@@ -186,32 +206,26 @@ struct BlockPlace {
     }
 };
 
-// Keys: lane n has unit n % units (16 elements) of token n / units.
-template <int TYPE, int FMT, int CH>
-__device__ __forceinline__ void append_keys(const AppendParams& p, BlockPlace& b, int lane, int dim) {
+// Keys: lane n has unit n % units (16 elements) of token n / units.  Lanes without a new token request one that there is.
+template <int TYPE, int FMT, int CH, bool QUADS>
+__device__ __forceinline__ void append_keys(const AppendParams& p, const BlockPlace& b, int lane, int dim) {
     const int units = dim / 16;
-    float x[CH][16];
+    Elems<TYPE, 16> raw[CH];
     u32x4 there[CH];
+    const float old_scale = b.old > 0 ? *b.scale : 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int n = lane + 64 * c, i = n / units, d0 = (n - i * units) * 16, row = i < b.old ? b.old : i < b.end ? i : b.end - 1;
+        raw[c].template request<QUADS>(static_cast<const typename Elem<TYPE>::T*>(p.k.data) + b.first + row * p.k.row_stride, d0);
+        there[c] = (u32x4){0u, 0u, 0u, 0u};
+        if (b.old > 0 && n < dim) there[c] = *reinterpret_cast<const u32x4*>(b.codes + n * 16);
+    }
+    float x[CH][16];
     uint32_t bits = 0;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int n = lane + 64 * c, i = n / units, d0 = (n - i * units) * 16;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[c][e] = 0.f;
-        if (i >= b.old && i < b.end) load16<TYPE>(p.k, b.first + i * p.k.row_stride + d0, x[c]);
-    }
-    if (!b.find()) return;
-    const float old_scale = b.old > 0 ? *b.scale : 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int n = lane + 64 * c;
-        there[c] = (u32x4){0u, 0u, 0u, 0u};
-        if (b.old > 0 && n < dim) there[c] = *reinterpret_cast<const u32x4*>(b.codes + n * 16);
-    }
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int n = lane + 64 * c, i = n / units, d0 = (n - i * units) * 16;
-        if (p.rotation.angles && i >= b.old && i < b.end) turn16<TYPE>(p.k, b.first + i * p.k.row_stride, p.rotation, b.t0 + i, d0, x[c]);
+        turn16<TYPE, QUADS>(p.k, b.first + i * p.k.row_stride, p.rotation, b.t0 + i, d0, i >= b.old && i < b.end, raw[c], x[c]);
         bits = most_bits(x[c], bits);
     }
     const BlockScale s = block_scale<FMT>(max_over_wave(bits), old_scale);
@@ -219,50 +233,60 @@ __device__ __forceinline__ void append_keys(const AppendParams& p, BlockPlace& b
     for (int c = 0; c < CH; ++c) {
         const int n = lane + 64 * c, i = n / units;
         if (n >= dim) continue;
-        *reinterpret_cast<u32x4*>(b.codes + n * 16) = encode16<FMT>(x[c], there[c], i >= b.old && i < b.end ? 0xffffu : 0u, i < b.old ? 0xffffu : 0u, s);
+        const u32x4 kept = i < b.old ? there[c] : (u32x4){0u, 0u, 0u, 0u};
+        *reinterpret_cast<u32x4*>(b.codes + n * 16) = encode16<FMT>(x[c], kept, i >= b.old ? 0xffffu : 0u, s);
     }
     if (lane == 0) *b.scale = s.scale;
 }
 
-// Values: lane n has the 16 tokens at elements 2 n and 2 n + 1 (so that a row is read 4 or 8 bytes a lane).
-template <int TYPE, int FMT, int CH>
-__device__ __forceinline__ void append_values(const AppendParams& p, BlockPlace& b, int lane, int dim) {
+// Values: lane n has the 16 tokens at elements 2 n and 2 n + 1 (so that a row is read 4 or 8 bytes a lane).  Tokens that are not
+// new stand for one that is, lanes beyond the head for its first one.
+template <int TYPE, int FMT, int CH, bool QUADS>
+__device__ __forceinline__ void append_values(const AppendParams& p, const BlockPlace& b, int lane, int dim) {
+    typedef typename Elem<TYPE>::T T;
     constexpr int PARTS = (CH + 1) / 2;
-    float x[PARTS][2][16];
+    Elems<TYPE, 2> raw[PARTS][16];
     u32x4 there[PARTS][2];
-    uint32_t bits = 0;
+    const float old_scale = b.old > 0 ? *b.scale : 0.f;
 #pragma unroll
     for (int c = 0; c < PARTS; ++c) {
         const int d = 2 * (lane + 64 * c);
+        typedef const __attribute__((address_space(1))) T* Row;
+        Row row = (Row)(static_cast<const T*>(p.v.data) + b.first + b.old * p.v.row_stride);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            f32x2 v = {0.f, 0.f};
-            if (i >= b.old && i < b.end && d < dim) v = load2<TYPE>(p.v, b.first + i * p.v.row_stride + d);
-            x[c][0][i] = v[0];
-            x[c][1][i] = v[1];
+            if (i > 0) row += i > b.old && i < b.end ? p.v.row_stride : 0;
+            asm("" : "+s"(row));                                // (an address of the wave: no lane adds its offset to 64 bits)
+            raw[c][i].template request<QUADS>((const T*)row, d < dim ? d : 0);
         }
-    }
-    if (!b.find()) return;
-    const float old_scale = b.old > 0 ? *b.scale : 0.f;
-#pragma unroll
-    for (int c = 0; c < PARTS; ++c)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int d = 2 * (lane + 64 * c);
             there[c][h] = (u32x4){0u, 0u, 0u, 0u};
             if (b.old > 0 && d < dim) there[c][h] = *reinterpret_cast<const u32x4*>(b.codes + (d + h) * 16);
         }
+    }
+    float x[PARTS][2][16];
+    uint32_t bits = 0;
 #pragma unroll
-    for (int c = 0; c < PARTS; ++c) bits = most_bits(x[c][1], most_bits(x[c][0], bits));
+    for (int c = 0; c < PARTS; ++c) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float two[2];
+            raw[c][i].get(two, i >= b.old && i < b.end);        // (lanes beyond the head: numbers of the block, no matter)
+            x[c][0][i] = two[0];
+            x[c][1][i] = two[1];
+        }
+        bits = most_bits(x[c][1], most_bits(x[c][0], bits));
+    }
     const BlockScale s = block_scale<FMT>(max_over_wave(bits), old_scale);
-    const uint32_t is_old = (1u << b.old) - 1u, is_new = ((1u << b.end) - 1u) & ~is_old;
+    const uint32_t is_old = (1u << b.old) - 1u;
 #pragma unroll
     for (int c = 0; c < PARTS; ++c) {
         const int d = 2 * (lane + 64 * c);
         if (d >= dim) continue;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            *reinterpret_cast<u32x4*>(b.codes + (d + h) * 16) = encode16<FMT>(x[c][h], there[c][h], is_new, is_old, s);
+            *reinterpret_cast<u32x4*>(b.codes + (d + h) * 16) = encode16<FMT>(x[c][h], chosen_codes(there[c][h], is_old), ~is_old, s);
     }
     if (lane == 0) *b.scale = s.scale;
 }
@@ -286,8 +310,14 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p)
     BlockPlace at = {p.cache, seq, b, head, values,
                      (range.x + static_cast<long long>(t0 - pos0)) * src.row_stride + head * src.head_stride, t0,
                      pos0 - t0 < 0 ? 0 : pos0 - t0, len - t0 < kCacheBlock ? len - t0 : kCacheBlock, nullptr, nullptr};
-    if (values) append_values<TYPE, FMT, CH>(p, at, lane, dim);
-    else append_keys<TYPE, FMT, CH>(p, at, lane, dim);
+    if (!at.find()) return;
+    if (values) {
+        if (src.quads) append_values<TYPE, FMT, CH, true>(p, at, lane, dim);
+        else append_values<TYPE, FMT, CH, false>(p, at, lane, dim);
+    } else {
+        if (src.quads) append_keys<TYPE, FMT, CH, true>(p, at, lane, dim);
+        else append_keys<TYPE, FMT, CH, false>(p, at, lane, dim);
+    }
 }
 
 struct ReadParams {

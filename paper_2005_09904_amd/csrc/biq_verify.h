@@ -43,7 +43,7 @@ struct Verdict { int accepted, token; bool all; };
 
 // Lanes of one wave: draft i is lane i's.
 template <int TYPE>
-__device__ __forceinline__ Verdict judge(const VerifyParams& p, int seq, int lane) {
+__device__ __forceinline__ Verdict examine(const VerifyParams& p, int seq, int lane) {
     int drafts = p.draft_lens ? p.draft_lens[seq] : p.drafts;
     drafts = drafts < 0 ? 0 : drafts > p.drafts ? p.drafts : drafts;
     bool ok = false;
@@ -128,7 +128,7 @@ __device__ __forceinline__ unsigned long long running_sum(unsigned long long x, 
     return x;
 }
 
-// Sums of spans of weights, one per wave (workgroups of 4).  Every wave judges the drafts itself: it needs to know the row.
+// Sums of spans of weights, one per wave (workgroups of 4).  Every wave examines the drafts itself: it needs to know the row.
 template <int TYPE>
 __device__ __forceinline__ unsigned long long span_sum(const VerifyParams& p, const Source& s, int span, int lane) {
     unsigned long long total = 0, w[4];
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyParams p) 
     const int lane = threadIdx.x & 63, groups = (p.spans + 3) / 4;
     const int seq = blockIdx.x / groups, span = (blockIdx.x - seq * groups) * 4 + (threadIdx.x >> 6);
     if (span >= p.spans) return;
-    const Verdict v = judge<TYPE>(p, seq, lane);
+    const Verdict v = examine<TYPE>(p, seq, lane);
     const Source s = source_of(p, seq, v);
     if (span == 0 && lane == 0) {
         p.verdicts[4 * seq] = v.accepted;
@@ -260,7 +260,7 @@ template <int TYPE>
 __global__ __launch_bounds__(kVerifyThreads) void verify_one_kernel(const VerifyParams p) {
     __shared__ unsigned long long sums[kVerifyOneSpans];
     const int seq = blockIdx.x, lane = threadIdx.x & 63;
-    const Verdict v = judge<TYPE>(p, seq, lane);
+    const Verdict v = examine<TYPE>(p, seq, lane);
     const Source s = source_of(p, seq, v);
     const int span = threadIdx.x >> 6;
     if (span < p.spans) {
