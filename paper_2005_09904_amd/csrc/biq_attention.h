@@ -144,18 +144,6 @@ __device__ __forceinline__ void f16_terms(const float (&x)[8], f16x8 (&out)[TERM
 }
 
 template <int TYPE>
-__device__ __forceinline__ void load_q8(const Rows& q, long long at, float (&x)[8]) {
-    if (q.quads) {
-        const f32x4 a = load_elem4<TYPE>(q.data, at), b = load_elem4<TYPE>(q.data, at + 4);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { x[j] = a[j]; x[4 + j] = b[j]; }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = load_elem<TYPE>(q.data, at + j);
-    }
-}
-
-template <int TYPE>
 __device__ __forceinline__ void store_row4(const Rows& out, long long at, f32x4 x) {
     if (out.quads) store_elem4<TYPE>(out.data, at, x);
     else
@@ -178,19 +166,28 @@ __device__ __forceinline__ RowPlace row_place(const AttendParams& p, int2 range,
     return r;
 }
 
-// Elements of the row of a lane's column: part (c, h) holds elements 64 c + 16 (lane / 16) + 8 h ..
+// Elements of the row of a lane's column: part (c, h) holds elements 64 c + 16 (lane / 16) + 8 h ..  Lanes without a row and parts
+// beyond the head request some of a row that there is (row `other`), and get zeros.
 template <int TYPE, int CH>
-__device__ __forceinline__ void load_row(const AttendParams& p, const RowPlace& r, int dim, int grp, float (&x)[CH][2][8]) {
+struct RowElems {
+    Elems<TYPE, 8> part[CH][2];
+    __device__ __forceinline__ void request(const AttendParams& p, const RowPlace& r, int other, int dim, int grp) {
+        const auto* row = static_cast<const typename Elem<TYPE>::T*>(p.q.data) + (r.row >= 0 ? r.row : other) * p.q.row_stride + r.head * p.q.head_stride;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h) {
+                const int d = c * 64 + grp * 16 + h * 8;
+                part[c][h].request(row + (d < dim ? d : 0));
+            }
+    }
+    __device__ __forceinline__ void get(const RowPlace& r, int dim, int grp, float (&x)[CH][2][8]) const {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[c][h][j] = 0.f;
-            const int d = c * 64 + grp * 16 + h * 8;
-            if (r.row >= 0 && d < dim) load_q8<TYPE>(p.q, r.row * p.q.row_stride + r.head * p.q.head_stride + d, x[c][h]);
-        }
-}
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) part[c][h].get(x[c][h], r.row >= 0 && c * 64 + grp * 16 + h * 8 < dim);
+    }
+};
 
 // The same as right operands.  Rows of 32-bit or bf16 elements are scaled by a power of two, their largest magnitude to
 // [2^14, 2^15); returned is what undoes it.
@@ -365,7 +362,8 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 w, int valid) {
 // Memory bounds it where units are long: one token of 32 heads over 131071 tokens (269 MB, fp8, bf16) takes 50.5 us, 5.3 TB/s.
 // Where a workgroup has several shorter units, what it does beside their steps shows (10 steps' worth each), and with 32-bit rows
 // the instructions of a step (4 waves of a CU issue 5000 cycles each: 320 of 520 vector instructions turn codes into 16-bit
-// floats): 32 sequences of 410 .. 4096 tokens (140 MB, int8, fp32) take 35 us, 4 TB/s, 5 rows of 16 sequences 42 us.
+// floats): 32 sequences of 410 .. 4096 tokens (140 MB, int8, fp32) take 35 us, 4 TB/s, 5 rows of 16 sequences 40 us
+// (42 where 16-bit rows were converted one load after the other).
 // CH: 64 elements of a head each; FULL: the head has all of them; NT: tiles of 16 rows.
 template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1) void attend_rows_kernel(const AttendParams p) {
@@ -427,11 +425,11 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
 
     // the rows are requested first: they are needed first
     RowPlace place[NT];
-    float x[NT][CH][2][8];
+    RowElems<TYPE, CH> elems[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         place[n] = row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
-        load_row<TYPE, CH>(p, place[n], dim, grp, x[n]);
+        elems[n].request(p, place[n], range.x, dim, grp);
     }
     u32x4 kc[4][CH];                                            // token 4 t + col % 4 of that block
     float ks = 0.f, vs = 0.f;
@@ -461,7 +459,11 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     f16x8 q[NT][CH][2][QT];
     float unit_of[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) unit_of[n] = row_terms<TYPE, CH>(p.negative, x[n], q[n]) * p.scale;
+    for (int n = 0; n < NT; ++n) {
+        float x[CH][2][8];
+        elems[n].get(place[n], dim, grp, x);
+        unit_of[n] = row_terms<TYPE, CH>(p.negative, x, q[n]) * p.scale;
+    }
 
     // tokens that every row of the tile sees
     const int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0;
@@ -607,7 +609,7 @@ __device__ __forceinline__ void read_ahead() {
 //
 // What the SIMDs issue bounds it: matrix products (64 a step of a wave with two tiles of bf16 rows, 19 cycles each), exponentials (32, 27
 // cycles) and other vector instructions (240, 3 cycles) measured apart add up to 2800 cycles, a step takes 2300.  Two prompts of
-// 4096 rows over 8192 tokens, 32 heads of 128: 804 us, 1.03 PFLOP/s.  Tiles of 16 x 16 rather than 32 x 32 as their products
+// 4096 rows over 8192 tokens, 32 heads of 128: 802 us, 1.03 PFLOP/s.  Tiles of 16 x 16 rather than 32 x 32 as their products
 // are 20 % faster a flop here and their layout gives a lane one scale.
 template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kernel(const AttendParams p) {
@@ -645,13 +647,18 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
 
     // this wave's rows
     RowPlace place[NT];
+    RowElems<TYPE, CH> elems[NT];
     f16x8 q[NT][CH][2][QT];
     float unit_of[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         place[n] = row_place(p, range, len, head, row0 + (wave * NT + n) * 16 + col, rows_all);
+        elems[n].request(p, place[n], range.x, dim, grp);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
         float x[CH][2][8];
-        load_row<TYPE, CH>(p, place[n], dim, grp, x);
+        elems[n].get(place[n], dim, grp, x);
         unit_of[n] = row_terms<TYPE, CH>(p.negative, x, q[n]) * p.scale;
     }
     // what all and what some of them see

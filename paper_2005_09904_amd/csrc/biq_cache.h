@@ -99,32 +99,8 @@ __device__ __forceinline__ u32x4 encode16(const float (&x)[16], u32x4 codes, uin
     return out;
 }
 
-// N adjacent elements of a row as they are.  They become floats once everything that a block needs is requested: a conversion
-// right behind a load, or in a branch with it, waits for it.  QUADS: Rows.quads.
-template <int TYPE, int N>
-struct Elems {
-    typedef typename Elem<TYPE>::T T;
-    typedef T V __attribute__((ext_vector_type(N)));
-    V v;
-    template <bool QUADS>
-    __device__ __forceinline__ void request(const T* row, uint32_t d) {
-        typedef T Loose __attribute__((ext_vector_type(N), aligned(4)));
-        const T* from = row + d;
-        if (QUADS) {
-            v = *reinterpret_cast<const Loose*>(from);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = from[e];
-        }
-    }
-    __device__ __forceinline__ void get(float (&x)[N], bool used) const {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = used ? static_cast<float>(v[e]) : 0.f;
-    }
-};
-
 // Elements d0 .. d0 + 15 of a key (raw; row `at` of src) turned by the angles of its position.
-template <int TYPE, bool QUADS>
+template <int TYPE>
 __device__ __forceinline__ void turn16(const Rows& src, long long at, const Rotation& r, int pos, int d0, bool used, const Elems<TYPE, 16>& raw, float (&x)[16]) {
     const int rot = r.rot, half = rot / 2;
     if (!r.angles || d0 >= rot || !used) {
@@ -149,7 +125,7 @@ __device__ __forceinline__ void turn16(const Rows& src, long long at, const Rota
         const bool second = d0 >= half;
         const int p0 = second ? d0 - half : d0;
         Elems<TYPE, 16> partners;
-        partners.template request<QUADS>(static_cast<const typename Elem<TYPE>::T*>(src.data) + at, second ? p0 : d0 + half);
+        partners.request(static_cast<const typename Elem<TYPE>::T*>(src.data) + at + (second ? p0 : d0 + half));
         f32x2 cs[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) cs[e] = *reinterpret_cast<const f32x2*>(angles + 2 * (p0 + e));
@@ -161,12 +137,23 @@ __device__ __forceinline__ void turn16(const Rows& src, long long at, const Rota
     } else {
         raw.get(x, true);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int d = d0 + e;
-            if (d >= rot) continue;
-            const bool second = d >= half;
-            const int pair = second ? d - half : d;
-            x[e] = turned(x[e], load_elem<TYPE>(src.data, at + (second ? pair : d + half)), angles[2 * pair], angles[2 * pair + 1], second);
+        for (int q = 0; q < 16; q += 4) {                       // (four at a time: registers)
+            Elems<TYPE, 1> partners[4];
+            f32x2 cs[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int d = d0 + q + e < rot ? d0 + q + e : d0, pair = d < half ? d : d - half;
+                partners[e].request(static_cast<const typename Elem<TYPE>::T*>(src.data) + at + (d < half ? d + half : pair));
+                cs[e] = *reinterpret_cast<const f32x2*>(angles + 2 * pair);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float y[1];
+                partners[e].get(y, true);
+                if (d0 + q + e < rot) x[q + e] = turned(x[q + e], y[0], cs[e][0], cs[e][1], d0 + q + e >= half);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     if (!known)
@@ -207,7 +194,7 @@ struct BlockPlace {
 };
 
 // Keys: lane n has unit n % units (16 elements) of token n / units.  Lanes without a new token request one that there is.
-template <int TYPE, int FMT, int CH, bool QUADS>
+template <int TYPE, int FMT, int CH>
 __device__ __forceinline__ void append_keys(const AppendParams& p, const BlockPlace& b, int lane, int dim) {
     const int units = dim / 16;
     Elems<TYPE, 16> raw[CH];
@@ -216,7 +203,7 @@ __device__ __forceinline__ void append_keys(const AppendParams& p, const BlockPl
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int n = lane + 64 * c, i = n / units, d0 = (n - i * units) * 16, row = i < b.old ? b.old : i < b.end ? i : b.end - 1;
-        raw[c].template request<QUADS>(static_cast<const typename Elem<TYPE>::T*>(p.k.data) + b.first + row * p.k.row_stride, d0);
+        raw[c].request(static_cast<const typename Elem<TYPE>::T*>(p.k.data) + b.first + row * p.k.row_stride + d0);
         there[c] = (u32x4){0u, 0u, 0u, 0u};
         if (b.old > 0 && n < dim) there[c] = *reinterpret_cast<const u32x4*>(b.codes + n * 16);
     }
@@ -225,7 +212,7 @@ __device__ __forceinline__ void append_keys(const AppendParams& p, const BlockPl
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int n = lane + 64 * c, i = n / units, d0 = (n - i * units) * 16;
-        turn16<TYPE, QUADS>(p.k, b.first + i * p.k.row_stride, p.rotation, b.t0 + i, d0, i >= b.old && i < b.end, raw[c], x[c]);
+        turn16<TYPE>(p.k, b.first + i * p.k.row_stride, p.rotation, b.t0 + i, d0, i >= b.old && i < b.end, raw[c], x[c]);
         bits = most_bits(x[c], bits);
     }
     const BlockScale s = block_scale<FMT>(max_over_wave(bits), old_scale);
@@ -241,7 +228,7 @@ __device__ __forceinline__ void append_keys(const AppendParams& p, const BlockPl
 
 // Values: lane n has the 16 tokens at elements 2 n and 2 n + 1 (so that a row is read 4 or 8 bytes a lane).  Tokens that are not
 // new stand for one that is, lanes beyond the head for its first one.
-template <int TYPE, int FMT, int CH, bool QUADS>
+template <int TYPE, int FMT, int CH>
 __device__ __forceinline__ void append_values(const AppendParams& p, const BlockPlace& b, int lane, int dim) {
     typedef typename Elem<TYPE>::T T;
     constexpr int PARTS = (CH + 1) / 2;
@@ -257,7 +244,7 @@ __device__ __forceinline__ void append_values(const AppendParams& p, const Block
         for (int i = 0; i < 16; ++i) {
             if (i > 0) row += i > b.old && i < b.end ? p.v.row_stride : 0;
             asm("" : "+s"(row));                                // (an address of the wave: no lane adds its offset to 64 bits)
-            raw[c][i].template request<QUADS>((const T*)row, d < dim ? d : 0);
+            raw[c][i].request((const T*)row + static_cast<uint32_t>(d < dim ? d : 0));
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -311,13 +298,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p)
                      (range.x + static_cast<long long>(t0 - pos0)) * src.row_stride + head * src.head_stride, t0,
                      pos0 - t0 < 0 ? 0 : pos0 - t0, len - t0 < kCacheBlock ? len - t0 : kCacheBlock, nullptr, nullptr};
     if (!at.find()) return;
-    if (values) {
-        if (src.quads) append_values<TYPE, FMT, CH, true>(p, at, lane, dim);
-        else append_values<TYPE, FMT, CH, false>(p, at, lane, dim);
-    } else {
-        if (src.quads) append_keys<TYPE, FMT, CH, true>(p, at, lane, dim);
-        else append_keys<TYPE, FMT, CH, false>(p, at, lane, dim);
-    }
+    if (values) append_values<TYPE, FMT, CH>(p, at, lane, dim);
+    else append_keys<TYPE, FMT, CH>(p, at, lane, dim);
 }
 
 struct ReadParams {

@@ -44,6 +44,23 @@ __device__ __forceinline__ void store_elem4(void* base, long long i, f32x4 x) {
     *reinterpret_cast<Loose*>(static_cast<typename Elem<TYPE>::T*>(base) + i) = __builtin_convertvector(x, V);
 }
 
+// N adjacent elements as they are, at any address of an element (wide loads need no more).  They become floats once everything
+// that a block or a unit starts with is requested: a conversion in a branch with its load waits for it.
+template <int TYPE, int N>
+struct Elems {
+    typedef typename Elem<TYPE>::T T;
+    typedef T V __attribute__((ext_vector_type(N)));
+    V v;
+    __device__ __forceinline__ void request(const T* from) {
+        typedef T Loose __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+        v = *reinterpret_cast<const Loose*>(from);
+    }
+    __device__ __forceinline__ void get(float (&x)[N], bool used) const {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = used ? static_cast<float>(v[e]) : 0.f;
+    }
+};
+
 // biq_rows, with what the host has checked: quads = every 4th element lies at a multiple of 4 bytes.
 struct Rows {
     void* data;
