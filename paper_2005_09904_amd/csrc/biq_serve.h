@@ -33,11 +33,6 @@ __device__ __forceinline__ void store_elem(void* base, long long i, float x) {
 
 // 4 adjacent elements at a multiple of 4 bytes (wide accesses to memory need no more).
 template <int TYPE>
-__device__ __forceinline__ f32x4 load_elem4(const void* base, long long i) {
-    typedef typename Elem<TYPE>::T V __attribute__((ext_vector_type(4), aligned(4)));
-    return __builtin_convertvector(*reinterpret_cast<const V*>(static_cast<const typename Elem<TYPE>::T*>(base) + i), f32x4);
-}
-template <int TYPE>
 __device__ __forceinline__ void store_elem4(void* base, long long i, f32x4 x) {
     typedef typename Elem<TYPE>::T V __attribute__((ext_vector_type(4)));
     typedef typename Elem<TYPE>::T Loose __attribute__((ext_vector_type(4), aligned(4)));

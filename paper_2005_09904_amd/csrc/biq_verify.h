@@ -25,7 +25,6 @@ struct VerifyParams {
     unsigned long long* sums;    // [seqs][spans]
     int* verdicts;               // [seqs][4] accepted drafts, the refused one's token, whether none was refused
     int seqs, drafts, vocab, spans;
-    int p_quads, q_quads;
 };
 
 // floor(2^40 min(1, max(0, r))), 0 for NaN: 20 bits, then 20 more of what is left (both exact).
@@ -44,19 +43,31 @@ struct Verdict { int accepted, token; bool all; };
 // Lanes of one wave: draft i is lane i's.
 template <int TYPE>
 __device__ __forceinline__ Verdict examine(const VerifyParams& p, int seq, int lane) {
+    typedef typename Elem<TYPE>::T T;
+    // (tokens and random numbers of drafts that the sequence does not have are requested as well: none waits for its number of them)
+    const int mine = lane < p.drafts ? lane : 0;
+    int token = -1;
+    float u = 0.f;
+    if (p.drafts > 0) {
+        token = p.draft_tokens[static_cast<long long>(seq) * p.drafts + mine];
+        u = p.uniform[static_cast<long long>(seq) * (p.drafts + 1) + mine];
+    }
     int drafts = p.draft_lens ? p.draft_lens[seq] : p.drafts;
     drafts = drafts < 0 ? 0 : drafts > p.drafts ? p.drafts : drafts;
+    const bool known = lane < drafts && token >= 0 && token < p.vocab;
     bool ok = false;
-    int token = -1;
-    if (lane < drafts) {
-        token = p.draft_tokens[static_cast<long long>(seq) * p.drafts + lane];
-        if (token >= 0 && token < p.vocab) {
-            const float pt = load_elem<TYPE>(p.p, seq * p.p_seq_stride + lane * p.p_stride + token);
-            const float qt = p.q ? load_elem<TYPE>(p.q, seq * p.q_seq_stride + lane * p.q_stride + token) : 1.f;
-            const float u = p.uniform[static_cast<long long>(seq) * (p.drafts + 1) + lane];
-            ok = u * qt < pt;
+    if (known) {
+        Elems<TYPE, 1> pt, qt;
+        float px[1], qx[1] = {1.f};
+        pt.request(static_cast<const T*>(p.p) + seq * p.p_seq_stride + lane * p.p_stride + token);
+        if (p.q) {
+            qt.request(static_cast<const T*>(p.q) + seq * p.q_seq_stride + lane * p.q_stride + token);
+            qt.get(qx, true);
         }
+        pt.get(px, true);
+        ok = u * qx[0] < px[0];
     }
+    token = lane < drafts ? token : -1;
     const unsigned long long refused = ~__ballot(ok);            // (lane `drafts` refuses)
     const int n = __ffsll(refused) - 1;
     Verdict v;
@@ -81,37 +92,46 @@ __device__ __forceinline__ Source source_of(const VerifyParams& p, int seq, cons
     return s;
 }
 
-// Weights of the tokens t .. t + 3 (0 beyond the vocabulary).
-template <int TYPE>
-__device__ __forceinline__ void weights4(const VerifyParams& p, const Source& s, int t, unsigned long long (&w)[4]) {
-    float r[4] = {0.f, 0.f, 0.f, 0.f};
-    const bool inside = t + 4 <= p.vocab;
-    if (inside && p.p_quads) {
-        const f32x4 x = load_elem4<TYPE>(p.p, s.p_at + t);
+// N times 4 adjacent tokens of a row, t + 256 i .., requested together.  whole(i): all 4 of them are there, else they are requested
+// one by one, the last one for those that are not.
+template <int TYPE, int N>
+struct RowTokens {
+    Elems<TYPE, 4> p[N], q[N];
+    template <typename Whole>
+    __device__ __forceinline__ void request_row(Elems<TYPE, 4> (&to)[N], const void* base, long long at, int t, int vocab, const Whole& whole) {
+        const auto* row = static_cast<const typename Elem<TYPE>::T*>(base) + at;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = x[i];
-    } else {
+        for (int i = 0; i < N; ++i) {
+            if (whole(i)) {
+                to[i].request(row + (t + 256 * i));
+            } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (t + i < p.vocab) r[i] = load_elem<TYPE>(p.p, s.p_at + t + i);
-    }
-    if (s.minus) {
-        if (inside && p.q_quads) {
-            const f32x4 x = load_elem4<TYPE>(p.q, s.q_at + t);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] -= x[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (t + i < p.vocab) r[i] -= load_elem<TYPE>(p.q, s.q_at + t + i);
+                for (int e = 0; e < 4; ++e) to[i].v[e] = row[t + 256 * i + e < vocab ? t + 256 * i + e : vocab - 1];
+            }
         }
     }
+    template <typename Whole>
+    __device__ __forceinline__ void request(const VerifyParams& params, const Source& s, int t, const Whole& whole) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (t + i == s.gone) r[i] -= 1.f;
-        w[i] = weight40(r[i]);
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[i].v[e] = typename Elem<TYPE>::T(0.f);
+        request_row(p, params.p, s.p_at, t, params.vocab, whole);
+        if (s.minus) request_row(q, params.q, s.q_at, t, params.vocab, whole);
     }
-}
+    // Weights of the tokens t + 256 i ..  (0 beyond the vocabulary)
+    __device__ __forceinline__ void weights(const Source& s, int vocab, int i, int t, unsigned long long (&w)[4]) const {
+        float r[4], less[4];
+        p[i].get(r, true);
+        q[i].get(less, true);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            r[e] -= less[e];
+            if (t + 256 * i + e == s.gone) r[e] -= 1.f;
+            w[e] = t + 256 * i + e < vocab ? weight40(r[e]) : 0;
+        }
+    }
+};
 
 __device__ __forceinline__ unsigned long long sum_over_wave(unsigned long long x) {
 #pragma unroll
@@ -131,10 +151,13 @@ __device__ __forceinline__ unsigned long long running_sum(unsigned long long x, 
 // Sums of spans of weights, one per wave (workgroups of 4).  Every wave examines the drafts itself: it needs to know the row.
 template <int TYPE>
 __device__ __forceinline__ unsigned long long span_sum(const VerifyParams& p, const Source& s, int span, int lane) {
+    RowTokens<TYPE, kVerifySpan / 256> row;
+    const int t0 = span * kVerifySpan, t = t0 + 4 * lane;
+    row.request(p, s, t, [&](int i) { return t0 + 256 * i + 256 <= p.vocab; });
     unsigned long long total = 0, w[4];
 #pragma unroll
     for (int i = 0; i < kVerifySpan / 256; ++i) {
-        weights4<TYPE>(p, s, span * kVerifySpan + i * 256 + 4 * lane, w);
+        row.weights(s, p.vocab, i, t, w);
         total += (w[0] + w[1]) + (w[2] + w[3]);
     }
     return sum_over_wave(total);
@@ -143,7 +166,7 @@ __device__ __forceinline__ unsigned long long span_sum(const VerifyParams& p, co
 template <int TYPE>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyParams p) {
     const int lane = threadIdx.x & 63, groups = (p.spans + 3) / 4;
-    const int seq = blockIdx.x / groups, span = (blockIdx.x - seq * groups) * 4 + (threadIdx.x >> 6);
+    const int seq = blockIdx.x / groups, span = (blockIdx.x - seq * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (span >= p.spans) return;
     const Verdict v = examine<TYPE>(p, seq, lane);
     const Source s = source_of(p, seq, v);
@@ -181,6 +204,7 @@ __device__ __forceinline__ void draw_token(const VerifyParams& p, int seq, const
     __shared__ unsigned long long rest;                         // the goal less the sums before the span
     __shared__ int found;
     const int me = threadIdx.x;
+    const int draft = me < v.accepted ? p.draft_tokens[static_cast<long long>(seq) * p.drafts + me] : -1;
     unsigned long long x[4], total;
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = 4 * me + i < p.spans ? sums[4 * me + i] : 0;
@@ -195,7 +219,10 @@ __device__ __forceinline__ void draw_token(const VerifyParams& p, int seq, const
             if (4 * me + i >= p.spans) continue;
             for (int t = 0; t < kVerifySpan; t += 4) {
                 unsigned long long w[4];
-                weights4<TYPE>(p, s, (4 * me + i) * kVerifySpan + t, w);
+                RowTokens<TYPE, 1> row;
+                const int at = (4 * me + i) * kVerifySpan + t;
+                row.request(p, s, at, [&](int) { return at + 4 <= p.vocab; });
+                row.weights(s, p.vocab, 0, at, w);
                 x[i] += (w[0] + w[1]) + (w[2] + w[3]);
             }
         }
@@ -225,7 +252,11 @@ __device__ __forceinline__ void draw_token(const VerifyParams& p, int seq, const
         const unsigned long long left = rest;
         unsigned long long w[4] = {0, 0, 0, 0}, all;
         const int t = span * kVerifySpan + 4 * me;
-        if (me < kVerifySpan / 4) weights4<TYPE>(p, s, t, w);
+        if (me < kVerifySpan / 4) {
+            RowTokens<TYPE, 1> row;
+            row.request(p, s, t, [&](int) { return t + 4 <= p.vocab; });
+            row.weights(s, p.vocab, 0, t, w);
+        }
         const unsigned long long mine = (w[0] + w[1]) + (w[2] + w[3]);
         unsigned long long at = running_over_group(mine, lds, all) - mine;
         if (at <= left && at + mine > left) {
@@ -240,7 +271,7 @@ __device__ __forceinline__ void draw_token(const VerifyParams& p, int seq, const
         __syncthreads();
     }
     if (me <= p.drafts) {
-        const int token = me < v.accepted ? p.draft_tokens[static_cast<long long>(seq) * p.drafts + me] : me == v.accepted ? found : -1;
+        const int token = me == v.accepted ? found : draft;
         p.tokens[static_cast<long long>(seq) * (p.drafts + 1) + me] = token;
         if (me == 0) p.accepted[seq] = v.accepted;
     }
@@ -262,7 +293,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_one_kernel(const Verify
     const int seq = blockIdx.x, lane = threadIdx.x & 63;
     const Verdict v = examine<TYPE>(p, seq, lane);
     const Source s = source_of(p, seq, v);
-    const int span = threadIdx.x >> 6;
+    const int span = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (span < p.spans) {
         const unsigned long long total = span_sum<TYPE>(p, s, span, lane);
         if (lane == 0) sums[span] = total;

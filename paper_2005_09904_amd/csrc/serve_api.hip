@@ -312,9 +312,6 @@ biq_status biq_verify_drafts(const biq_verify_args* a, void* workspace, size_t w
     p.vocab = a->vocab;
     p.spans = (a->vocab + kVerifySpan - 1) / kVerifySpan;
     p.verdicts = reinterpret_cast<int*>(p.sums + static_cast<size_t>(a->seqs) * p.spans);
-    const long long words = static_cast<long long>(4 / size);       // elements in 4 bytes
-    p.p_quads = aligned(a->p, 4) && a->p_seq_stride % words == 0 && a->p_stride % words == 0;
-    p.q_quads = aligned(a->q, 4) && a->q_seq_stride % words == 0 && a->q_stride % words == 0;
     return status(launch_verify(a->type, p, static_cast<hipStream_t>(stream)));
 }
 
