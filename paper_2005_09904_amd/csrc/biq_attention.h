@@ -167,17 +167,20 @@ __device__ __forceinline__ RowPlace row_place(const AttendParams& p, int2 range,
 }
 
 // Elements of the row of a lane's column: part (c, h) holds elements 64 c + 16 (lane / 16) + 8 h ..  Lanes without a row and parts
-// beyond the head request some of a row that there is (row `other`), and get zeros.
-template <int TYPE, int CH>
+// beyond the head request some of a row that there is (row `other`), and get zeros.  HALF: of the last 64 elements only the first 32
+// are there, and part (CH - 1, 0) holds 8 (lane / 16) .. of these.
+template <int TYPE, int CH, bool HALF>
 struct RowElems {
     Elems<TYPE, 8> part[CH][2];
+    __device__ __forceinline__ static int element(int c, int h, int grp) { return c * 64 + (HALF && c == CH - 1 ? grp * 8 : grp * 16 + h * 8); }
     __device__ __forceinline__ void request(const AttendParams& p, const RowPlace& r, int other, int dim, int grp) {
         const auto* row = static_cast<const typename Elem<TYPE>::T*>(p.q.data) + (r.row >= 0 ? r.row : other) * p.q.row_stride + r.head * p.q.head_stride;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int d = c * 64 + grp * 16 + h * 8;
+                if (HALF && c == CH - 1 && h == 1) continue;
+                const int d = element(c, h, grp);
                 part[c][h].request(row + (d < dim ? d : 0));
             }
     }
@@ -185,7 +188,14 @@ struct RowElems {
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) part[c][h].get(x[c][h], r.row >= 0 && c * 64 + grp * 16 + h * 8 < dim);
+            for (int h = 0; h < 2; ++h) {
+                if (HALF && c == CH - 1 && h == 1) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[c][h][j] = 0.f;
+                } else {
+                    part[c][h].get(x[c][h], r.row >= 0 && element(c, h, grp) < dim);
+                }
+            }
     }
 };
 
@@ -425,7 +435,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
 
     // the rows are requested first: they are needed first
     RowPlace place[NT];
-    RowElems<TYPE, CH> elems[NT];
+    RowElems<TYPE, CH, false> elems[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         place[n] = row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
@@ -611,11 +621,12 @@ __device__ __forceinline__ void read_ahead() {
 // cycles) and other vector instructions (240, 3 cycles) measured apart add up to 2800 cycles, a step takes 2300.  Two prompts of
 // 4096 rows over 8192 tokens, 32 heads of 128: 802 us, 1.03 PFLOP/s.  Tiles of 16 x 16 rather than 32 x 32 as their products
 // are 20 % faster a flop here and their layout gives a lane one scale.
-template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES>
+template <int TYPE, int FMT, int CH, bool FULL, bool HALF, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kernel(const AttendParams p) {
     constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE>::value;
     constexpr int STEPS = WAVES / 4, ROWS = 16 * NT * WAVES;
-    constexpr int HALF = 8 * CH * 64;                           // operands of a step's keys; as many of its values
+    constexpr int SIDE = 8 * CH * 64;                           // places for a step's keys as operands; as many for its values
+    constexpr int KEYS = 2 * CH - HALF, VALUES = 4 * CH - 2 * HALF;      // operands of 32 elements; of 16
     extern __shared__ float lds[];
     f16x8* buffers = reinterpret_cast<f16x8*>(lds);             // [2][STEPS][keys [4][CH][2], values [CH * 4][2]][64]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -647,7 +658,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
 
     // this wave's rows
     RowPlace place[NT];
-    RowElems<TYPE, CH> elems[NT];
+    RowElems<TYPE, CH, HALF> elems[NT];
     f16x8 q[NT][CH][2][QT];
     float unit_of[NT];
 #pragma unroll
@@ -686,7 +697,18 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int kd = c * 64 + grp * 16, vd = (my_part * CH + c) * 16;
-                kc[c] = *reinterpret_cast<const u32x4*>(at.keys + (4 * my_part + (col & 3)) * dim + (FULL || kd < dim ? kd : 0));
+                const uint8_t* key = at.keys + (4 * my_part + (col & 3)) * dim;
+                if constexpr (HALF) {
+                    if (c == CH - 1) {
+                        const int hd = c * 64 + grp * 8;
+                        const u32x2 eight = *reinterpret_cast<const u32x2*>(key + (hd < dim ? hd : 0));
+                        kc[c] = (u32x4){eight[0], eight[1], 0u, 0u};
+                    } else {
+                        kc[c] = *reinterpret_cast<const u32x4*>(key + kd);
+                    }
+                } else {
+                    kc[c] = *reinterpret_cast<const u32x4*>(key + (FULL || kd < dim ? kd : 0));
+                }
                 vc[c] = *reinterpret_cast<const u32x4*>(at.values + ((FULL || vd < dim ? vd : 0) + col) * kCacheBlock);
             }
         }
@@ -698,24 +720,25 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
 #pragma unroll
                 for (int c = 0; c < CH; ++c) vc[c] = first_codes(vc[c], valid[i]);
             }
-        to += my_step * 2 * HALF;
+        to += my_step * 2 * SIDE;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                to[((my_part * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(kc[c][2 * h], kc[c][2 * h + 1]);
-                to[HALF + ((my_part * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(vc[c][2 * h], vc[c][2 * h + 1]);
+                if (!HALF || c < CH - 1 || h == 0) to[((my_part * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(kc[c][2 * h], kc[c][2 * h + 1]);
+                if (HALF && my_part * CH + c >= VALUES) continue;
+                to[SIDE + ((my_part * CH + c) * 2 + h) * 64 + lane] = codes_f16<FMT>(vc[c][2 * h], vc[c][2 * h + 1]);
             }
     };
 
-    f32x4 o[NT][CH * 4];
+    f32x4 o[NT][VALUES];
     float ref[NT], l[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         ref[n] = kNoRef;
         l[n] = 0.f;
 #pragma unroll
-        for (int t = 0; t < CH * 4; ++t) o[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < VALUES; ++t) o[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     if (begin < end) {
         request(begin);
@@ -739,7 +762,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int t0 = stage + 64 * i;
-            const f16x8* from = buffers + (parity * STEPS + i) * 2 * HALF;
+            const f16x8* from = buffers + (parity * STEPS + i) * 2 * SIDE;
             if (t0 >= end || t0 > any_hi || t0 + 63 < any_lo) continue;
             f32x4 s[NT][4];
 #pragma unroll
@@ -750,6 +773,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
                 for (int c = 0; c < CH; ++c)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
+                        if (2 * c + h >= KEYS) continue;
                         const f16x8 k = from[((t * CH + c) * 2 + h) * 64 + lane];
 #pragma unroll
                         for (int e = 0; e < QT; ++e)
@@ -757,7 +781,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
                             for (int n = 0; n < NT; ++n) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[n][c][h][e], s[n][t], 0, 0, 0);
                     }
             }
-            read_ahead<8 * CH, QT * NT>();
+            read_ahead<4 * KEYS, QT * NT>();
             __builtin_amdgcn_sched_barrier(0);
             const bool whole = step_valid[i] && t0 + 63 <= all_hi && t0 >= all_lo;
             f16x8 w[NT][2][PT];
@@ -769,25 +793,25 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
                 weigh<PT>(s[n], kscale[i] * unit_of[n], vscale[i], whole, see, ref[n], l[n], grown, keep, w[n]);
                 if (grown) {
 #pragma unroll
-                    for (int t = 0; t < CH * 4; ++t) o[n][t] *= keep;
+                    for (int t = 0; t < VALUES; ++t) o[n][t] *= keep;
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < CH * 4; ++t)
+            for (int t = 0; t < VALUES; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const f16x8 v = from[HALF + (t * 2 + h) * 64 + lane];
+                    const f16x8 v = from[SIDE + (t * 2 + h) * 64 + lane];
 #pragma unroll
                     for (int e = 0; e < PT; ++e)
 #pragma unroll
                         for (int n = 0; n < NT; ++n) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[n][h][e], o[n][t], 0, 0, 0);
                 }
-            read_ahead<8 * CH, PT * NT>();
+            read_ahead<2 * VALUES, PT * NT>();
         }
         __builtin_amdgcn_sched_barrier(0);
         parity ^= 1;
-        lay_down(buffers + parity * STEPS * 2 * HALF);
+        lay_down(buffers + parity * STEPS * 2 * SIDE);
         __syncthreads();
     }
 #pragma unroll
@@ -797,7 +821,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
         const float inv = total == 0.f ? 0.f : 1.f / total;
         const long long to = place[n].row * p.out.row_stride + place[n].head * p.out.head_stride + grp * 4;
 #pragma unroll
-        for (int i = 0; i < CH * 4; ++i)
+        for (int i = 0; i < VALUES; ++i)
             if (FULL || i * 16 < dim) store_row4<TYPE>(p.out, to + i * 16, o[n][i] * inv);
         if (p.lse && grp == 0) p.lse[place[n].row * p.q_heads + place[n].head] = log_sum(ref[n], total);
     }

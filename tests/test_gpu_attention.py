@@ -250,6 +250,14 @@ def test_one_long_sequence_is_shared(biq):
     check(biq, su.filled([9000, 0, 17], 1, 32, 256, "fp8", 1), [6, 1, 2], "bf16", 3, 1, window=5000)
 
 
+@pytest.mark.parametrize("typ", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("dim", [32, 80, 96, 112, 160, 224])
+def test_prompts_heads_between_multiples_of_64(biq, fmt, typ, dim):
+    """Rows enough for the kernel of many rows, whatever the size of the head."""
+    check(biq, su.filled([150, 70, 400], 16, dim, 48, fmt, dim), [150, 70, 200], typ, 64, dim, True, 90)
+
+
 @pytest.mark.parametrize("dim,typ,window", [(64, "bf16", 0), (80, "fp32", 300), (128, "fp16", 0)])
 def test_prompts_that_fill_the_gpu(biq, dim, typ, window):
     """Rows enough for the widest workgroups (ragged, the last of them partly filled); a sample of them is checked."""
