@@ -427,7 +427,7 @@ biq_status biq_rotary(const biq_rotary_args* args, void* stream);
  *     scales  float [2][H][T / 16] keys, values
  * and nothing outside it, so a page is copied by copying its bytes.
  *
- * format BIQ_CACHE_INT8: integers in [-127, 127], scale = (largest magnitude of the block) / 127, codes rounded to nearest, ties
+ * format BIQ_CACHE_INT8: integers in [-127, 127], scale = (largest magnitude of the block) * (1 / 127 in 32 bits), codes rounded to nearest, ties
  * to even.  BIQ_CACHE_FP8: 8-bit floats with 4 exponent and 3 fraction bits (OCP E4M3), scale = the least power of two that
  * makes every magnitude at most 448; rounded to nearest, ties to even.  Integers have the smaller mean error (0.9 % of the
  * standard deviation for normal values, floats 2.5 %), floats keep small channels beside large ones.

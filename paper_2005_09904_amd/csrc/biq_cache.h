@@ -41,7 +41,7 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t bits, float old) {
     const float amax = __uint_as_float(bits);
     float scale;
     if constexpr (FMT == BIQ_CACHE_INT8) {
-        scale = amax / 127.0f;
+        scale = amax * (1.0f / 127.0f);                      // (a product with the rounded constant: as biq.h says)
     } else {
         // 448 = 1.75 * 2^8: exponent - 8, one more for a larger significand
         const uint32_t e = (bits >> 23) - 8u + ((bits & 0x7fffffu) > 0x600000u ? 1u : 0u);

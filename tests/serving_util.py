@@ -42,7 +42,7 @@ def fresh_scale(amax, fmt):
     if amax < 2.0 ** -100:
         return np.float32(0)
     if fmt == "int8":
-        return np.float32(amax) / np.float32(127)
+        return np.float32(amax) * np.float32(1 / 127)
     return np.float32(2.0 ** np.ceil(np.log2(np.float64(amax) / 448.0)))
 
 
