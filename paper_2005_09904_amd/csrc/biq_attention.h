@@ -369,7 +369,7 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 w, int valid) {
 // steps of 64 tokens in turn, straight from memory to registers: every code is used by one wave only.  Keys are requested a
 // step ahead, values before the scores.  The waves' sums are joined through LDS.
 //
-// Memory bounds it where units are long: one token of 32 heads over 131071 tokens (269 MB, fp8, bf16) takes 50.5 us, 5.3 TB/s.
+// Memory bounds it where units are long: one token of 32 heads over 131071 tokens (269 MB, fp8, bf16) takes 49.8 us, 5.4 TB/s.
 // Where a workgroup has several shorter units, what it does beside their steps shows (10 steps' worth each), and with 32-bit rows
 // the instructions of a step (4 waves of a CU issue 5000 cycles each: 320 of 520 vector instructions turn codes into 16-bit
 // floats): 32 sequences of 410 .. 4096 tokens (140 MB, int8, fp32) take 35 us, 4 TB/s, 5 rows of 16 sequences 40 us

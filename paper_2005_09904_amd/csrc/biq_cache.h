@@ -5,8 +5,8 @@
 // already come with one load to the lanes that may have to round them anew.
 //
 // The writer waits for loads that depend on each other (lengths, page; then rows, angles and codes, all requested before the first
-// is used: 19.7 us instead of 25): 10300 tokens of 8 heads of 128 (bf16 to fp8, 63 MB) take 19.7 us, 3.2 TB/s, one token of 64
-// sequences 6.8 us.  The reader is bound by its writes: 105 MB (to fp32) take 20.5 us, 5.1 TB/s.
+// is used: 17.5 us instead of 26): 10300 tokens of 8 heads of 128 (bf16 to fp8, 63 MB) take 17.5 us, 3.6 TB/s, one token of 64
+// sequences 6.4 us.  The reader is bound by its writes: 105 MB (to fp32) take 20.8 us, 5.0 TB/s.
 #pragma once
 
 #include "biq_serve.h"

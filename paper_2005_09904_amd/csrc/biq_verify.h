@@ -2,8 +2,8 @@
 //
 // The drawn token needs the sum of a row's weights before it needs their order, so a row of probabilities is read once, a
 // wave per span of 1024 tokens, for the spans' sums, and the span where the goal lies once more.  Weights are integers (40 bits below the point), so that
-// every order of additions gives the same sums and the same token.  64 rows of 120011 (two of them each, 61 MB): 12.6 us for the
-// sums, 4.9 TB/s, and 6 for the tokens, whose loads depend on each other.
+// every order of additions gives the same sums and the same token.  64 rows of 120011 (two of them each, 61 MB): 12 us for the
+// sums, 5.1 TB/s, and 6 for the tokens, whose loads depend on each other.
 #pragma once
 
 #include "biq_serve.h"
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(const Verif
 }
 
 // Both in one launch, for a span per wave at most: the spans' sums stay in LDS.  (One sequence, 5000 tokens: 6.8 us instead of 8.3;
-// 16000: 7.5 and 8.8; 32000 would be 9.4 and 8.9.)
+// 16000: 7.5 and 8.8; 32000, two spans a wave: 10.6 and 9.0.)
 constexpr int kVerifyOneSpans = kVerifyThreads / 64;
 template <int TYPE>
 __global__ __launch_bounds__(kVerifyThreads) void verify_one_kernel(const VerifyParams p) {
