@@ -238,7 +238,7 @@ __device__ __forceinline__ float row_terms(bool negative, float (&x)[CH][2][8], 
 // 2^-100 at least: the sums themselves have 32 bits' range), 6 below it, and only where y would pass 2^14: then `grown` is
 // set (for the whole wave), and what was summed is to be multiplied by `keep`.  A y below 2^-25 (2^-39 of the largest one) is
 // lost.
-// With one term v is added to the exponent as its logarithm, and divided out of the sum once.
+// With one term v is added to the exponent as its logarithm, and divided out of the sum once, where that logarithm is v's own.
 struct Sight { int lo, hi, first, valid; };           // tokens seen: lo .. hi, and the block's first `valid`
 template <int PT>
 __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v, bool whole, Sight see, float& ref, float& sum, bool& grown,
@@ -267,7 +267,7 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v
         ref = next;
     }
     float part = 0.f;
-    if (PT == 1 && __all(v > 0.f && v < INFINITY)) {
+    if (PT == 1 && __all(v >= 0x1p-100f && v < INFINITY)) {
         const float c = lv - ref;
 #pragma unroll
         for (int h = 0; h < 2; ++h)

@@ -1,0 +1,46 @@
+"""biq_attention where values, scales or weights are at the ends of their ranges."""
+import numpy as np
+import pytest
+import torch
+
+import attention_util as au
+import serving_util as su
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def biq():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2005_09904_amd as biq
+
+    biq.load_library()
+    return biq
+
+
+def with_values(lens, heads, dim, fmt, seed, magnitudes):
+    """A cache whose block b has values of magnitude magnitudes[b % len]."""
+    rng = np.random.default_rng(seed)
+    c = su.Pages(lens, heads, dim, 64, fmt, rng)
+    for s, n in enumerate(lens):
+        v = rng.uniform(0.5, 1.0, (n, heads, dim)) * rng.choice([-1.0, 1.0], (n, heads, dim))
+        v *= np.array([magnitudes[t // 16 % len(magnitudes)] for t in range(n)])[:, None, None]
+        c.append(s, 0, rng.standard_normal((n, heads, dim)).astype(np.float32).astype(np.float64), v.astype(np.float32).astype(np.float64))
+    return c
+
+
+MAGNITUDES = [[2.0 ** -99.5], [2.0 ** -98], [2.0 ** -95], [2.0 ** -92], [2.0 ** -88], [2.0 ** -84], [2.0 ** -60], [2.0 ** -97, 2.0 ** -91, 2.0 ** -85],
+              [2.0 ** -98, 2.0 ** -70], [2.0 ** -98, 1.0], [2.0 ** 100], [0.0, 2.0 ** -98], [0.0]]
+
+
+@pytest.mark.parametrize("magnitudes", MAGNITUDES)
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+def test_values_of_any_magnitude(biq, typ, fmt, magnitudes):
+    """Errors stay relative to the largest value, whatever it is (a block is held from 2^-100 on, so its scale is down to 2^-108)."""
+    pages = with_values([300, 90], 2, 64, fmt, 1, magnitudes)
+    for counts in ([1, 1], [40, 3]):                            # few rows
+        au.check(biq, pages, counts, au.rows_like(counts, 4, 64, typ, 2), typ)
+    pages = with_values([160, 100], 16, 32, fmt, 2, magnitudes)
+    counts = [160, 90]                                          # many
+    au.check(biq, pages, counts, au.rows_like(counts, 128, 32, typ, 3), typ, sample=[0, 1, 17, 70, 89, 159])
