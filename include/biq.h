@@ -457,8 +457,8 @@ size_t biq_cache_page_bytes(int page_tokens, int heads, int head_dim);
 /*
  * Rows of a call that belong to sequences: sequence s has rows starts[s] .. starts[s + 1] (device, seqs + 1 numbers that do not
  * fall, bounded to [0, rows] on the device), or rows s * max_rows .. (s + 1) * max_rows where starts is NULL (then rows must be
- * seqs * max_rows).  max_rows bounds the rows of a sequence (rows beyond it are not served; `rows` is always enough).  The n
- * rows of sequence s are its last n tokens: row i is token lens[s] - n + i.
+ * seqs * max_rows).  The n rows of sequence s are its last n tokens: row i is token lens[s] - n + i.  max_rows bounds the rows of
+ * a sequence that are served: its first ones, the same tokens whether or not rows follow (`rows` is always enough).
  */
 typedef struct {
     const int32_t* starts;

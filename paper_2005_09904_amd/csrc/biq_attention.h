@@ -39,7 +39,7 @@ constexpr int kUnitCost = 10;
 // A unit is a tile of rows of a sequence and head; its work is steps of 64 tokens, [base, base + 64 steps), the same for all
 // units of a sequence (every token that one of its rows sees).
 struct SeqWork {
-    int2 range;              // first row, rows
+    RowRange range;
     int len, base, steps;    // steps of a unit: one at least, as a row that sees nothing has a result too
     int tiles;               // units per head
     __device__ __forceinline__ int cost() const { return steps + kUnitCost; }
@@ -48,14 +48,14 @@ struct SeqWork {
 template <int ROWS>
 __device__ __forceinline__ SeqWork seq_work(const AttendParams& p, int seq) {
     SeqWork w;
-    w.range = p.ragged.range(seq);
     w.len = p.cache.length(seq);
-    int lo = p.window > 0 ? w.len - w.range.y - p.window + 1 : 0;
+    w.range = p.ragged.range(seq, w.len);
+    int lo = p.window > 0 ? w.range.token - p.window + 1 : 0;
     lo = lo < 0 ? 0 : lo;
     w.base = lo & ~63;
     w.steps = (w.len - w.base + 63) >> 6;
     w.steps = w.steps < 1 ? 1 : w.steps;
-    w.tiles = (w.range.y * p.group + ROWS - 1) / ROWS;
+    w.tiles = (w.range.count * p.group + ROWS - 1) / ROWS;
     return w;
 }
 
@@ -156,10 +156,10 @@ struct RowPlace {
     long long row;           // -1: none
     int head, lo, hi;
 };
-__device__ __forceinline__ RowPlace row_place(const AttendParams& p, int2 range, int len, int head, int rr, int rows_all) {
+__device__ __forceinline__ RowPlace row_place(const AttendParams& p, RowRange range, int len, int head, int rr, int rows_all) {
     RowPlace r;
-    const int i = rr / p.group, pos = len - range.y + i;
-    r.row = rr < rows_all ? range.x + i : -1;
+    const int i = rr / p.group, pos = range.token + i;
+    r.row = rr < rows_all ? range.first + i : -1;
     r.head = head * p.group + (rr - i * p.group);
     r.hi = p.causal ? pos : len - 1;
     r.lo = p.window > 0 ? pos - p.window + 1 : 0;
@@ -425,10 +425,10 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         p.owners[2 * id] = blockIdx.x;
         p.owners[2 * id + 1] = stop == work.steps ? blockIdx.x : shares.owner(from - 1 - stop + work.steps);
     }
-    const int2 range = work.range;
+    const RowRange range = work.range;
     const int len = work.len;
-    const int rows_all = range.y * p.group, row0 = tile * ROWS;     // (token, head of the group), heads fastest
-    const int pos0 = len - range.y;                             // token of row 0 (negative: before the first token)
+    const int rows_all = range.count * p.group, row0 = tile * ROWS;     // (token, head of the group), heads fastest
+    const int pos0 = range.token;                               // (negative: before the first token)
     const int pos_first = pos0 + row0 / p.group;
     const int pos_last = pos0 + ((row0 + ROWS < rows_all ? row0 + ROWS : rows_all) - 1) / p.group;
     const int begin = work.base + step * 64, end = work.base + stop * 64;
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         place[n] = row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
-        elems[n].request(p, place[n], range.x, dim, grp);
+        elems[n].request(p, place[n], range.first, dim, grp);
     }
     u32x4 kc[4][CH];                                            // token 4 t + col % 4 of that block
     float ks = 0.f, vs = 0.f;
@@ -646,11 +646,11 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
         tile = p.row_tiles - 1 - blockIdx.x / pairs;
     }
     const int seq = pair / p.cache.heads, head = pair - seq * p.cache.heads;
-    const int2 range = p.ragged.range(seq);
     const int len = p.cache.length(seq);
-    const int rows_all = range.y * p.group, row0 = tile * ROWS;
+    const RowRange range = p.ragged.range(seq, len);
+    const int rows_all = range.count * p.group, row0 = tile * ROWS;
     if (row0 >= rows_all) return;
-    const int pos0 = len - range.y;
+    const int pos0 = range.token;
     const int last_row = (row0 + ROWS < rows_all ? row0 + ROWS : rows_all) - 1;
     int begin = p.window > 0 ? pos0 + row0 / p.group - p.window + 1 : 0;
     begin = begin < 0 ? 0 : begin & ~63;
@@ -664,7 +664,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         place[n] = row_place(p, range, len, head, row0 + (wave * NT + n) * 16 + col, rows_all);
-        elems[n].request(p, place[n], range.x, dim, grp);
+        elems[n].request(p, place[n], range.first, dim, grp);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -836,7 +836,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendParams p, 
     const int unit = blockIdx.x / tile_rows, rr = blockIdx.x - unit * tile_rows;
     const int tile = unit % p.row_tiles, head = unit / p.row_tiles % p.cache.heads, seq = unit / p.row_tiles / p.cache.heads;
     const SeqWork work = seq_work<ROWS>(p, seq);
-    const int rows_all = work.range.y * p.group;
+    const int rows_all = work.range.count * p.group;
     if (tile * ROWS + rr >= rows_all) return;
     // pieces: the second slot of share w0, then the first ones of w0 + 1 .. w1
     const int w0 = p.owners[2 * unit], n = p.owners[2 * unit + 1] - w0 + 1;

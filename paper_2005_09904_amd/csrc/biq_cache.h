@@ -287,16 +287,16 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p)
     const int seq = pair / p.blocks, j = pair - seq * p.blocks;
     if (kind >= kinds) return;
     const int head = kind >> 1;
-    const int2 range = p.ragged.range(seq);
-    const int len = p.cache.length(seq), pos0 = len - range.y;
+    const RowRange range = p.ragged.range(seq, p.cache.length(seq));
+    const int pos0 = range.token, end = pos0 + range.count;     // tokens of the rows
     const int b = (pos0 < 0 ? 0 : pos0) / kCacheBlock + j, t0 = b * kCacheBlock;
-    if (range.y <= 0 || t0 >= len) return;
+    if (range.count <= 0 || t0 >= end) return;
     const bool values = kind & 1;
     const Rows& src = values ? p.v : p.k;
     const int dim = p.cache.dim;
     BlockPlace at = {p.cache, seq, b, head, values,
-                     (range.x + static_cast<long long>(t0 - pos0)) * src.row_stride + head * src.head_stride, t0,
-                     pos0 - t0 < 0 ? 0 : pos0 - t0, len - t0 < kCacheBlock ? len - t0 : kCacheBlock, nullptr, nullptr};
+                     (range.first + static_cast<long long>(t0 - pos0)) * src.row_stride + head * src.head_stride, t0,
+                     pos0 - t0 < 0 ? 0 : pos0 - t0, end - t0 < kCacheBlock ? end - t0 : kCacheBlock, nullptr, nullptr};
     if (!at.find()) return;
     if (values) append_values<TYPE, FMT, CH>(p, at, lane, dim);
     else append_keys<TYPE, FMT, CH>(p, at, lane, dim);
@@ -318,11 +318,11 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const ReadParams p) {
     if (kind >= kinds) return;
     const int head = kind >> 1;
     const bool values = kind & 1;
-    const int2 range = p.ragged.range(seq);
-    const int len = p.cache.length(seq), pos0 = len - range.y;
+    const RowRange range = p.ragged.range(seq, p.cache.length(seq));
+    const int pos0 = range.token, end = pos0 + range.count;
     const int b = (pos0 >> 4) + j;                              // (rounded down: below 0 before the first token)
     const long long t0 = static_cast<long long>(b) * kCacheBlock;
-    if (range.y <= 0 || t0 >= len) return;
+    if (range.count <= 0 || t0 >= end) return;
     const int number = b < 0 ? -1 : p.cache.page_number(seq, b);
     const int dim = p.cache.dim;
     const uint8_t* base = nullptr;
@@ -335,9 +335,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const ReadParams p) {
         scale = reinterpret_cast<const float*>(page + 2 * codes)[(values ? p.cache.heads * p.cache.page_blocks : 0) + block];
     }
     const Rows& dst = values ? p.v : p.k;
-    const long long first = (range.x + (t0 - pos0)) * dst.row_stride + head * dst.head_stride;
+    const long long first = (range.first + (t0 - pos0)) * dst.row_stride + head * dst.head_stride;
     const int from = pos0 > t0 ? static_cast<int>(pos0 - t0) : 0;
-    const int to = len - t0 < kCacheBlock ? static_cast<int>(len - t0) : kCacheBlock;
+    const int to = end - t0 < kCacheBlock ? static_cast<int>(end - t0) : kCacheBlock;
     const int units = dim / 16;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {

@@ -99,17 +99,21 @@ struct Cache {
     }
 };
 
+// Rows of a sequence that are served: row `first` + i, i < count, is token `token` + i (below 0: before the first token).
+struct RowRange { int first, count, token; };
+
 struct Ragged {
     const int* starts;
     int rows, max_rows;
-    // First row and number of rows of sequence s.
-    __device__ __forceinline__ int2 range(int s) const {
-        if (!starts) return make_int2(s * max_rows, max_rows);
+    // The n rows of sequence s are its last n tokens, whether or not all of them are served.
+    __device__ __forceinline__ RowRange range(int s, int len) const {
+        if (!starts) return {s * max_rows, max_rows, len - max_rows};
         int a = starts[s], e = starts[s + 1];
         a = a < 0 ? 0 : a > rows ? rows : a;
         e = e < a ? a : e > rows ? rows : e;
-        const int n = e - a;
-        return make_int2(a, n > max_rows ? max_rows : n);
+        const int n = e - a, token = len - n;
+        // (a first row more than max_rows before token 0: no served one is a token, and sums of these numbers keep to 32 bits)
+        return {a, n > max_rows ? max_rows : n, token < -max_rows ? -max_rows : token};
     }
 };
 
