@@ -231,18 +231,22 @@ __device__ __forceinline__ float row_terms(bool negative, float (&x)[CH][2][8], 
 }
 
 // A lane's 16 scores of one row against the tokens first .. first + 15 of a block -> weights times the block's value scale v,
-//     y = 2^(score kscale - ref) v,  sum += sum of 2^(score kscale - ref),
+//     y = 2^(score kscale - ref) v,  sum += unit * sum of 2^(score kscale - ref),
 // as PT 16-bit terms per 8 tokens.
 //
 // y has to stay in the range of 16-bit floats whatever v is, so ref follows the running maximum of score + log2 v (v taken as
-// 2^-100 at least: the sums themselves have 32 bits' range), 6 below it, and only where y would pass 2^14: then `grown` is
+// 2^-108 at least, the least that the cache's writer makes), 6 below it, and only where y would pass 2^14: then `grown` is
 // set (for the whole wave), and what was summed is to be multiplied by `keep`.  A y below 2^-25 (2^-39 of the largest one) is
 // lost.
 // With one term v is added to the exponent as its logarithm, and divided out of the sum once, where that logarithm is v's own.
+//
+// A weight without its v is up to 2^(14 - log2 v), which over many tokens of tiny or no values leaves 32 bits' range: from the
+// first block with v below 2^-60 on a wave keeps its sum in units of 2^32 (widen_sum), which 2^31 weights of 2^122 fit in.
+// (Values above 2^105 beside such blocks would fall out of the sum at its other end.)
 struct Sight { int lo, hi, first, valid; };           // tokens seen: lo .. hi, and the block's first `valid`
 template <int PT>
-__device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v, bool whole, Sight see, float& ref, float& sum, bool& grown,
-                                      float& keep, f16x8 (&out)[2][PT]) {
+__device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v, bool whole, Sight see, float unit, float& ref, float& sum,
+                                      bool& grown, float& keep, f16x8 (&out)[2][PT]) {
     float x[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = s[j >> 2][j & 3];
@@ -256,7 +260,7 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v
     float top = x[0];
 #pragma unroll
     for (int j = 1; j < 16; ++j) top = fmaxf(top, x[j]);
-    const float lv = fmaxf(__builtin_amdgcn_logf(v), -100.f);
+    const float lv = fmaxf(__builtin_amdgcn_logf(v), -108.f);
     top = __builtin_fmaf(top, kscale, lv);            // (kscale >= 0, or NaN)
     grown = __any(top > ref + 14.f);
     keep = 1.f;
@@ -267,7 +271,7 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v
         ref = next;
     }
     float part = 0.f;
-    if (PT == 1 && __all(v >= 0x1p-100f && v < INFINITY)) {
+    if (PT == 1 && __all(v >= 0x1p-108f && v < INFINITY)) {
         const float c = lv - ref;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -293,7 +297,28 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v
             f16_terms<PT>(y, out[h]);
         }
     }
-    sum = __builtin_fmaf(sum, keep, part);
+    sum = __builtin_fmaf(sum, keep, part * unit);
+}
+
+// Before a step whose value scales are v (valid: tokens of the lane's block): the unit of the sums, 1 or 2^-32.
+template <int NT>
+__device__ __forceinline__ void widen_sum(float v, int valid, float& unit, float (&sum)[NT]) {
+    if (unit == 1.f && __any(valid > 0 && v < 0x1p-60f)) {
+        unit = 0x1p-32f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sum[n] *= unit;
+    }
+}
+// After the last step: reference, sum of weights and sums of values in the same unit.
+template <int NT, int TILES>
+__device__ __forceinline__ void same_unit(float unit, float (&ref)[NT], f32x4 (&o)[NT][TILES]) {
+    if (unit == 1.f) return;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        ref[n] += 32.f;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) o[n][t] *= unit;
+    }
 }
 
 // Where a lane finds the codes of a step of 64 tokens (4 blocks): keys of block kblock, values and scales of block vblock.  The
@@ -479,7 +504,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     const int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0;
     const int all_hi = p.causal ? pos_first : len - 1;
     f32x4 o[NT][CH * 4];
-    float ref[NT], l[NT];
+    float ref[NT], l[NT], unit_of_sum = 1.f;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         ref[n] = kNoRef;
@@ -527,13 +552,14 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
 #pragma unroll
             for (int t = 0; t < CH * 4; ++t) vc[t] = first_codes(vc[t], nvalid);
         }
+        widen_sum(vscale, nvalid, unit_of_sum, l);
         f16x8 w[NT][2][PT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             bool grown;
             float keep;
             const Sight see = {place[n].lo, place[n].hi, t0 + grp * kCacheBlock, nvalid};
-            weigh<PT>(s[n], kscale * unit_of[n], vscale, whole, see, ref[n], l[n], grown, keep, w[n]);
+            weigh<PT>(s[n], kscale * unit_of[n], vscale, whole, see, unit_of_sum, ref[n], l[n], grown, keep, w[n]);
             if (grown) {
 #pragma unroll
                 for (int t = 0; t < CH * 4; ++t) o[n][t] *= keep;
@@ -551,6 +577,8 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
                         o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[n][h][e], o[n][t], 0, 0, 0);
             }
     }
+
+    same_unit(unit_of_sum, ref, o);
 
     // ---- the waves' sums, joined: every wave's go to LDS, then every thread adds 4 elements of a row ------------------
     // Sums (tile i of 16 elements, lane) lie at 16-byte place 64 i + 16 grp + (col + 4 i + grp) % 16: neither the lanes that
@@ -732,7 +760,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     };
 
     f32x4 o[NT][VALUES];
-    float ref[NT], l[NT];
+    float ref[NT], l[NT], unit_of_sum = 1.f;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         ref[n] = kNoRef;
@@ -784,13 +812,14 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
             read_ahead<4 * KEYS, QT * NT>();
             __builtin_amdgcn_sched_barrier(0);
             const bool whole = step_valid[i] && t0 + 63 <= all_hi && t0 >= all_lo;
+            widen_sum(vscale[i], nvalid[i], unit_of_sum, l);
             f16x8 w[NT][2][PT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 bool grown;
                 float keep;
                 const Sight see = {place[n].lo, place[n].hi, t0 + grp * kCacheBlock, nvalid[i]};
-                weigh<PT>(s[n], kscale[i] * unit_of[n], vscale[i], whole, see, ref[n], l[n], grown, keep, w[n]);
+                weigh<PT>(s[n], kscale[i] * unit_of[n], vscale[i], whole, see, unit_of_sum, ref[n], l[n], grown, keep, w[n]);
                 if (grown) {
 #pragma unroll
                     for (int t = 0; t < VALUES; ++t) o[n][t] *= keep;
@@ -814,6 +843,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
         lay_down(buffers + parity * STEPS * 2 * SIDE);
         __syncthreads();
     }
+    same_unit(unit_of_sum, ref, o);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float total = sum_over_groups(l[n]);

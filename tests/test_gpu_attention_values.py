@@ -44,3 +44,26 @@ def test_values_of_any_magnitude(biq, typ, fmt, magnitudes):
     pages = with_values([160, 100], 16, 32, fmt, 2, magnitudes)
     counts = [160, 90]                                          # many
     au.check(biq, pages, counts, au.rows_like(counts, 128, 32, typ, 3), typ, sample=[0, 1, 17, 70, 89, 159])
+
+
+def constant(length, low, k_low, k_high, value):
+    """One head of 16: keys k_low for the first `low` tokens, k_high for the others, values value(tokens); rows of ones see
+    16 k_low scale and 16 k_high scale."""
+    c = su.Pages([length], 1, 16, 256, "int8", np.random.default_rng(1))
+    k = np.where(np.arange(length) < low, k_low, k_high)[:, None, None] * np.ones((1, 1, 16))
+    v = value(np.arange(length))[:, None, None] * np.ones((1, 1, 16))
+    c.append(0, 0, k, v)
+    return c
+
+
+def test_many_tokens_whose_values_are_zeros(biq):
+    """The sum of the weights stays a number although no value bounds the reference: 40000 tokens, 7.5 doublings above the first ones."""
+    up = 7.5 * np.log(2) / 16
+    pages = constant(40000, 256, 0.0, up, lambda t: 0.0 * t)
+    q = torch.ones((1, 1, 16))
+    out, _ = au.check(biq, pages, [1], q, "fp32", scale=1.0, max_len=64)       # one workgroup walks through all tokens
+    assert (out == 0).all()
+    au.check(biq, pages, [1], q.bfloat16(), "bf16", scale=1.0, max_len=64)
+    q = torch.ones((3000, 16, 16))                              # one wave does
+    au.check(biq, pages, [3000], q, "fp32", scale=1.0, sample=[0, 1499, 2999])
+    au.check(biq, pages, [3000], q.bfloat16(), "bf16", scale=1.0, sample=[0, 1499, 2999])
