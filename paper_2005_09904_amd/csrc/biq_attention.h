@@ -122,6 +122,15 @@ __device__ __forceinline__ float log_sum(float ref, float total) {
 
 constexpr float kNoRef = -3.402823466e38f;            // reference of a row that has seen nothing
 
+// 2^x, x <= 0, in two factors.  A sum of weights is brought to a later reference by both, one after the other: references follow the
+// values' scales, so that zeros or tiny values beside large ones make x less than -126, and a sum of weights of 2^100 and more.
+struct Factor {
+    float half;
+    __device__ __forceinline__ explicit Factor(float x) : half(exp2_raw(0.5f * x)) {}
+    __device__ __forceinline__ float of(float sum) const { return sum * half * half; }
+    __device__ __forceinline__ float whole() const { return half * half; }
+};
+
 // The matrix cores multiply 16-bit floats: both code formats fit them exactly, and a 32-bit number is two of them to 22 bits
 // once it is scaled into their range.  Terms of q: two for 32-bit elements, one otherwise (bf16 values have 8 bits).
 template <int TYPE> struct RowTerms { static constexpr int value = TYPE == BIQ_F32 ? 2 : 1; };
@@ -231,21 +240,47 @@ __device__ __forceinline__ float row_terms(bool negative, float (&x)[CH][2][8], 
 }
 
 // A lane's 16 scores of one row against the tokens first .. first + 15 of a block -> weights times the block's value scale v,
-//     y = 2^(score kscale - ref) v,  sum += unit * sum of 2^(score kscale - ref),
+//     y = 2^(score kscale - ref) v,  sum += range.unit * sum of 2^(score kscale - ref),
 // as PT 16-bit terms per 8 tokens.
 //
 // y has to stay in the range of 16-bit floats whatever v is, so ref follows the running maximum of score + log2 v (v taken as
 // 2^-108 at least, the least that the cache's writer makes), 6 below it, and only where y would pass 2^14: then `grown` is
 // set (for the whole wave), and what was summed is to be multiplied by `keep`.  A y below 2^-25 (2^-39 of the largest one) is
 // lost.
-// With one term v is added to the exponent as its logarithm, and divided out of the sum once, where that logarithm is v's own.
+// With one term v is added to the exponent as its logarithm, and divided out of the sum once, as long as all scales of the wave's
+// steps were between 2^-60 and 2^40 (range.narrow): then no y that counts in the sum is below 2^-126.
 //
 // A weight without its v is up to 2^(14 - log2 v), which over many tokens of tiny or no values leaves 32 bits' range: from the
-// first block with v below 2^-60 on a wave keeps its sum in units of 2^32 (widen_sum), which 2^31 weights of 2^122 fit in.
+// first block with v below 2^-60 on a wave keeps its sum in units of 2^32 (range.unit), which 2^31 weights of 2^122 fit in.
 // (Values above 2^105 beside such blocks would fall out of the sum at its other end.)
+struct ScaleRange {
+    bool narrow = true;
+    float unit = 1.f;
+    // Before a step whose value scales are v (valid: tokens of the lane's block).
+    template <int NT>
+    __device__ __forceinline__ void see(float v, int valid, float (&sum)[NT]) {
+        if (narrow) narrow = !__any(valid > 0 && !(v >= 0x1p-60f && v <= 0x1p40f));
+        if (!narrow && unit == 1.f && __any(valid > 0 && v < 0x1p-60f)) {
+            unit = 0x1p-32f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sum[n] *= unit;
+        }
+    }
+    // After the last step: reference, sum of weights and sums of values in the same unit.
+    template <int NT, int TILES>
+    __device__ __forceinline__ void leave(float (&ref)[NT], f32x4 (&o)[NT][TILES]) const {
+        if (unit == 1.f) return;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            ref[n] += 32.f;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) o[n][t] *= unit;
+        }
+    }
+};
 struct Sight { int lo, hi, first, valid; };           // tokens seen: lo .. hi, and the block's first `valid`
 template <int PT>
-__device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v, bool whole, Sight see, float unit, float& ref, float& sum,
+__device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v, bool whole, Sight see, const ScaleRange& range, float& ref, float& sum,
                                       bool& grown, float& keep, f16x8 (&out)[2][PT]) {
     float x[16];
 #pragma unroll
@@ -267,11 +302,13 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v
     if (grown) {
         const float most = max_over_groups(top);
         const float next = most > ref + 14.f ? most - 6.f : ref;       // (a row's bits do not depend on its neighbours)
-        keep = exp2_raw(ref - next);
+        const Factor down(ref - next);
+        sum = down.of(sum);
+        keep = down.whole();
         ref = next;
     }
     float part = 0.f;
-    if (PT == 1 && __all(v >= 0x1p-108f && v < INFINITY)) {
+    if (PT == 1 && range.narrow) {
         const float c = lv - ref;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -297,28 +334,7 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float kscale, float v
             f16_terms<PT>(y, out[h]);
         }
     }
-    sum = __builtin_fmaf(sum, keep, part * unit);
-}
-
-// Before a step whose value scales are v (valid: tokens of the lane's block): the unit of the sums, 1 or 2^-32.
-template <int NT>
-__device__ __forceinline__ void widen_sum(float v, int valid, float& unit, float (&sum)[NT]) {
-    if (unit == 1.f && __any(valid > 0 && v < 0x1p-60f)) {
-        unit = 0x1p-32f;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) sum[n] *= unit;
-    }
-}
-// After the last step: reference, sum of weights and sums of values in the same unit.
-template <int NT, int TILES>
-__device__ __forceinline__ void same_unit(float unit, float (&ref)[NT], f32x4 (&o)[NT][TILES]) {
-    if (unit == 1.f) return;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        ref[n] += 32.f;
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) o[n][t] *= unit;
-    }
+    sum = __builtin_fmaf(part, range.unit, sum);
 }
 
 // Where a lane finds the codes of a step of 64 tokens (4 blocks): keys of block kblock, values and scales of block vblock.  The
@@ -504,7 +520,8 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     const int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0;
     const int all_hi = p.causal ? pos_first : len - 1;
     f32x4 o[NT][CH * 4];
-    float ref[NT], l[NT], unit_of_sum = 1.f;
+    float ref[NT], l[NT];
+    ScaleRange scales;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         ref[n] = kNoRef;
@@ -552,14 +569,14 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
 #pragma unroll
             for (int t = 0; t < CH * 4; ++t) vc[t] = first_codes(vc[t], nvalid);
         }
-        widen_sum(vscale, nvalid, unit_of_sum, l);
+        scales.see(vscale, nvalid, l);
         f16x8 w[NT][2][PT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             bool grown;
             float keep;
             const Sight see = {place[n].lo, place[n].hi, t0 + grp * kCacheBlock, nvalid};
-            weigh<PT>(s[n], kscale * unit_of[n], vscale, whole, see, unit_of_sum, ref[n], l[n], grown, keep, w[n]);
+            weigh<PT>(s[n], kscale * unit_of[n], vscale, whole, see, scales, ref[n], l[n], grown, keep, w[n]);
             if (grown) {
 #pragma unroll
                 for (int t = 0; t < CH * 4; ++t) o[n][t] *= keep;
@@ -578,7 +595,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
             }
     }
 
-    same_unit(unit_of_sum, ref, o);
+    scales.leave(ref, o);
 
     // ---- the waves' sums, joined: every wave's go to LDS, then every thread adds 4 elements of a row ------------------
     // Sums (tile i of 16 elements, lane) lie at 16-byte place 64 i + 16 grp + (col + 4 i + grp) % 16: neither the lanes that
@@ -609,9 +626,9 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float f = exp2_raw(st[w][0] - now);
-            total += st[w][1] * f;
-            acc += sums[((w * NT + rr / 16) * (CH * 4) + d / 4) * 64 + (d & 3) * 16 + ((rr + d) & 15)] * f;
+            const Factor f(st[w][0] - now);
+            total += f.of(st[w][1]);
+            acc += sums[((w * NT + rr / 16) * (CH * 4) + d / 4) * 64 + (d & 3) * 16 + ((rr + d) & 15)] * f.whole();
         }
         if (slot >= 0) {
             const long long to = static_cast<long long>(slot) * ROWS + rr;
@@ -760,7 +777,8 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     };
 
     f32x4 o[NT][VALUES];
-    float ref[NT], l[NT], unit_of_sum = 1.f;
+    float ref[NT], l[NT];
+    ScaleRange scales;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         ref[n] = kNoRef;
@@ -812,14 +830,14 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
             read_ahead<4 * KEYS, QT * NT>();
             __builtin_amdgcn_sched_barrier(0);
             const bool whole = step_valid[i] && t0 + 63 <= all_hi && t0 >= all_lo;
-            widen_sum(vscale[i], nvalid[i], unit_of_sum, l);
+            scales.see(vscale[i], nvalid[i], l);
             f16x8 w[NT][2][PT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 bool grown;
                 float keep;
                 const Sight see = {place[n].lo, place[n].hi, t0 + grp * kCacheBlock, nvalid[i]};
-                weigh<PT>(s[n], kscale[i] * unit_of[n], vscale[i], whole, see, unit_of_sum, ref[n], l[n], grown, keep, w[n]);
+                weigh<PT>(s[n], kscale[i] * unit_of[n], vscale[i], whole, see, scales, ref[n], l[n], grown, keep, w[n]);
                 if (grown) {
 #pragma unroll
                     for (int t = 0; t < VALUES; ++t) o[n][t] *= keep;
@@ -843,7 +861,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
         lay_down(buffers + parity * STEPS * 2 * SIDE);
         __syncthreads();
     }
-    same_unit(unit_of_sum, ref, o);
+    scales.leave(ref, o);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float total = sum_over_groups(l[n]);
@@ -879,7 +897,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendParams p, 
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) ref = fmaxf(ref, __shfl_xor(ref, d));
     float total = 0.f;
-    for (int k = lane; k < n; k += 64) total += stats[at(k)][1] * exp2_raw(stats[at(k)][0] - ref);
+    for (int k = lane; k < n; k += 64) total += Factor(stats[at(k)][0] - ref).of(stats[at(k)][1]);
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) total += __shfl_xor(total, d);
     const int g = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;

@@ -46,6 +46,16 @@ def test_values_of_any_magnitude(biq, typ, fmt, magnitudes):
     au.check(biq, pages, counts, au.rows_like(counts, 128, 32, typ, 3), typ, sample=[0, 1, 17, 70, 89, 159])
 
 
+@pytest.mark.parametrize("magnitudes", [[0.0, 2.0 ** 100], [2.0 ** 100, 2.0 ** -98]])
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+def test_nothing_beside_large_values(biq, typ, magnitudes):
+    """Rows whose window has blocks of either kind, and of one kind only."""
+    pages = with_values([300, 90], 2, 64, "int8", 1, magnitudes)
+    for counts in ([1, 1], [40, 3]):
+        for window in (0, 16, 5):
+            au.check(biq, pages, counts, au.rows_like(counts, 4, 64, typ, 2), typ, window=window)
+
+
 def constant(length, low, k_low, k_high, value):
     """One head of 16: keys k_low for the first `low` tokens, k_high for the others, values value(tokens); rows of ones see
     16 k_low scale and 16 k_high scale."""
