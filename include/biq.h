@@ -495,8 +495,9 @@ biq_status biq_cache_read(const biq_cache_read_args* args, void* stream);
  * context computed apart can be joined.
  *
  * Codes enter the matrix cores as 16-bit floats, which hold them exactly; a 32-bit q as two of them (22 bits, below 2^-24
- * of the row's largest element fewer), and so do the weights of 32-bit and 16-bit outputs; those of a bf16 output are one (11
- * bits).  Sums, maxima and the softmax are in 32 bits.  Deterministic.
+ * of the row's largest element fewer), and so do the weights of 32-bit and 16-bit outputs (22 bits, fewer where a weight times its
+ * block's value scale is small beside the row's largest, none below 2^-38 of it); those of a bf16 output are one (11 bits, none below
+ * 2^-31).  Sums, maxima and the softmax are in 32 bits.  Deterministic.
  * max_len: about the largest of lens (0: table_stride * page_tokens).  It only sets how the tokens are split over workgroups:
  * results are right whatever it is (splits differ in the order of additions).  workspace: biq_attention_workspace_bytes(), 16-byte aligned (may be 0).
  */

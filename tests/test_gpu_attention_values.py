@@ -77,3 +77,21 @@ def test_many_tokens_whose_values_are_zeros(biq):
     q = torch.ones((3000, 16, 16))                              # one wave does
     au.check(biq, pages, [3000], q, "fp32", scale=1.0, sample=[0, 1499, 2999])
     au.check(biq, pages, [3000], q.bfloat16(), "bf16", scale=1.0, sample=[0, 1499, 2999])
+
+
+@pytest.mark.parametrize("doublings", [26.0, 31.4, 33.0])
+def test_a_long_tail_behind_one_large_weight(biq, doublings):
+    """130984 weights of 2^-31.4 of the first one are 5e-5 of the sum, which a 32-bit output shows: the first token's value is 0, the
+    others' are 1, so the output is the tail's share.  Weights are lost below 2^-38 of the largest; the tail's sum is off by a unit for every
+    step of 64 (2047 of 2^-24) and by the weights' own errors (1e-5), 2^-10 of it in all at most."""
+    up = doublings * np.log(2) / 32
+    length = 131000
+    pages = constant(length, 16, up, -up, lambda t: np.where(t == 0, 0.0, 1.0))
+    for s in range(1, 16):                                      # of the first block one token only has the large score
+        pages.store[pages.table[0, 0], s * 16:(s + 1) * 16] = np.int8(-127).view(np.uint8)
+    q = torch.ones((2900, 16, 16))
+    for rows, how in ((q, {}), (q[:1, :1].contiguous(), dict(max_len=64))):    # one wave; one workgroup
+        out, _ = au.check(biq, pages, [rows.shape[0]], rows, "fp32", scale=1.0, sample=[0, 1450, 2899], **how)
+        k, v = (torch.from_numpy(x) for x in pages.values(0))
+        want, _, _, _ = au.softmax64(rows[-1:].double(), k, v, 1.0, torch.tensor([length - 1]), True, 0)
+        assert ((out[-1:] - want).abs() <= length * 2.0 ** -38 + 2.0 ** -10 * want).all(), (out[-1, 0, 0].item(), want[0, 0, 0].item())
