@@ -28,6 +28,7 @@ struct AttendParams {
     int q_heads, group, causal, window;
     int seqs, row_tiles;     // row_tiles: the most that a sequence's rows make
     int shares;              // > 0: workgroups that share all steps equally; 0: a workgroup per unit
+    unsigned first;          // first workgroup of this launch (0 where they share the steps)
     int negative;            // the scale is below 0: q is negated
     float scale;             // |scale| * log2(e)
 };
@@ -445,7 +446,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         stop = from;
         seq = __builtin_amdgcn_readfirstlane(shares.find(stop));
     } else {
-        seq = blockIdx.x / (p.cache.heads * p.row_tiles);
+        seq = static_cast<int>(p.first + blockIdx.x) / (p.cache.heads * p.row_tiles);
     }
     const SeqWork work = seq_work<ROWS>(p, seq);
     if (p.shares > 0) {
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         from += left < work.cost() - place ? left : work.cost() - place;
         if (stop <= step) continue;                             // no step in this share
     } else {
-        const int r = blockIdx.x - seq * (p.cache.heads * p.row_tiles), t = r % p.row_tiles;
+        const int r = static_cast<int>(p.first + blockIdx.x) - seq * (p.cache.heads * p.row_tiles), t = r % p.row_tiles;
         if (t >= work.tiles) return;
         unit = r / p.row_tiles * work.tiles + t;
         stop = work.steps;
@@ -684,15 +685,15 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     const long long codes = static_cast<long long>(p.cache.heads) * p.cache.page_blocks * kCacheBlock * dim;
     // Later rows see more tokens and come first.  Where the sequences and heads can be dealt to the XCDs evenly, each keeps to
     // its own, whose tokens then stay in its L2.
-    const int pairs = p.seqs * p.cache.heads;
+    const int pairs = p.seqs * p.cache.heads, group = p.first + blockIdx.x;
     int pair, tile;
     if (pairs % kXcds == 0) {
-        const int at = blockIdx.x / kXcds;
-        pair = at / p.row_tiles * kXcds + blockIdx.x % kXcds;
+        const int at = group / kXcds;
+        pair = at / p.row_tiles * kXcds + group % kXcds;
         tile = p.row_tiles - 1 - at % p.row_tiles;
     } else {
-        pair = blockIdx.x % pairs;
-        tile = p.row_tiles - 1 - blockIdx.x / pairs;
+        pair = group % pairs;
+        tile = p.row_tiles - 1 - group / pairs;
     }
     const int seq = pair / p.cache.heads, head = pair - seq * p.cache.heads;
     const int len = p.cache.length(seq);

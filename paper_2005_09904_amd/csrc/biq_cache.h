@@ -31,6 +31,7 @@ struct AppendParams {
     Rows k, v;
     Rotation rotation;
     int seqs, blocks;        // blocks: the most that a sequence's rows can touch
+    unsigned first;          // first workgroup of this launch
 };
 
 // The block's new scale and the factors for new values and old codes.  bits: largest magnitude of the new values as an integer
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p)
     const int lane = threadIdx.x & 63;
     // (sequence, block) pairs and, four waves of a workgroup, the heads' keys and values
     const int kinds = 2 * p.cache.heads, parts = (kinds + 3) / 4;
-    const int pair = blockIdx.x / parts, kind = (blockIdx.x - pair * parts) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = p.first + blockIdx.x, pair = group / parts, kind = (group - pair * parts) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int seq = pair / p.blocks, j = pair - seq * p.blocks;
     if (kind >= kinds) return;
     const int head = kind >> 1;
@@ -307,13 +308,14 @@ struct ReadParams {
     Ragged ragged;
     Rows k, v;
     int seqs, blocks;
+    unsigned first;
 };
 
 template <int TYPE, int FMT, int CH>
 __global__ __launch_bounds__(256) void cache_read_kernel(const ReadParams p) {
     const int lane = threadIdx.x & 63;
     const int kinds = 2 * p.cache.heads, parts = (kinds + 3) / 4;
-    const int pair = blockIdx.x / parts, kind = (blockIdx.x - pair * parts) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = p.first + blockIdx.x, pair = group / parts, kind = (group - pair * parts) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int seq = pair / p.blocks, j = pair - seq * p.blocks;
     if (kind >= kinds) return;
     const int head = kind >> 1;

@@ -10,13 +10,14 @@ struct RotaryParams {
     const int* positions;
     Rotation rotation;
     int rows, heads, dim, inverse, copy;    // copy: y is another tensor, what is not turned is copied
+    unsigned first;                         // first workgroup of this launch (rotary_kernel)
 };
 
 // One thread per row, head and pair (or element that is not turned): any sizes, strides and alignment.
 template <int TYPE>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryParams p) {
     const int half = p.rotation.rot / 2, items = half + (p.copy ? p.dim - p.rotation.rot : 0);
-    const long long at = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    const long long at = static_cast<long long>(p.first + blockIdx.x) * 256 + threadIdx.x;
     const int item = static_cast<int>(at % items);
     const long long rh = at / items;
     const int head = static_cast<int>(rh % p.heads);

@@ -25,6 +25,7 @@ struct VerifyParams {
     unsigned long long* sums;    // [seqs][spans]
     int* verdicts;               // [seqs][4] accepted drafts, the refused one's token, whether none was refused
     int seqs, drafts, vocab, spans;
+    unsigned first;              // first workgroup of this launch (verify_sums_kernel)
 };
 
 // floor(2^40 min(1, max(0, r))), 0 for NaN: 20 bits, then 20 more of what is left (both exact).
@@ -166,7 +167,7 @@ __device__ __forceinline__ unsigned long long span_sum(const VerifyParams& p, co
 template <int TYPE>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyParams p) {
     const int lane = threadIdx.x & 63, groups = (p.spans + 3) / 4;
-    const int seq = blockIdx.x / groups, span = (blockIdx.x - seq * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = p.first + blockIdx.x, seq = group / groups, span = (group - seq * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (span >= p.spans) return;
     const Verdict v = examine<TYPE>(p, seq, lane);
     const Source s = source_of(p, seq, v);

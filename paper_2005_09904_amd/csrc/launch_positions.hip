@@ -6,8 +6,8 @@ namespace {
 
 // The product is reduced to a part of a turn in 64 bits (2^-53 of the turns in all), then to 32 bits.
 __global__ __launch_bounds__(256) void rotary_table_kernel(const double* turns, float* angles, int pairs, int first, int positions,
-                                                           double amplitude) {
-    const long long at = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+                                                           double amplitude, unsigned first_group) {
+    const long long at = static_cast<long long>(first_group + blockIdx.x) * 256 + threadIdx.x;
     if (at >= static_cast<long long>(positions) * pairs) return;
     const long long row = at / pairs;
     double t = static_cast<double>(first + row) * turns[at - row * pairs];
@@ -19,7 +19,7 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(const double* turns, 
 }
 
 template <int TYPE>
-hipError_t rotary_t(const RotaryParams& p, hipStream_t s) {
+hipError_t rotary_t(RotaryParams p, hipStream_t s) {
     constexpr int V = TYPE == BIQ_F32 ? 4 : 8;
     const int rot = p.rotation.rot, part = p.rotation.interleaved ? rot : rot / 2, rest = p.dim - rot;
     auto wide = [](const Rows& r) {
@@ -44,18 +44,25 @@ hipError_t rotary_t(const RotaryParams& p, hipStream_t s) {
     }
     const int items = rot / 2 + (p.copy ? rest : 0);
     const long long threads = static_cast<long long>(p.rows) * p.heads * items;
-    hipLaunchKernelGGL(rotary_kernel<TYPE>, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, p);
-    return hipGetLastError();
+    return launch_parts((threads + 255) / 256, 256, [&](unsigned first, unsigned grid) {
+        p.first = first;
+        hipLaunchKernelGGL(rotary_kernel<TYPE>, dim3(grid), dim3(256), 0, s, p);
+        return hipGetLastError();
+    });
 }
 
 template <int TYPE>
-hipError_t verify_t(const VerifyParams& p, hipStream_t s) {
+hipError_t verify_t(VerifyParams p, hipStream_t s) {
     if (p.spans <= kVerifyOneSpans) {
         hipLaunchKernelGGL(verify_one_kernel<TYPE>, dim3(p.seqs), dim3(kVerifyThreads), 0, s, p);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL(verify_sums_kernel<TYPE>, dim3(static_cast<unsigned>(p.seqs) * ((p.spans + 3) / 4)), dim3(256), 0, s, p);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    const hipError_t e = launch_parts(static_cast<long long>(p.seqs) * ((p.spans + 3) / 4), 256, [&](unsigned first, unsigned grid) {
+        p.first = first;
+        hipLaunchKernelGGL(verify_sums_kernel<TYPE>, dim3(grid), dim3(256), 0, s, p);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(verify_draw_kernel<TYPE>, dim3(p.seqs), dim3(kVerifyThreads), 0, s, p);
     return hipGetLastError();
 }
@@ -74,9 +81,10 @@ hipError_t launch_rotary(int type, const RotaryParams& p, hipStream_t s) {
 hipError_t launch_rotary_table(const double* turns, float* angles, int pairs, int first, int positions, double amplitude,
                                hipStream_t s) {
     const long long threads = static_cast<long long>(positions) * pairs;
-    hipLaunchKernelGGL(rotary_table_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, turns, angles, pairs,
-                       first, positions, amplitude);
-    return hipGetLastError();
+    return launch_parts((threads + 255) / 256, 256, [&](unsigned first_group, unsigned grid) {
+        hipLaunchKernelGGL(rotary_table_kernel, dim3(grid), dim3(256), 0, s, turns, angles, pairs, first, positions, amplitude, first_group);
+        return hipGetLastError();
+    });
 }
 
 hipError_t launch_verify(int type, const VerifyParams& p, hipStream_t s) {
