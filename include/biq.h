@@ -520,8 +520,10 @@ biq_status biq_attention(const biq_attention_args* args, void* workspace, size_t
  * p_drafts.  q NULL: the draft was certain of its tokens (q_i is 1 at its token, 0 elsewhere).  drafts = 0: a token is drawn.
  * Drawn: weights w = floor(2^40 min(1, max(0, p - q))) (0 for NaN), the first token whose running sum of w exceeds
  * floor(floor(2^31 uniform[drafts]) * (sum of all w) / 2^31).  Integers, so the token depends on no order of additions.  If all w
- * are 0, p_j alone is drawn from; if it is 0 as well, the token is -1.  uniform in [0, 1) (bounded to it; NaN: 0, and no draft
- * is accepted).
+ * are 0, p_j alone is drawn from; if it is 0 as well, the token is -1.
+ * uniform is meant to be in [0, 1).  The number for the drawn token is bounded to that (NaN: 0).  Of those for the drafts, numbers
+ * below 0 count as 0, so that a token of probability 0 is never accepted; numbers from 1 on are compared as they are, and NaN
+ * accepts nothing.
  * draft_lens (NULL: all of them): sequence s has draft_lens[s] of the drafts, bounded to [0, drafts].  A token outside
  * [0, vocab) is not accepted.
  * tokens [seqs][drafts + 1]: the accepted drafts, the drawn token, then -1.  accepted [seqs]: how many drafts were.

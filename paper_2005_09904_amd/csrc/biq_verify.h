@@ -66,7 +66,7 @@ __device__ __forceinline__ Verdict examine(const VerifyParams& p, int seq, int l
             qt.get(qx, true);
         }
         pt.get(px, true);
-        ok = u * qx[0] < px[0];
+        ok = (u < 0.f ? 0.f : u) * qx[0] < px[0];              // (NaN stays, and accepts nothing)
     }
     token = lane < drafts ? token : -1;
     const unsigned long long refused = ~__ballot(ok);            // (lane `drafts` refuses)
