@@ -120,7 +120,8 @@ def _ragged(starts, max_rows, rows, cache) -> _Ragged:
 class _Prepared:
     """A call with its descriptor built once."""
 
-    def __init__(self, name, args, keep, workspace=None, takes_workspace=False, stream=None):
+    def __init__(self, name, args, keep, workspace=None, takes_workspace=False, device=None, stream=None):
+        _need(workspace is None or (workspace.is_contiguous() and workspace.device == device), "workspace: dense memory on %s expected" % device)
         lib = binding.load_library()
         from ._calls import Operation
 
@@ -251,7 +252,7 @@ class PreparedAttention(_Prepared):
         a = _attention_args(cache, q, scale, starts, max_rows, max_len, causal, window)
         a.out = _rows(out, "out", q, q.shape[1], q.shape[2], q.shape[0])
         a.lse = None if lse is None else _whole(lse, "lse", "float32", q.shape[:2], q.device)
-        super().__init__("biq_attention", a, (cache, q, out, lse, starts), workspace, True, stream)
+        super().__init__("biq_attention", a, (cache, q, out, lse, starts), workspace, True, q.device, stream)
 
 
 def biq_attention(cache, q, out, lse=None, scale=None, starts=None, max_rows=None, max_len=0, causal=True, window=0,
@@ -283,7 +284,7 @@ class PreparedVerify(_Prepared):
                         tokens=_whole(tokens, "tokens", "int32", [seqs, drafts + 1], p.device),
                         accepted=_whole(accepted, "accepted", "int32", [seqs], p.device), type=_type(p), seqs=seqs, drafts=drafts,
                         vocab=vocab)
-        super().__init__("biq_verify_drafts", a, (p, q, draft_tokens, draft_lens, uniform, tokens, accepted), workspace, True, stream)
+        super().__init__("biq_verify_drafts", a, (p, q, draft_tokens, draft_lens, uniform, tokens, accepted), workspace, True, p.device, stream)
 
 
 def biq_verify_drafts(p, q, draft_tokens, uniform, tokens, accepted, draft_lens=None, workspace=None, stream=None) -> None:
