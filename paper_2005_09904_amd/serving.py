@@ -189,7 +189,7 @@ class KvCache:
         page = biq_cache_page_bytes(page_tokens, heads, head_dim)
         _need(page > 0, "page_tokens and head_dim: multiples of 16 up to 256")
         _need(store.dim() == 2 and store.shape[1] == page, "store: pages of %d bytes expected" % page)
-        _need(table.dim() == 2, "table: [seqs, pages of a sequence] expected")
+        _need(table.dim() == 2 and table.numel() > 0, "table: [seqs, pages of a sequence] expected")
         self.store, self.table, self.lens = store, table, lens
         self.seqs, self.page_tokens, self.heads, self.head_dim, self.format = table.shape[0], page_tokens, heads, head_dim, format
         self._c = _Cache(_whole(store, "store", "uint8", store.shape, store.device),

@@ -1,4 +1,4 @@
-"""What the binding checks of a workspace: where it is, and that it is dense.  Tensors without memory: every check comes before a call."""
+"""What the binding checks of workspaces (where they are, and that they are dense) and of tables.  Nothing is called."""
 import pytest
 import torch
 
@@ -39,3 +39,10 @@ def test_workspace(biq, call):
             call(biq, bad)
     for good in (None, torch.empty(4096, dtype=torch.uint8), torch.empty((4, 64))):
         call(biq, good)                                         # (prepared, not called)
+
+
+@pytest.mark.parametrize("shape", [(0, 4), (2, 0), (0, 0)])
+def test_a_table_without_sequences_or_pages(biq, shape):
+    page = biq.biq_cache_page_bytes(32, 2, 64)
+    with pytest.raises(ValueError, match="table"):
+        biq.KvCache(torch.zeros((5, page), dtype=torch.uint8), torch.zeros(shape, dtype=torch.int32), torch.zeros(shape[0], dtype=torch.int32), 32, 2, 64)
