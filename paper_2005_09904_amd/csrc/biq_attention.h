@@ -259,27 +259,17 @@ __device__ __forceinline__ float row_terms(bool negative, float (&x)[CH][2][8], 
 struct ScaleRange {
     bool narrow = true;
     float unit = 1.f;
-    // Before a step whose value scales are v (valid: tokens of the lane's block).
+    // Before a step whose value scales are v (valid: tokens of the lane's block).  (With branches prompts in fp32 are 2 to 3 % slower.)
     template <int NT>
     __device__ __forceinline__ void see(float v, int valid, float (&sum)[NT]) {
-        if (narrow) narrow = !__any(valid > 0 && !(v >= 0x1p-60f && v <= 0x1p40f));
-        if (!narrow && unit == 1.f && __any(valid > 0 && v < 0x1p-60f)) {
-            unit = 0x1p-32f;
+        narrow &= !__any((valid > 0) & !((v >= 0x1p-60f) & (v <= 0x1p40f)));
+        const float by = (unit == 1.f) & static_cast<bool>(__any((valid > 0) & (v < 0x1p-60f))) ? 0x1p-32f : 1.f;
+        unit *= by;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) sum[n] *= unit;
-        }
+        for (int n = 0; n < NT; ++n) sum[n] *= by;
     }
-    // After the last step: reference, sum of weights and sums of values in the same unit.
-    template <int NT, int TILES>
-    __device__ __forceinline__ void leave(float (&ref)[NT], f32x4 (&o)[NT][TILES]) const {
-        if (unit == 1.f) return;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            ref[n] += 32.f;
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) o[n][t] *= unit;
-        }
-    }
+    // After the last step: reference of a sum in that unit (the sums of values are to be multiplied by it).
+    __device__ __forceinline__ float reference(float ref) const { return unit == 1.f ? ref : ref + 32.f; }
 };
 struct Sight { int lo, hi, first, valid; };           // tokens seen: lo .. hi, and the block's first `valid`
 template <int PT> constexpr float kRefStart = PT == 1 ? 6.f : 13.f;
@@ -600,8 +590,6 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
             }
     }
 
-    scales.leave(ref, o);
-
     // ---- the waves' sums, joined: every wave's go to LDS, then every thread adds 4 elements of a row ------------------
     // Sums (tile i of 16 elements, lane) lie at 16-byte place 64 i + 16 grp + (col + 4 i + grp) % 16: neither the lanes that
     // write a tile nor those that read a row meet on a bank.
@@ -612,10 +600,10 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float total = sum_over_groups(l[n]);
-        if (grp == 0) *reinterpret_cast<f32x2*>(stats + (wave * ROWS + n * 16 + col) * 2) = (f32x2){ref[n], total};
+        if (grp == 0) *reinterpret_cast<f32x2*>(stats + (wave * ROWS + n * 16 + col) * 2) = (f32x2){scales.reference(ref[n]), total};
 #pragma unroll
         for (int i = 0; i < CH * 4; ++i)
-            sums[((wave * NT + n) * (CH * 4) + i) * 64 + grp * 16 + ((col + 4 * i + grp) & 15)] = o[n][i];
+            sums[((wave * NT + n) * (CH * 4) + i) * 64 + grp * 16 + ((col + 4 * i + grp) & 15)] = o[n][i] * scales.unit;
     }
     __syncthreads();
     const int quads = dim / 4, rows_here = rows_all - row0 < ROWS ? rows_all - row0 : ROWS;
@@ -648,18 +636,37 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     }
 }
 
-// Order of READS operands from LDS and the EACH products of every one of them: four reads ahead.  (Left alone, the compiler
-// reads each operand right before its products and waits for it.)
-template <int READS, int EACH>
-__device__ __forceinline__ void read_ahead() {
-    constexpr int kReads = 0x100, kProducts = 0x8;
-    __builtin_amdgcn_sched_group_barrier(kReads, 4, 0);
+// READS operands from LDS and the EACH products of every one of them: read(i) four ahead of use(i, operand).  (Left alone, the compiler
+// reads each operand right before its products and waits for it.)  Either the scheduler is asked for this order, which leaves it
+// free to place what else there is to do (two prompts with heads of 128: 806 us instead of 812), or, FENCED, the reads stand where they
+// are meant to be and only other vector and scalar instructions pass: with heads above 128 the scheduler gives up its own order now and
+// then (heads of 256 in bf16: 365 us instead of 288).
+template <int READS, int EACH, bool FENCED, typename Read, typename Use>
+__device__ __forceinline__ void read_ahead(const Read& read, const Use& use) {
+    constexpr int kAhead = 4;
+    if constexpr (FENCED) {
+        constexpr int kVectorAndScalar = 0x6;
+        f16x8 ring[kAhead];
 #pragma unroll
-    for (int i = 0; i < READS - 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kProducts, EACH, 0);
-        __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+        for (int i = 0; i < kAhead; ++i) ring[i] = read(i);
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            use(i, ring[i % kAhead]);
+            if (i + kAhead < READS) ring[i % kAhead] = read(i + kAhead);
+            __builtin_amdgcn_sched_barrier(kVectorAndScalar);
+        }
+    } else {
+        constexpr int kReads = 0x100, kProducts = 0x8;
+#pragma unroll
+        for (int i = 0; i < READS; ++i) use(i, read(i));
+        __builtin_amdgcn_sched_group_barrier(kReads, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < READS - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, EACH, 0);
+            __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kProducts, kAhead * EACH, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(kProducts, 4 * EACH, 0);
 }
 
 // Many rows of a sequence and head (prompts).  The waves of a workgroup hold different rows, NT tiles of 16 each, and share the
@@ -791,10 +798,15 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
 #pragma unroll
         for (int t = 0; t < VALUES; ++t) o[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
+    auto see_scales = [&]() {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) scales.see(vs[i], valid[i], l);
+    };
     if (begin < end) {
         request(begin);
         lay_down(buffers);
         __syncthreads();
+        see_scales();
     }
     int parity = 0;
     for (int stage = begin; stage < end; stage += 64 * STEPS) {
@@ -817,25 +829,18 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
             if (t0 >= end || t0 > any_hi || t0 + 63 < any_lo) continue;
             f32x4 s[NT][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) s[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            read_ahead<4 * KEYS, QT * NT, (CH > 2)>([&](int r) { return from[(r / KEYS * 2 * CH + r % KEYS) * 64 + lane]; }, [&](int r, f16x8 k) {
+                const int t = r / KEYS, c = r % KEYS / 2, h = r % KEYS % 2;
 #pragma unroll
-                for (int c = 0; c < CH; ++c)
+                for (int e = 0; e < QT; ++e)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (2 * c + h >= KEYS) continue;
-                        const f16x8 k = from[((t * CH + c) * 2 + h) * 64 + lane];
-#pragma unroll
-                        for (int e = 0; e < QT; ++e)
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[n][c][h][e], s[n][t], 0, 0, 0);
-                    }
-            }
-            read_ahead<4 * KEYS, QT * NT>();
+                    for (int n = 0; n < NT; ++n) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[n][c][h][e], s[n][t], 0, 0, 0);
+            });
             __builtin_amdgcn_sched_barrier(0);
             const bool whole = step_valid[i] && t0 + 63 <= all_hi && t0 >= all_lo;
-            scales.see(vscale[i], nvalid[i], l);
             f16x8 w[NT][2][PT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -849,24 +854,20 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
+            read_ahead<2 * VALUES, PT * NT, (CH > 2)>([&](int r) { return from[SIDE + r * 64 + lane]; }, [&](int r, f16x8 v) {
+                const int t = r / 2, h = r % 2;
 #pragma unroll
-            for (int t = 0; t < VALUES; ++t)
+                for (int e = 0; e < PT; ++e)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const f16x8 v = from[SIDE + (t * 2 + h) * 64 + lane];
-#pragma unroll
-                    for (int e = 0; e < PT; ++e)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[n][h][e], o[n][t], 0, 0, 0);
-                }
-            read_ahead<2 * VALUES, PT * NT>();
+                    for (int n = 0; n < NT; ++n) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[n][h][e], o[n][t], 0, 0, 0);
+            });
         }
         __builtin_amdgcn_sched_barrier(0);
         parity ^= 1;
         lay_down(buffers + parity * STEPS * 2 * SIDE);
         __syncthreads();
+        see_scales();
     }
-    scales.leave(ref, o);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float total = sum_over_groups(l[n]);
@@ -875,8 +876,8 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
         const long long to = place[n].row * p.out.row_stride + place[n].head * p.out.head_stride + grp * 4;
 #pragma unroll
         for (int i = 0; i < VALUES; ++i)
-            if (FULL || i * 16 < dim) store_row4<TYPE>(p.out, to + i * 16, o[n][i] * inv);
-        if (p.lse && grp == 0) p.lse[place[n].row * p.q_heads + place[n].head] = log_sum(ref[n], total);
+            if (FULL || i * 16 < dim) store_row4<TYPE>(p.out, to + i * 16, o[n][i] * scales.unit * inv);
+        if (p.lse && grp == 0) p.lse[place[n].row * p.q_heads + place[n].head] = log_sum(scales.reference(ref[n]), total);
     }
 }
 
