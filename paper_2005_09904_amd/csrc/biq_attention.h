@@ -535,6 +535,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         const int nvalid = valid;
         const bool step_valid = all_valid;
         __builtin_amdgcn_sched_barrier(0);                      // (the requests stay ahead of the products)
+        scales.see(vscale, nvalid, l);
         f32x4 s[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -564,7 +565,6 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
 #pragma unroll
             for (int t = 0; t < CH * 4; ++t) vc[t] = first_codes(vc[t], nvalid);
         }
-        scales.see(vscale, nvalid, l);
         f16x8 w[NT][2][PT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
