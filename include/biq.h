@@ -352,8 +352,8 @@ biq_status biq_gemm_noalloc(const uint8_t* K, const float* alpha, const float* X
  *
  * Every operation takes one descriptor (read during the call only), a workspace where it needs one, and a stream.  The
  * general rules above hold: device pointers of the caller, no allocation, no synchronisation, statuses.  Differences:
- *   - Elements are 32-bit, bfloat16 or 16-bit floats (biq_type).  Arithmetic is in 32 bits or more whatever the type, and a
- *     result is rounded once, to the output's type.
+ *   - Elements are 32-bit, bfloat16 or 16-bit floats (biq_type).  Arithmetic is in 32 bits or more whatever the type, but for the
+ *     factors that biq_attention gives the matrix cores (described there), and a result is rounded once, to the output's type.
  *   - Infinities and NaN are values like others: they show in the results of the rows that depend on them, and in no others.
  *   - Rows of a tensor have strides of their own (biq_rows).  Elements of one head are adjacent.  Any alignment of the
  *     element's size is accepted; rows at multiples of 4 bytes are faster (16 for biq_rotary).
@@ -429,7 +429,8 @@ biq_status biq_rotary(const biq_rotary_args* args, void* stream);
  *
  * format BIQ_CACHE_INT8: integers in [-127, 127], scale = (largest magnitude of the block) * (1 / 127 in 32 bits), codes rounded to nearest, ties
  * to even.  BIQ_CACHE_FP8: 8-bit floats with 4 exponent and 3 fraction bits (OCP E4M3), scale = the least power of two that
- * makes every magnitude at most 448; rounded to nearest, ties to even.  Integers have the smaller mean error (0.9 % of the
+ * makes every magnitude at most 448; rounded to nearest, ties to even.  (Its codes for NaN, 127 and 255, are never written, and are
+ * not to stand among a sequence's tokens: they would show in rows that do not see them.)  Integers have the smaller mean error (0.9 % of the
  * standard deviation for normal values, floats 2.5 %), floats keep small channels beside large ones.
  *
  * Tokens of a block that came earlier are written anew where a later one needs a larger scale (a block's scale never falls
@@ -458,7 +459,9 @@ size_t biq_cache_page_bytes(int page_tokens, int heads, int head_dim);
  * Rows of a call that belong to sequences: sequence s has rows starts[s] .. starts[s + 1] (device, seqs + 1 numbers that do not
  * fall, bounded to [0, rows] on the device), or rows s * max_rows .. (s + 1) * max_rows where starts is NULL (then rows must be
  * seqs * max_rows).  The n rows of sequence s are its last n tokens: row i is token lens[s] - n + i.  max_rows bounds the rows of
- * a sequence that are served: its first ones, the same tokens whether or not rows follow (`rows` is always enough).
+ * a sequence that are served: its first ones, the same tokens whether or not rows follow.  `rows` is always enough, but a call is
+ * planned for max_rows in every sequence: single tokens with max_rows of many are served by the kernel for prompts, and workgroups
+ * are launched for rows that are not there.  rows and max_rows are at least 1 (BIQ_EINVAL): a caller without rows makes no call.
  */
 typedef struct {
     const int32_t* starts;
@@ -499,7 +502,8 @@ biq_status biq_cache_read(const biq_cache_read_args* args, void* stream);
  * block's value scale is small beside the row's largest, none below 2^-38 of it); those of a bf16 output are one (11 bits, none below
  * 2^-31).  Sums, maxima and the softmax are in 32 bits.  Deterministic.
  * max_len: about the largest of lens (0: table_stride * page_tokens).  It only sets how the tokens are split over workgroups:
- * results are right whatever it is (splits differ in the order of additions).  workspace: biq_attention_workspace_bytes(), 16-byte aligned (may be 0).
+ * results are right whatever it is (splits differ in the order of additions).  workspace: biq_attention_workspace_bytes(), 16-byte
+ * aligned (may be 0).  BIQ_EUNSUPPORTED: rows * q_heads of 2^31 and more, heads above 65536.
  */
 typedef struct {
     biq_cache cache;

@@ -34,7 +34,7 @@ struct AttendParams {
 };
 
 // What a workgroup spends on a unit beside its steps (rows, first keys, joining its waves, results), in steps: 32 sequences of 410 ..
-// 4096 tokens take 44.7, 41.7, 39.9, 40.8 us with 2, 5, 10, 14.
+// 4096 tokens take 44.7, 41.7, 39.9, 40.8 us with 2, 5, 10, 14, five rows of 16 sequences 50.0, 50.0, 48.6, 47.7.
 constexpr int kUnitCost = 10;
 
 // A unit is a tile of rows of a sequence and head; its work is steps of 64 tokens, [base, base + 64 steps), the same for all
@@ -405,10 +405,10 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 w, int valid) {
 // steps of 64 tokens in turn, straight from memory to registers: every code is used by one wave only.  Keys are requested a
 // step ahead, values before the scores.  The waves' sums are joined through LDS.
 //
-// Memory bounds it where units are long: one token of 32 heads over 131071 tokens (269 MB, fp8, bf16) takes 49.8 us, 5.4 TB/s.
+// Memory bounds it where units are long: one token of 32 heads over 131071 tokens (269 MB, fp8, bf16) takes 50.4 us, 5.3 TB/s.
 // Where a workgroup has several shorter units, what it does beside their steps shows (10 steps' worth each), and with 32-bit rows
 // the instructions of a step (4 waves of a CU issue 5000 cycles each: 320 of 520 vector instructions turn codes into 16-bit
-// floats): 32 sequences of 410 .. 4096 tokens (140 MB, int8, fp32) take 35 us, 4 TB/s, 5 rows of 16 sequences 40 us
+// floats): 32 sequences of 410 .. 4096 tokens (155 MB, int8, fp32) take 35 us, 4.4 TB/s, 5 rows of 16 sequences 40 us
 // (42 where 16-bit rows were converted one load after the other).
 // CH: 64 elements of a head each; FULL: the head has all of them; NT: tiles of 16 rows.
 template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES>
@@ -419,7 +419,6 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, grp = lane >> 4;
     const int dim = FULL ? 64 * CH : p.cache.dim;
-    const long long codes = static_cast<long long>(p.cache.heads) * p.cache.page_blocks * kCacheBlock * dim;
     const int kblock = col >> 2;                                // block of this lane's key rows, 0 .. 3
 
     // steps of this workgroup: a share of all, or all of one unit
@@ -676,7 +675,7 @@ __device__ __forceinline__ void read_ahead(const Read& read, const Use& use) {
 //
 // What the SIMDs issue bounds it: matrix products (64 a step of a wave with two tiles of bf16 rows, 19 cycles each), exponentials (32, 27
 // cycles) and other vector instructions (240, 3 cycles) measured apart add up to 2800 cycles, a step takes 2300.  Two prompts of
-// 4096 rows over 8192 tokens, 32 heads of 128: 802 us, 1.03 PFLOP/s.  Tiles of 16 x 16 rather than 32 x 32 as their products
+// 4096 rows over 8192 tokens, 32 heads of 128: 806 us, 1.02 PFLOP/s.  Tiles of 16 x 16 rather than 32 x 32 as their products
 // are 20 % faster a flop here and their layout gives a lane one scale.
 template <int TYPE, int FMT, int CH, bool FULL, bool HALF, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kernel(const AttendParams p) {
@@ -689,7 +688,6 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
     const int dim = FULL ? 64 * CH : p.cache.dim;
-    const long long codes = static_cast<long long>(p.cache.heads) * p.cache.page_blocks * kCacheBlock * dim;
     // Later rows see more tokens and come first.  Where the sequences and heads can be dealt to the XCDs evenly, each keeps to
     // its own, whose tokens then stay in its L2.
     const int pairs = p.seqs * p.cache.heads, group = p.first + blockIdx.x;

@@ -5,8 +5,8 @@
 // already come with one load to the lanes that may have to round them anew.
 //
 // The writer waits for loads that depend on each other (lengths, page; then rows, angles and codes, all requested before the first
-// is used: 17.5 us instead of 26): 10300 tokens of 8 heads of 128 (bf16 to fp8, 63 MB) take 17.5 us, 3.6 TB/s, one token of 64
-// sequences 6.4 us.  The reader is bound by its writes: 105 MB (to fp32) take 20.8 us, 5.0 TB/s.
+// is used: 17.5 us instead of 26): 8755 tokens of 8 heads of 128 (bf16 to fp8, 54 MB) take 17.5 us, 3.1 TB/s, one token of 64
+// sequences 6.2 us.  The reader is bound by its writes where there are many: 90 MB (to fp32) take 20.8 us, 4.3 TB/s.
 #pragma once
 
 #include "biq_serve.h"
@@ -42,7 +42,9 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t bits, float old) {
     const float amax = __uint_as_float(bits);
     float scale;
     if constexpr (FMT == BIQ_CACHE_INT8) {
-        scale = amax * (1.0f / 127.0f);                      // (a product with the rounded constant: as biq.h says)
+        // a product with the rounded constant, as biq.h says: what a division by 127 becomes in tensor programs on GPUs, so that their
+        // codes and these agree where x / scale is halfway between two (the correctly rounded quotient differs in its last bit now and then)
+        scale = amax * (1.0f / 127.0f);
     } else {
         // 448 = 1.75 * 2^8: exponent - 8, one more for a larger significand
         const uint32_t e = (bits >> 23) - 8u + ((bits & 0x7fffffu) > 0x600000u ? 1u : 0u);

@@ -104,7 +104,10 @@ AttendPlan attend_plan(const biq_attention_args& a) {
     // Few rows or many: by the time of a step of 64 tokens (bf16, us; heads of 64, 128, 192, 256).  For few rows the CUs share the
     // steps of all units: kRows each.  For many a workgroup walks through its steps alone: kAlone each, kShared where two of
     // them are on a CU (one for heads above 128).  Measured for 8 heads of 4, 1 .. 16 sequences of 4 .. 512 rows over 1024 and
-    // 8192 tokens: 64 rows of 16 sequences and 8192 tokens 90 us by rows, 217 by tiles, 512 rows 660 and 318.
+    // 8192 tokens: 64 rows of 16 sequences and 8192 tokens 90 us by rows, 217 by tiles, 512 rows 660 and 318.  Other types change
+    // both times alike: over these sizes in bf16, fp32 and fp16 the choice takes 1.00 to 1.02 of the better one's time on average for each
+    // head size, at most 1.05 for heads of 64 and 128, 1.18 for 192 (256 rows of 16 sequences) and 1.45 for 256 (one sequence, tiles for half
+    // of the CUs).
     static const double kRows[4] = {0.46, 0.64, 0.95, 1.19}, kAlone[4] = {1.25, 1.64, 2.0, 2.27}, kShared[4] = {1.7, 2.4, 2.0, 2.27};
     const int ch = chunks_of(c.head_dim) - 1;
     const int few = rows <= 16 || ch > 1 ? 16 : 32, many = ch <= 1 ? 128 : 64;
@@ -114,7 +117,7 @@ AttendPlan attend_plan(const biq_attention_args& a) {
     if (rows > 16 && by_tiles < by_rows) {
         pl.tiles = true;
         // Eight waves a workgroup spread the tokens' conversion over twice the rows, but are fewer workgroups: where these still
-        // fill the GPU four times (two prompts of 4096 rows: 808 us instead of 854; six ragged ones of up to 1500: 100 instead of 87).
+        // fill the GPU four times (two prompts of 4096 rows: 806 us instead of 848; six ragged ones of up to 1500: 93 instead of 79).
         const long long wide = pairs * ((rows + 255) / 256);
         pl.waves = ch <= 1 && wide >= 4 * kCus ? 8 : 4;
         pl.nt = ch <= 1 ? 2 : 1;

@@ -6,6 +6,9 @@ their buffers (calling the object only crosses the C ABI).  Tensors give their o
 uses the stream that it is given or torch's current one at preparation; its tensors must stay alive and in place (it keeps
 references to them).
 
+Ragged calls take starts (int32 [seqs + 1]) and max_rows, the most rows that a sequence has.  Left open, max_rows is all rows: right,
+but single tokens then run as prompts do.
+
 Checked here is what the C functions cannot see of tensors: their number of dimensions, sizes that have to agree, types, devices.
 """
 from __future__ import annotations
