@@ -178,3 +178,14 @@ def test_many_rows_in_a_graph(biq):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dim", [16, 32, 48])
+@pytest.mark.parametrize("typ", ["fp32", "bf16", "fp16"])
+def test_many_rows_that_fill_the_gpu_small_heads(biq, typ, dim):
+    """Rows enough for workgroups of eight waves; a sample of them is checked."""
+    lens, counts = (1100, 700, 1500), [1100, 650, 1300]
+    pages = held(lens, 16, dim, 64, "int8", dim)
+    q = au.rows_like(counts, 96, dim, typ, 3)
+    for window in (0, 200):
+        au.check(biq, pages, counts, q, typ, window=window, sample=[0, 1, 217, 649, 1057, 1299])
