@@ -548,6 +548,115 @@ typedef struct {
 size_t biq_verify_workspace_bytes(int seqs, int vocab);
 biq_status biq_verify_drafts(const biq_verify_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- the end of a decoder step: norm, products with 4-bit weights, logits ---- */
+
+/*
+ * These follow the rules of the operations above: one descriptor, strides in elements, any alignment of the element's size,
+ * arithmetic in 32 bits or more, infinities and NaN only in the rows that depend on them.
+ */
+
+/*
+ * Root-mean-square norm with the residual's addition, per row of n elements:
+ *     s = x + residual,  r = 1 / sqrt(mean(s^2) + eps),  y = s r (weight + weight_add).
+ * residual NULL: s = x.  sum (NULL, or rows like x; needs residual): s, rounded to x's type; the norm is of s before that rounding.
+ * weight (NULL: ones) float [n]; weight_add: 1 for weights that are stored less 1.  y (NULL, or rows of y_type).
+ * codes (NULL, or rows of n bytes) with scales float [rows][groups]: y in 8 bits, as the cache holds its blocks.  A group is
+ * `group` adjacent elements (32, 64 or 128; the last one may be shorter), or the row (0).  With t = s (weight + weight_add):
+ *   BIQ_CACHE_INT8: u = (largest |t| of the group) * (1 / 127 in 32 bits), codes rn(t * (1 / u)) in [-127, 127];
+ *   BIQ_CACHE_FP8 : u = the least power of two that makes every |t| at most 448 u, codes t / u rounded to nearest (E4M3);
+ * scale = u r.  Groups whose largest |t| is below 2^-100 are zeros with scale 0; with an infinity or a NaN: codes 0, scale NaN.
+ * x, residual and sum have one type.  sum may be x or residual, y may be x (same data, type and stride); otherwise outputs overlap
+ * nothing.  One of y and codes at least.  n <= 2^24 (BIQ_EUNSUPPORTED beyond).
+ * Squares whose sum leaves the range of 32 bits are summed in 64.
+ */
+typedef struct {
+    const void* x;
+    const void* residual;
+    void* sum;
+    const float* weight;
+    void* y;
+    void* codes;
+    float* scales;
+    int64_t x_stride, residual_stride, sum_stride, y_stride, code_stride;
+    int type, y_type, rows, n, group, format;
+    float eps, weight_add;
+} biq_norm_args;
+biq_status biq_norm(const biq_norm_args* args, void* stream);
+
+/*
+ * Weights in 4 bits with a scale per group, for the layers that need more than binary codes (a model's output head, for
+ * one): W[i][j] = scales[i][j / group] * code[i][j], codes -8 .. 7, scales bfloat16, group 32, 64 or 128 elements of a row.
+ *
+ * Packed: records of 16 rows and 128 elements, [ceil(m / 16)][ceil(n / 128)], each 1024 bytes of codes and 128 / group * 32 of
+ * scales; what lies behind the last row or element is code 0 with scale 0.  16-byte aligned, biq_packed4_bytes() bytes (0 on
+ * invalid arguments).  m <= 2^28, n <= 2^24 (BIQ_EUNSUPPORTED beyond).
+ *   biq_pack4:     from codes int8 [m][n] (bounded to -8 .. 7) and scales float [m][ceil(n / group)] (rounded to bfloat16).
+ *   biq_quantize4: from W (rows `stride` apart, of `type`): scale = (largest magnitude of the group) * (1 / 7 in 32 bits) in bfloat16, codes
+ *                  rn(w * (1 / scale)).  Groups below 2^-100 are zeros, groups with an infinity or a NaN have scale NaN.
+ *   biq_unpack4:   the values, float (rows `stride` apart).
+ */
+size_t biq_packed4_bytes(int m, int n, int group);
+biq_status biq_pack4(const int8_t* codes, const float* scales, uint8_t* packed, int m, int n, int group, void* stream);
+biq_status biq_quantize4(const void* W, int64_t stride, int type, uint8_t* packed, int m, int n, int group, void* stream);
+biq_status biq_unpack4(const uint8_t* packed, float* W, int64_t stride, int m, int n, int group, void* stream);
+
+/*
+ * Y[b][i] = sum_j W[i][j] X[b][j] with packed weights.  X: rows of x_type, one of biq_type or codes (BIQ_X_INT8, BIQ_X_FP8) with
+ * x_scales float [batch][groups], a group being x_group adjacent elements (32, 64 or 128) or the row (0): what biq_norm writes.
+ * Y: rows of y_type.
+ *
+ * Weights' codes, X's codes and 16-bit floats enter the matrix cores as they are.  32-bit and bfloat16 elements are scaled by a power
+ * of two per 128 elements and keep 22 bits (bfloat16 all of theirs), none below 2^-39 of the largest of the 128.  Sums are in 32 bits.
+ * Deterministic.  A vector with an infinity or a NaN gives NaN or infinities.
+ * batch <= 65535 (BIQ_EUNSUPPORTED beyond).  workspace: biq_gemm4_workspace_bytes(), 16-byte aligned (0 for a few vectors).
+ */
+typedef enum { BIQ_X_INT8 = 3, BIQ_X_FP8 = 4 } biq_x_type;
+typedef struct {
+    const uint8_t* weights;
+    const void* x;
+    const float* x_scales;
+    void* y;
+    int64_t x_stride, y_stride;
+    int m, n, group, batch, x_type, x_group, y_type;
+} biq_gemm4_args;
+size_t biq_gemm4_workspace_bytes(const biq_gemm4_args* args);
+biq_status biq_gemm4(const biq_gemm4_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * What happens to logits between a model's output and the choice of tokens.  x [seqs][rows][vocab] (the rows of a sequence
+ * are those of its drafted tokens and the one after them, as biq_verify_drafts takes them), in this order, per token v of row i of sequence s:
+ *   1. tokens said before.  history int32 [seqs][width], lens[s] of them (bounded to [0, width]), the first prompt_lens[s] (NULL: 0) the
+ *      prompt's; drafts int32 [seqs][rows - 1] (NULL: none): the first i of a sequence's have been said before its row i.
+ *      If v is among them: z > 0 ? z / repetition[s] : z * repetition[s].  If v was said c > 0 times other than in the prompt:
+ *      z - c frequency[s] - presence[s].  Each of the three NULL: left out.  Tokens outside [0, vocab) count nowhere.
+ *   2. biases: of the bias_tokens [seqs][biases] that are v the bias_values are added, in the list's order.
+ *   3. temperature[s] (NULL: 1): z * (1 / temperature).  One that is not above 0 leaves z.
+ *   4. mask: bit v % 32 of the 32-bit word v / 32 of a row is 0: z = -infinity, whatever it was.
+ * out: z, or with `probabilities` exp(z) / sum exp(z) over the row (temperature not above 0: 1 at the largest z, the first of
+ * several, 0 elsewhere).  A row whose every z is -infinity has probabilities 0.  A NaN that is not masked makes its row's probabilities NaN.
+ * out may be x (same data, type and strides).  vocab <= 2^22, biases <= 4096 (BIQ_EUNSUPPORTED beyond).  Deterministic.
+ * workspace: biq_logits_workspace_bytes(), 16-byte aligned (may be 0; none is needed without probabilities).
+ */
+typedef struct {
+    const void* x;
+    void* out;
+    int64_t x_seq_stride, x_stride, out_seq_stride, out_stride, mask_seq_stride, mask_stride;
+    const int32_t* history;
+    const int32_t* lens;
+    const int32_t* prompt_lens;
+    const int32_t* drafts;
+    const float* repetition;
+    const float* presence;
+    const float* frequency;
+    const float* temperature;
+    const int32_t* bias_tokens;
+    const float* bias_values;
+    const uint32_t* mask;
+    int type, out_type, seqs, rows, vocab, width, biases, probabilities;
+} biq_logits_args;
+size_t biq_logits_workspace_bytes(int seqs, int rows, int vocab);
+biq_status biq_logits(const biq_logits_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

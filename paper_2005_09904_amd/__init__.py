@@ -14,3 +14,7 @@ from .serving import (  # noqa: F401
     biq_attention_workspace_bytes, biq_cache_append, biq_cache_page_bytes, biq_cache_read, biq_rotary, biq_rotary_frequencies,
     biq_rotary_table, biq_verify_drafts, biq_verify_workspace_bytes,
 )
+from .step import (  # noqa: F401
+    PreparedGemm4, PreparedLogits, PreparedNorm, biq_gemm4, biq_gemm4_workspace_bytes, biq_logits, biq_logits_workspace_bytes,
+    biq_norm, biq_pack4, biq_packed4_bytes, biq_quantize4, biq_unpack4,
+)

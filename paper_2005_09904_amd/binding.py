@@ -25,6 +25,9 @@ EXPORTS = [
     # (serving.py)
     "biq_rotary_frequencies", "biq_rotary_table", "biq_rotary", "biq_cache_page_bytes", "biq_cache_append", "biq_cache_read",
     "biq_attention_workspace_bytes", "biq_attention", "biq_verify_workspace_bytes", "biq_verify_drafts",
+    # (step.py)
+    "biq_norm", "biq_packed4_bytes", "biq_pack4", "biq_quantize4", "biq_unpack4", "biq_gemm4_workspace_bytes", "biq_gemm4",
+    "biq_logits_workspace_bytes", "biq_logits",
 ]
 
 
@@ -114,6 +117,15 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "biq_attention": (I, [P, P, Z, P]),
         "biq_verify_workspace_bytes": (Z, [I, I]),
         "biq_verify_drafts": (I, [P, P, Z, P]),
+        "biq_norm": (I, [P, P]),
+        "biq_packed4_bytes": (Z, [I, I, I]),
+        "biq_pack4": (I, [P, P, P, I, I, I, P]),
+        "biq_quantize4": (I, [P, ctypes.c_int64, I, P, I, I, I, P]),
+        "biq_unpack4": (I, [P, P, ctypes.c_int64, I, I, I, P]),
+        "biq_gemm4_workspace_bytes": (Z, [P]),
+        "biq_gemm4": (I, [P, P, Z, P]),
+        "biq_logits_workspace_bytes": (Z, [I, I, I]),
+        "biq_logits": (I, [P, P, Z, P]),
     }
     for name, (res, args) in [*sig.items(), *serving.items()]:
         fn = getattr(lib, name)

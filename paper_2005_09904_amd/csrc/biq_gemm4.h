@@ -1,0 +1,388 @@
+// Products with 4-bit weights (biq_gemm4), their layout and quantiser.
+//
+//   Y[b][i] = sum over groups g of scale[i][g] * sum over the group's j of code[i][j] X[b][j]
+//
+// Layout: records of 16 rows and 128 elements of each, all records of 16 rows one after the other.  A record holds 64 x 16 bytes
+// of codes, then the bfloat16 scales [128 / group][16].  Lane l of a wave takes the l-th 16 bytes: row l % 16, and of each of
+// the four spans of 32 elements the 8 from 8 (l / 16) on (a dword): the left operand of one 16 x 16 x 32 product per dword, whose
+// 32 elements belong to one group.  A dword holds code + 8 of element 2 i in its bits 4 i and of element 2 i + 1 in its bits
+// 16 + 4 i: ((w >> 4 i) & 0x000f000f) | 0x64006400 is two 16-bit floats 1024 + code + 8.
+// What is missing of the last rows and elements has code 0 and scale 0.
+#pragma once
+
+#include "biq_serve.h"
+
+namespace biq {
+
+constexpr int kBlock4 = 128;                         // elements of a record's rows
+constexpr int kInt8 = 3, kFp8 = 4;                   // types of X beside biq_type: codes
+
+struct Gemm4Params {
+    const uint8_t* weights;
+    const void* x;
+    const float* x_scales;   // [batch][x_groups], codes only
+    void* y;
+    uint8_t* operands;       // X as operands, where there are many vectors: groups of `columns` of them
+    long long x_stride, y_stride;
+    int m, n, batch, blocks, tiles;
+    int record;              // bytes of a record
+    int group;               // 32, 64 or 128
+    int x_group, x_groups;   // elements of a group of X's scales (0: the row), groups of a row
+    int y_type;
+    int splits;              // waves that share a tile's blocks
+    int columns;
+    unsigned first;
+};
+
+__device__ __forceinline__ float bf16_up(uint32_t bits) { return __uint_as_float(bits << 16); }
+
+// 8 codes as 16-bit floats (exact).
+__device__ __forceinline__ f16x8 weights_f16(uint32_t w) {
+    union { f16x8 v; f16x2 p[4]; uint32_t w[4]; } r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.w[i] = ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u;
+        r.p[i] -= (f16x2){1032.0f16, 1032.0f16};
+    }
+    return r.v;
+}
+
+// ---- laying out ---------------------------------------------------------------------------------------------
+
+// One thread per dword of codes; scale(row, group) is asked for once per scale.
+template <typename Code, typename Scale>
+__device__ __forceinline__ void lay_out4(uint8_t* record, int tile, int block, int dword, int m, int n, int group, const Code& code, const Scale& scale) {
+    const int lane = dword >> 2, j = dword & 3, row = tile * 16 + (lane & 15), e0 = block * kBlock4 + 32 * j + 8 * (lane >> 4);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int c = row < m && e0 + i < n ? code(row, e0 + i) : 0;
+        w |= static_cast<uint32_t>(c + 8) << (i & 1 ? 16 + 4 * (i >> 1) : 4 * (i >> 1));
+    }
+    reinterpret_cast<uint32_t*>(record)[dword] = w;
+    const int per = kBlock4 / group;                            // scales of a row in a record
+    if (dword < 16 * per) {
+        const int r = tile * 16 + (dword & 15), g = block * per + (dword >> 4);
+        const bool there = r < m && g * group < n;
+        reinterpret_cast<uint16_t*>(record + 1024)[dword] = there ? scale(r, g) : 0;
+    }
+}
+
+// To bfloat16, to nearest, ties to even (NaN stays one).
+__device__ __forceinline__ uint16_t bf16_bits(float x) {
+    union { __bf16 h; uint16_t u; } r;
+    r.h = static_cast<__bf16>(x);
+    return r.u;
+}
+
+struct Pack4Params {
+    const int8_t* codes;     // [m][n]
+    const void* source;      // the quantiser's W [m][n]
+    const float* scales;     // [m][groups]
+    uint8_t* packed;
+    float* out;              // biq_unpack4's W
+    long long stride;
+    int m, n, group, groups, blocks, record;
+    unsigned first;
+};
+
+static __global__ __launch_bounds__(256) void pack4_kernel(const Pack4Params p) {
+    const long long at = p.first + blockIdx.x;
+    const int tile = static_cast<int>(at / p.blocks), block = static_cast<int>(at - static_cast<long long>(tile) * p.blocks);
+    lay_out4(p.packed + at * p.record, tile, block, threadIdx.x, p.m, p.n, p.group,
+             [&](int r, int e) {
+                 const int c = p.codes[static_cast<long long>(r) * p.n + e];
+                 return c < -8 ? -8 : c > 7 ? 7 : c;
+             },
+             [&](int r, int g) { return bf16_bits(p.scales[static_cast<long long>(r) * p.groups + g]); });
+}
+
+// scale = (largest magnitude of the group) * (1 / 7) to bfloat16, codes rn(w * (1 / scale)) in -8 .. 7; groups below 2^-100: zeros;
+// groups with an infinity or a NaN: NaN.  A workgroup per record: scales first, through LDS.
+template <int TYPE>
+__global__ __launch_bounds__(256) void quantize4_kernel(const Pack4Params p) {
+    __shared__ float scales[64], factors[64];                   // [group in the record][row]
+    const long long at = p.first + blockIdx.x;
+    const int tile = static_cast<int>(at / p.blocks), block = static_cast<int>(at - static_cast<long long>(tile) * p.blocks);
+    {
+        // 16 threads a row, 8 elements each: 4, 8 or 16 of them are a group
+        const int row = tile * 16 + (threadIdx.x >> 4), e0 = block * kBlock4 + 8 * (threadIdx.x & 15);
+        uint32_t most = 0;
+        for (int i = 0; i < 8; ++i) {
+            const float x = row < p.m && e0 + i < p.n ? load_elem<TYPE>(p.source, row * p.stride + e0 + i) : 0.f;
+            const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
+            most = most > bits ? most : bits;
+        }
+        for (int d = 1; d < p.group / 8; d *= 2) {
+            const uint32_t other = __shfl_xor(most, d);
+            most = most > other ? most : other;
+        }
+        if ((threadIdx.x & 15) % (p.group / 8) == 0) {
+            const int to = (threadIdx.x & 15) / (p.group / 8) * 16 + (threadIdx.x >> 4);
+            const bool bad = most >= 0x7f800000u;
+            const float scale = bad ? __uint_as_float(0x7fc00000u) : most < 0x0d800000u ? 0.f : bf16_up(bf16_bits(__uint_as_float(most) * (1.0f / 7.0f)));
+            scales[to] = scale;
+            factors[to] = scale > 0.f && !bad ? 1.0f / scale : 0.f;
+        }
+    }
+    __syncthreads();
+    lay_out4(p.packed + at * p.record, tile, block, threadIdx.x, p.m, p.n, p.group,
+             [&](int r, int e) {
+                 const float f = factors[(e % kBlock4) / p.group * 16 + (r & 15)];
+                 const float x = f == 0.f ? 0.f : __builtin_rintf(load_elem<TYPE>(p.source, r * p.stride + e) * f);
+                 return static_cast<int>(x < -8.f ? -8.f : x > 7.f ? 7.f : x);
+             },
+             [&](int r, int g) { return bf16_bits(scales[g * p.group % kBlock4 / p.group * 16 + (r & 15)]); });
+}
+
+// The weights' values.
+static __global__ __launch_bounds__(256) void unpack4_kernel(const Pack4Params p) {
+    const long long at = p.first + blockIdx.x;
+    const int tile = static_cast<int>(at / p.blocks), block = static_cast<int>(at - static_cast<long long>(tile) * p.blocks);
+    const int lane = threadIdx.x >> 2, j = threadIdx.x & 3, row = tile * 16 + (lane & 15), e0 = block * kBlock4 + 32 * j + 8 * (lane >> 4);
+    const uint8_t* record = p.packed + at * p.record;
+    const uint32_t w = reinterpret_cast<const uint32_t*>(record)[threadIdx.x];
+    const float scale = bf16_up(reinterpret_cast<const uint16_t*>(record + 1024)[32 * j / p.group * 16 + (lane & 15)]);
+    if (row >= p.m) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (e0 + i < p.n)
+            p.out[row * p.stride + e0 + i] = static_cast<float>(static_cast<int>(w >> (i & 1 ? 16 + 4 * (i >> 1) : 4 * (i >> 1)) & 15u) - 8) * scale;
+}
+
+// ---- X as operands ------------------------------------------------------------------------------------------
+
+// 32-bit elements are two 16-bit floats, the others one.
+template <int XT> constexpr int kTerms4 = XT == BIQ_F32 ? 2 : 1;
+template <int XT> struct X4 { typedef typename Elem<XT>::T T; };
+template <> struct X4<kInt8> { typedef int8_t T; };
+template <> struct X4<kFp8> { typedef uint8_t T; };
+
+// 8 elements of an input vector (zeros behind its end) as terms; unit: what a 1 stands for.  The 16 lanes of a block of 128
+// call this together: 32-bit and bf16 elements are scaled by a power of two, the block's largest magnitude to [2^14, 2^15).  Elements
+// keep 22 bits (8 of bf16), and none below 2^-39 of the block's largest.
+template <int XT>
+__device__ __forceinline__ float operand8(const typename X4<XT>::T (&raw)[8], int e, int n, f16x8 (&out)[kTerms4<XT>]) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (XT == kFp8) x[i] = __builtin_amdgcn_cvt_f32_fp8(raw[i], 0);
+        else x[i] = static_cast<float>(raw[i]);
+        if (e + i >= n) x[i] = 0.f;
+    }
+    float unit = 1.f;
+    if constexpr (XT == BIQ_F32 || XT == BIQ_BF16) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
+            most = most > bits ? most : bits;
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2) {
+            const uint32_t other = __shfl_xor(most, d);
+            most = most > other ? most : other;
+        }
+        int b = static_cast<int>(most >> 23);                   // biased exponent
+        b = most == 0 ? 127 + 14 : b < 27 ? 27 : b;
+        const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 + 127 - b) << 23);
+        unit = __uint_as_float(static_cast<uint32_t>(b - 14) << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= up;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[0][i] = static_cast<_Float16>(x[i]);
+    if constexpr (kTerms4<XT> == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[1][i] = static_cast<_Float16>(x[i] - static_cast<float>(out[0][i]));
+    }
+    return unit;
+}
+
+// ---- the product --------------------------------------------------------------------------------------------
+
+// Where the operands of X are: [block][span of 32][term][lane / 16][column] of 16 bytes, and what units they have: [block][scale]
+// [column].  columns: how many there are of them.
+struct Operands4 {
+    const f16x8* x;
+    const float* units;
+    int columns;
+};
+
+// A wave's share of a tile of 16 rows: blocks `from`, from + step, ..., of NC times 16 columns.  F spans of 32 share both scales.
+// AHEAD records are requested before the first of them is used.
+template <int TERMS, int F, int NC, int AHEAD>
+__device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group, int blocks, int from, int step, const Operands4& x, int x_scales,
+                                      f32x4 (&acc)[NC]) {
+    constexpr int FLUSHES = 4 / F;
+    const int lane = threadIdx.x & 63, grp = lane >> 4;
+    int col[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) col[c] = (lane & 15) + 16 * c < x.columns ? (lane & 15) + 16 * c : x.columns - 1;
+    u32x4 codes[AHEAD];
+    u32x2 scales[AHEAD][FLUSHES];
+    auto request = [&](int i, int block) {
+        const uint8_t* at = tile + static_cast<long long>(block < blocks ? block : blocks - 1) * record;
+        codes[i] = *reinterpret_cast<const u32x4*>(at + 16 * lane);
+#pragma unroll
+        for (int f = 0; f < FLUSHES; ++f) scales[i][f] = *reinterpret_cast<const u32x2*>(at + 1024 + 32 * f * F / group * 32 + 8 * grp);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) request(i, from + i * step);
+    for (int b0 = from; b0 < blocks; b0 += AHEAD * step) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int block = b0 + i * step;
+            if (block < blocks) {
+#pragma unroll
+                for (int f = 0; f < FLUSHES; ++f) {
+                    f32x4 part[NC];
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) part[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = f * F; j < f * F + F; ++j) {
+                        const f16x8 w = weights_f16(codes[i][j]);
+#pragma unroll
+                        for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                            for (int c = 0; c < NC; ++c)
+                                part[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w, x.x[(((block * 4 + j) * TERMS + t) * 4 + grp) * x.columns + col[c]], part[c], 0, 0, 0);
+                    }
+                    const f32x4 ws = {bf16_up(scales[i][f][0] & 0xffffu), __uint_as_float(scales[i][f][0] & 0xffff0000u),
+                                      bf16_up(scales[i][f][1] & 0xffffu), __uint_as_float(scales[i][f][1] & 0xffff0000u)};
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        const float unit = x.units[(block * x_scales + f * x_scales / FLUSHES) * x.columns + col[c]];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[c][e] = __builtin_fmaf(part[c][e] * unit, ws[e], acc[c][e]);
+                    }
+                }
+            }
+            request(i, block + AHEAD * step);
+        }
+    }
+}
+
+// X's operands from its elements: blocks block0 .. block1 of the vectors from .. upto of `columns` ones that begin at column0.  `threads`
+// threads together (16 units of 8 elements are a block, so lanes that exchange magnitudes are all there).
+template <int XT>
+__device__ __forceinline__ void stage4(const Gemm4Params& p, int column0, int columns, int from, int upto, int block0, int block1, int x_scales, f16x8* to,
+                                       float* units, int thread, int threads) {
+    typedef typename X4<XT>::T T;
+    const int per = (block1 - block0) * 16;
+    for (int at = thread; at < per * (upto - from); at += threads) {
+        const int c = from + at / per, u = block0 * 16 + at % per, block = u >> 4, e = u * 8;
+        const T* row = static_cast<const T*>(p.x) + (column0 + c) * p.x_stride;
+        T raw[8];
+        typedef T Loose __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+        if (e + 8 <= p.n) {
+            const Loose all = *reinterpret_cast<const Loose*>(row + e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw[i] = all[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw[i] = row[e + i < p.n ? e + i : p.n - 1];
+        }
+        f16x8 out[kTerms4<XT>];
+        const float unit = operand8<XT>(raw, e, p.n, out);
+        const int j = (u >> 2) & 3, grp = u & 3;
+#pragma unroll
+        for (int t = 0; t < kTerms4<XT>; ++t) to[(((block * 4 + j) * kTerms4<XT> + t) * 4 + grp) * columns + c] = out[t];
+        if constexpr (XT == kInt8 || XT == kFp8) {
+            // (a scale of a group behind the last element is one that there is)
+            const int every = 16 / x_scales;
+            if ((u & 15) % every == 0) {
+                int g = p.x_group == 0 ? 0 : e / p.x_group;
+                g = g < p.x_groups ? g : p.x_groups - 1;
+                units[(block * x_scales + (u & 15) / every) * columns + c] = p.x_scales[static_cast<long long>(column0 + c) * p.x_groups + g];
+            }
+        } else if ((u & 15) == 0) {
+            units[block * columns + c] = unit;
+        }
+    }
+}
+
+template <int TYPE>
+__device__ __forceinline__ void store_y4(const Gemm4Params& p, int column, int row, f32x4 x) {
+    typedef typename Elem<TYPE>::T T;
+    T* to = static_cast<T*>(p.y) + column * p.y_stride + row;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (row + e < p.m) to[e] = static_cast<T>(x[e]);
+}
+__device__ __forceinline__ void store_y4(const Gemm4Params& p, int column, int row, f32x4 x) {
+    if (p.y_type == BIQ_F32) store_y4<BIQ_F32>(p, column, row, x);
+    else if (p.y_type == BIQ_BF16) store_y4<BIQ_BF16>(p, column, row, x);
+    else store_y4<BIQ_F16>(p, column, row, x);
+}
+
+// A few vectors: all of them as operands in LDS.  The WAVES waves of a workgroup take WAVES / splits tiles; waves of a tile
+// share its blocks and are joined through LDS.
+constexpr int kWaves4 = 8;
+template <int XT, int F>
+__global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Params p, int x_scales) {
+    extern __shared__ float lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int column0 = blockIdx.y * 16, columns = p.batch - column0 < 16 ? p.batch - column0 : 16;
+    f16x8* operands = reinterpret_cast<f16x8*>(lds);
+    float* units = reinterpret_cast<float*>(operands + p.blocks * 16 * kTerms4<XT> * columns);
+    stage4<XT>(p, column0, columns, 0, columns, 0, p.blocks, x_scales, operands, units, threadIdx.x, 64 * kWaves4);
+    __syncthreads();
+    const int per = kWaves4 / p.splits, split = wave % p.splits, tile = (p.first + blockIdx.x) * per + wave / p.splits;
+    f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+    if (tile < p.tiles)
+        tile4<kTerms4<XT>, F, 1, 4>(p.weights + static_cast<long long>(tile) * p.blocks * p.record, p.record, p.group, p.blocks, split, p.splits,
+                                    {operands, units, columns}, x_scales, acc);
+    if (p.splits > 1) {
+        __syncthreads();                                        // (the operands are read)
+        f32x4* sums = reinterpret_cast<f32x4*>(lds);
+        sums[wave * 64 + lane] = acc[0];
+        __syncthreads();
+        if (split > 0) return;
+        for (int s = 1; s < p.splits; ++s) acc[0] += sums[(wave + s) * 64 + lane];
+    }
+    if (tile < p.tiles && (lane & 15) < columns) store_y4(p, column0 + (lane & 15), tile * 16 + 4 * (lane >> 4), acc[0]);
+}
+
+// Many vectors: X as operands in memory first, groups of p.columns vectors one after the other, each [operands, units].
+template <int XT>
+__global__ __launch_bounds__(256) void gemm4_operands_kernel(const Gemm4Params p, int x_scales, long long group_bytes) {
+    // (a workgroup for 16 blocks of one vector)
+    const int column = blockIdx.y, g = column / p.columns, column0 = g * p.columns;
+    const int columns = p.batch - column0 < p.columns ? p.batch - column0 : p.columns;
+    f16x8* to = reinterpret_cast<f16x8*>(p.operands + g * group_bytes);
+    float* units = reinterpret_cast<float*>(to + static_cast<long long>(p.blocks) * 16 * kTerms4<XT> * columns);
+    const int block0 = blockIdx.x * 16, block1 = block0 + 16 < p.blocks ? block0 + 16 : p.blocks;
+    stage4<XT>(p, column0, columns, column - column0, column - column0 + 1, block0, block1, x_scales, to, units, threadIdx.x, 256);
+}
+
+template <int TERMS, int F, int NC>
+__global__ __launch_bounds__(64 * kWaves4) void gemm4_many_kernel(const Gemm4Params p, int x_scales, long long group_bytes) {
+    __shared__ f32x4 sums[kWaves4][NC][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int column0 = blockIdx.y * p.columns, columns = p.batch - column0 < p.columns ? p.batch - column0 : p.columns;
+    const f16x8* operands = reinterpret_cast<const f16x8*>(p.operands + blockIdx.y * group_bytes);
+    const float* units = reinterpret_cast<const float*>(operands + static_cast<long long>(p.blocks) * 16 * TERMS * columns);
+    const int per = kWaves4 / p.splits, split = wave % p.splits, tile = (p.first + blockIdx.x) * per + wave / p.splits;
+    f32x4 acc[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    if (tile < p.tiles)
+        tile4<TERMS, F, NC, 2>(p.weights + static_cast<long long>(tile) * p.blocks * p.record, p.record, p.group, p.blocks, split, p.splits,
+                               {operands, units, columns}, x_scales, acc);
+    if (p.splits > 1) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) sums[wave][c][lane] = acc[c];
+        __syncthreads();
+        if (split > 0) return;
+        for (int s = 1; s < p.splits; ++s)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) acc[c] += sums[wave + s][c][lane];
+    }
+    if (tile >= p.tiles) return;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        if ((lane & 15) + 16 * c < columns) store_y4(p, column0 + (lane & 15) + 16 * c, tile * 16 + 4 * (lane >> 4), acc[c]);
+}
+
+}  // namespace biq
