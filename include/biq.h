@@ -517,6 +517,21 @@ size_t biq_attention_workspace_bytes(const biq_attention_args* args);
 biq_status biq_attention(const biq_attention_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * The same for a batch whose sequences begin with the same tokens (an instruction, a document): the first `shared` tokens of every
+ * sequence are those of sequence 0, in the pages table[0][0 .. shared / page_tokens), which are read once for all rows of the call; the entries
+ * of the other sequences for them are not looked at.  shared: a multiple of page_tokens, at least one page and at most
+ * table_stride * page_tokens (BIQ_EINVAL).  lens count the shared tokens; a sequence may also be shorter than them.  Everything
+ * else, and what it costs in bits, is as with biq_attention; results differ from its in the order of additions.
+ * workspace: biq_attention_shared_workspace_bytes(), 16-byte aligned (never 0).
+ */
+typedef struct {
+    biq_attention_args attention;
+    int shared;
+} biq_attention_shared_args;
+size_t biq_attention_shared_workspace_bytes(const biq_attention_shared_args* args);
+biq_status biq_attention_shared(const biq_attention_shared_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Verification of drafted tokens against the target's probabilities, by given random numbers: the answer's tokens are
  * distributed as the target's, whatever the draft.  Per sequence: draft i (in order) is accepted if
  *     uniform[i] * q_i(token) < p_i(token)    (32 bits);

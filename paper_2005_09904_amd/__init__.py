@@ -10,8 +10,8 @@ from .binding import (  # noqa: F401
     biq_unpack_keys, biq_unpack_keys16, biq_workspace_bytes, load_library, status_str,
 )
 from .serving import (  # noqa: F401
-    KvCache, PreparedAppend, PreparedAttention, PreparedRead, PreparedRotary, PreparedVerify, biq_attention,
-    biq_attention_workspace_bytes, biq_cache_append, biq_cache_page_bytes, biq_cache_read, biq_rotary, biq_rotary_frequencies,
+    KvCache, PreparedAppend, PreparedAttention, PreparedRead, PreparedRotary, PreparedSharedAttention, PreparedVerify, biq_attention,
+    biq_attention_shared, biq_attention_shared_workspace_bytes, biq_attention_workspace_bytes, biq_cache_append, biq_cache_page_bytes, biq_cache_read, biq_rotary, biq_rotary_frequencies,
     biq_rotary_table, biq_verify_drafts, biq_verify_workspace_bytes,
 )
 from .step import (  # noqa: F401

@@ -24,7 +24,7 @@ EXPORTS = [
     "biq_gemm_noalloc", "biq_gemm_grouped", "biq_lstm_cell",
     # (serving.py)
     "biq_rotary_frequencies", "biq_rotary_table", "biq_rotary", "biq_cache_page_bytes", "biq_cache_append", "biq_cache_read",
-    "biq_attention_workspace_bytes", "biq_attention", "biq_verify_workspace_bytes", "biq_verify_drafts",
+    "biq_attention_workspace_bytes", "biq_attention", "biq_attention_shared_workspace_bytes", "biq_attention_shared", "biq_verify_workspace_bytes", "biq_verify_drafts",
     # (step.py)
     "biq_norm", "biq_packed4_bytes", "biq_pack4", "biq_quantize4", "biq_unpack4", "biq_gemm4_workspace_bytes", "biq_gemm4",
     "biq_logits_workspace_bytes", "biq_logits",
@@ -115,6 +115,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "biq_cache_read": (I, [P, P]),
         "biq_attention_workspace_bytes": (Z, [P]),
         "biq_attention": (I, [P, P, Z, P]),
+        "biq_attention_shared_workspace_bytes": (Z, [P]),
+        "biq_attention_shared": (I, [P, P, Z, P]),
         "biq_verify_workspace_bytes": (Z, [I, I]),
         "biq_verify_drafts": (I, [P, P, Z, P]),
         "biq_norm": (I, [P, P]),

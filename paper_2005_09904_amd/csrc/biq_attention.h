@@ -31,6 +31,11 @@ struct AttendParams {
     unsigned first;          // first workgroup of this launch (0 where they share the steps)
     int negative;            // the scale is below 0: q is negated
     float scale;             // |scale| * log2(e)
+    // Of a call whose sequences share their first tokens (SharedUnit):
+    int shared;              // these tokens
+    int front;               // this launch: the shared tokens for all rows of the call, else each sequence's own ones
+    int splits, split_steps; // pieces of a unit's steps; of own tokens the steps of each but the last, which has what is left
+    int set;                 // set of partial results of the first piece
 };
 
 // What a workgroup spends on a unit beside its steps (rows, first keys, joining its waves, results), in steps: 32 sequences of 410 ..
@@ -175,6 +180,116 @@ __device__ __forceinline__ RowPlace row_place(const AttendParams& p, RowRange ra
     r.hi = p.causal ? pos : len - 1;
     r.lo = p.window > 0 ? pos - p.window + 1 : 0;
     return r;
+}
+
+// ---- sequences that share their first tokens ---------------------------------------------------------------
+//
+// The shared tokens are one sequence (the first one's pages) whose rows are all rows of the call, every sequence's own tokens
+// are sequences as in other calls, and a row's result is joined of both.  Partial results are kept in sets, each with sums
+// [row][q_head][dim] and (reference, sum of weights) for every row and head: one set for each piece of the shared tokens, then one for
+// each piece of the own ones.
+
+// Sequence of row r of the call, -1 if it has none: the last one that begins at r or before.  All lanes of a wave take part, each
+// with its own row.
+__device__ __forceinline__ int seq_of_row(const AttendParams& p, int r) {
+    if (!p.ragged.starts) return r / p.ragged.max_rows;
+    int n = 0;
+    for (int s = 0; s < p.seqs; s += 64) {
+        const int lane = threadIdx.x & 63, at = p.ragged.starts[s + lane < p.seqs ? s + lane : p.seqs - 1];
+        const int most = p.seqs - s < 64 ? p.seqs - s : 64;
+        for (int j = 0; j < most; ++j) n += __builtin_amdgcn_readlane(at, j) <= r;
+    }
+    return n - 1;
+}
+
+// A row of the call and what it sees of the shared tokens.
+__device__ __forceinline__ RowPlace shared_place(const AttendParams& p, int head, int rr, int rows_all) {
+    RowPlace place;
+    const int r = rr < rows_all ? rr / p.group : 0, seq = seq_of_row(p, r);
+    place.head = head * p.group + (rr - rr / p.group * p.group);
+    place.row = -1;
+    place.lo = 0;
+    place.hi = -1;
+    if (rr >= rows_all || seq < 0) return place;
+    const int len = p.cache.length(seq);
+    const RowRange range = p.ragged.range(seq, len);
+    const int i = r - range.first;
+    if (i < 0 || i >= range.count) return place;
+    const int pos = range.token + i;
+    place.row = r;
+    place.hi = p.causal ? pos : len - 1;
+    place.hi = place.hi < p.shared - 1 ? place.hi : p.shared - 1;
+    place.lo = p.window > 0 ? pos - p.window + 1 : 0;
+    return place;
+}
+
+// What all rows of a wave's tiles see and what some of them do, by exchange between the lanes that hold them.
+struct SeenBy { int all_lo, all_hi, any_lo, any_hi; };
+template <int NT>
+__device__ __forceinline__ SeenBy seen_by(const RowPlace (&place)[NT]) {
+    SeenBy s = {0, 0x7fffffff, 0x7fffffff, -1};
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (place[n].row < 0) continue;
+        s.all_lo = s.all_lo > place[n].lo ? s.all_lo : place[n].lo;
+        s.all_hi = s.all_hi < place[n].hi ? s.all_hi : place[n].hi;
+        s.any_lo = s.any_lo < place[n].lo ? s.any_lo : place[n].lo;
+        s.any_hi = s.any_hi > place[n].hi ? s.any_hi : place[n].hi;
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) {
+        const int a = __shfl_xor(s.all_lo, d), b = __shfl_xor(s.all_hi, d), c = __shfl_xor(s.any_lo, d), e = __shfl_xor(s.any_hi, d);
+        s.all_lo = s.all_lo > a ? s.all_lo : a;
+        s.all_hi = s.all_hi < b ? s.all_hi : b;
+        s.any_lo = s.any_lo < c ? s.any_lo : c;
+        s.any_hi = s.any_hi > e ? s.any_hi : e;
+    }
+    return {__builtin_amdgcn_readfirstlane(s.all_lo), __builtin_amdgcn_readfirstlane(s.all_hi), __builtin_amdgcn_readfirstlane(s.any_lo),
+            __builtin_amdgcn_readfirstlane(s.any_hi)};
+}
+
+// A workgroup's tile of ROWS rows and its piece of the tokens, begin .. end.  Tiles that read the same tokens are splits * heads
+// workgroups apart, mostly on one XCD.
+struct SharedUnit {
+    int seq, head, tile, split, len, rows_all, begin, end;
+    RowRange range;
+    bool none;               // no rows
+};
+template <int ROWS>
+__device__ __forceinline__ SharedUnit shared_unit(const AttendParams& p) {
+    SharedUnit u;
+    const int group = p.first + blockIdx.x, pairs = p.cache.heads * p.splits;
+    const int at = group % pairs;
+    u.head = at % p.cache.heads;
+    u.split = at / p.cache.heads;
+    u.seq = group / pairs / p.row_tiles;
+    u.tile = group / pairs - u.seq * p.row_tiles;
+    if (p.front) {
+        const long long steps = (p.shared + 63) >> 6;
+        u.len = p.shared;
+        u.range = {0, p.ragged.rows, 0};
+        u.begin = static_cast<int>(steps * u.split / p.splits) * 64;
+        u.end = static_cast<int>(steps * (u.split + 1) / p.splits) * 64;
+    } else {
+        u.len = p.cache.length(u.seq);
+        u.range = p.ragged.range(u.seq, u.len);
+        int lo = p.window > 0 ? u.range.token - p.window + 1 : 0;
+        lo = lo < 0 ? 0 : lo & ~63;
+        lo = lo < p.shared ? p.shared : lo;
+        const int steps = u.len > lo ? (u.len - lo + 63) >> 6 : 0;
+        const int from = u.split * p.split_steps;               // (the host has checked the product)
+        const int upto = u.split == p.splits - 1 ? steps : from + p.split_steps < steps ? from + p.split_steps : steps;
+        u.begin = lo + (from < upto ? from : upto) * 64;
+        u.end = lo + upto * 64;
+    }
+    u.rows_all = u.range.count * p.group;
+    u.none = u.tile * ROWS >= u.rows_all;
+    return u;
+}
+
+// Where the partial result of a row lies, in rows of a set's sums.
+__device__ __forceinline__ long long partial_at(const AttendParams& p, int split, long long row, int head) {
+    return (static_cast<long long>(p.set + split) * p.ragged.rows + row) * p.q_heads + head;
 }
 
 // Elements of the row of a lane's column: part (c, h) holds elements 64 c + 16 (lane / 16) + 8 h ..  Lanes without a row and parts
@@ -412,7 +527,7 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 w, int valid) {
 // floats): 32 sequences of 410 .. 4096 tokens (155 MB, int8, fp32) take 35 us, 4.4 TB/s, 5 rows of 16 sequences 40 us
 // (42 where 16-bit rows were converted one load after the other).
 // CH: 64 elements of a head each; FULL: the head has all of them; NT: tiles of 16 rows.
-template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES>
+template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES, bool SHARED = false>
 __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1) void attend_rows_kernel(const AttendParams p) {
     constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE>::value;
     constexpr int ROWS = 16 * NT;
@@ -423,23 +538,36 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     const int kblock = col >> 2;                                // block of this lane's key rows, 0 .. 3
 
     // steps of this workgroup: a share of all, or all of one unit
-    const Shares<ROWS> shares(p, lane, p.shares > 0);
+    const Shares<ROWS> shares(p, lane, !SHARED && p.shares > 0);
     int from = 0, upto = 1;
-    if (p.shares > 0) {
+    if (!SHARED && p.shares > 0) {
         if (static_cast<int>(blockIdx.x) >= shares.count) return;
         from = shares.begin(blockIdx.x);
         upto = shares.begin(blockIdx.x + 1);
     }
     for (bool again = false; from < upto;) {
-    int seq, unit, step = 0, stop;                              // (unit of the sequence: head * tiles + tile)
-    if (p.shares > 0) {
+    int seq, unit = 0, step = 0, stop;                          // (unit of the sequence: head * tiles + tile)
+    SharedUnit piece;
+    SeqWork work;
+    if constexpr (SHARED) {
+        piece = shared_unit<ROWS>(p);
+        if (piece.none) return;
+        from = upto;
+        seq = piece.seq;
+        work.range = piece.range;
+        work.len = piece.len;
+        work.base = piece.begin;
+        work.steps = stop = (piece.end - piece.begin) >> 6;
+        work.tiles = 1;
+    } else if (p.shares > 0) {
         stop = from;
         seq = __builtin_amdgcn_readfirstlane(shares.find(stop));
     } else {
         seq = static_cast<int>(p.first + blockIdx.x) / (p.cache.heads * p.row_tiles);
     }
-    const SeqWork work = seq_work<ROWS>(p, seq);
-    if (p.shares > 0) {
+    if constexpr (!SHARED) work = seq_work<ROWS>(p, seq);
+    if (SHARED) {
+    } else if (p.shares > 0) {
         unit = stop / work.cost();
         const int place = stop - unit * work.cost(), left = upto - from;
         step = place > kUnitCost ? place - kUnitCost : 0;
@@ -453,10 +581,10 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         stop = work.steps;
         from = upto;
     }
-    const int head = unit / work.tiles, tile = unit - head * work.tiles;
+    const int head = SHARED ? piece.head : unit / work.tiles, tile = SHARED ? piece.tile : unit - head * work.tiles;
     // a piece that ends before its unit does: the share's second slot if it begins it, else the first
-    const int slot = stop - step == work.steps ? -1 : 2 * static_cast<int>(blockIdx.x) + (step == 0 ? 1 : 0);
-    if (p.shares > 0 && step == 0 && threadIdx.x == 0) {
+    const int slot = SHARED || stop - step == work.steps ? -1 : 2 * static_cast<int>(blockIdx.x) + (step == 0 ? 1 : 0);
+    if (!SHARED && p.shares > 0 && step == 0 && threadIdx.x == 0) {
         const int id = (seq * p.cache.heads + head) * p.row_tiles + tile;
         p.owners[2 * id] = blockIdx.x;
         p.owners[2 * id + 1] = stop == work.steps ? blockIdx.x : shares.owner(from - 1 - stop + work.steps);
@@ -474,7 +602,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     RowElems<TYPE, CH, false> elems[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        place[n] = row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
+        place[n] = SHARED && p.front ? shared_place(p, head, row0 + n * 16 + col, rows_all) : row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
         elems[n].request(p, place[n], range.first, dim, grp);
     }
     u32x4 kc[4][CH];                                            // token 4 t + col % 4 of that block
@@ -512,8 +640,13 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     }
 
     // tokens that every row of the tile sees
-    const int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0;
-    const int all_hi = p.causal ? pos_first : len - 1;
+    int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0;
+    int all_hi = p.causal ? pos_first : len - 1;
+    if (SHARED && p.front) {
+        const SeenBy seen = seen_by(place);
+        all_lo = seen.all_lo;
+        all_hi = seen.all_hi;
+    }
     f32x4 o[NT][CH * 4];
     float ref[NT], l[NT];
     ScaleRange scales;
@@ -623,6 +756,13 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
             total += f.of(st[w][1]);
             acc += sums[((w * NT + rr / 16) * (CH * 4) + d / 4) * 64 + (d & 3) * 16 + ((rr + d) & 15)] * f.whole();
         }
+        if constexpr (SHARED) {
+            const int r = row0 + rr, i = r / p.group;
+            const long long to = partial_at(p, piece.split, range.first + i, head * p.group + (r - i * p.group));
+            if (stop > 0) *reinterpret_cast<f32x4*>(p.part + to * dim + 4 * d) = acc;
+            if (d == 0) *reinterpret_cast<f32x2*>(p.stats + to * 2) = (f32x2){now, total};
+            continue;
+        }
         if (slot >= 0) {
             const long long to = static_cast<long long>(slot) * ROWS + rr;
             *reinterpret_cast<f32x4*>(p.part + to * dim + 4 * d) = acc;
@@ -678,7 +818,7 @@ __device__ __forceinline__ void read_ahead(const Read& read, const Use& use) {
 // cycles) and other vector instructions (240, 3 cycles) measured apart add up to 2800 cycles, a step takes 2300.  Two prompts of
 // 4096 rows over 8192 tokens, 32 heads of 128: 806 us, 1.02 PFLOP/s.  Tiles of 16 x 16 rather than 32 x 32 as their products
 // are 20 % faster a flop here and their layout gives a lane one scale.
-template <int TYPE, int FMT, int CH, bool FULL, bool HALF, int NT, int WAVES>
+template <int TYPE, int FMT, int CH, bool FULL, bool HALF, int NT, int WAVES, bool SHARED = false>
 __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kernel(const AttendParams p) {
     constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE>::value;
     constexpr int STEPS = WAVES / 4, ROWS = 16 * NT * WAVES;
@@ -689,28 +829,46 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
     const int dim = FULL ? 64 * CH : p.cache.dim;
-    // Later rows see more tokens and come first.  Where the sequences and heads can be dealt to the XCDs evenly, each keeps to
-    // its own, whose tokens then stay in its L2.
-    const int pairs = p.seqs * p.cache.heads, group = p.first + blockIdx.x;
-    int pair, tile;
-    if (pairs % kXcds == 0) {
-        const int at = group / kXcds;
-        pair = at / p.row_tiles * kXcds + group % kXcds;
-        tile = p.row_tiles - 1 - at % p.row_tiles;
+    int seq, head, tile, len, begin, end;
+    RowRange range;
+    SharedUnit piece;
+    if constexpr (SHARED) {
+        piece = shared_unit<ROWS>(p);
+        if (piece.none) return;
+        seq = piece.seq;
+        head = piece.head;
+        tile = piece.tile;
+        len = piece.len;
+        range = piece.range;
+        begin = piece.begin;
+        end = piece.end;
     } else {
-        pair = group % pairs;
-        tile = p.row_tiles - 1 - group / pairs;
+        // Later rows see more tokens and come first.  Where the sequences and heads can be dealt to the XCDs evenly, each keeps to
+        // its own, whose tokens then stay in its L2.
+        const int pairs = p.seqs * p.cache.heads, group = p.first + blockIdx.x;
+        int pair;
+        if (pairs % kXcds == 0) {
+            const int at = group / kXcds;
+            pair = at / p.row_tiles * kXcds + group % kXcds;
+            tile = p.row_tiles - 1 - at % p.row_tiles;
+        } else {
+            pair = group % pairs;
+            tile = p.row_tiles - 1 - group / pairs;
+        }
+        seq = pair / p.cache.heads;
+        head = pair - seq * p.cache.heads;
+        len = p.cache.length(seq);
+        range = p.ragged.range(seq, len);
     }
-    const int seq = pair / p.cache.heads, head = pair - seq * p.cache.heads;
-    const int len = p.cache.length(seq);
-    const RowRange range = p.ragged.range(seq, len);
     const int rows_all = range.count * p.group, row0 = tile * ROWS;
     if (row0 >= rows_all) return;
     const int pos0 = range.token;
     const int last_row = (row0 + ROWS < rows_all ? row0 + ROWS : rows_all) - 1;
-    int begin = p.window > 0 ? pos0 + row0 / p.group - p.window + 1 : 0;
-    begin = begin < 0 ? 0 : begin & ~63;
-    const int end = p.causal ? pos0 + last_row / p.group + 1 : len;
+    if constexpr (!SHARED) {
+        begin = p.window > 0 ? pos0 + row0 / p.group - p.window + 1 : 0;
+        begin = begin < 0 ? 0 : begin & ~63;
+        end = p.causal ? pos0 + last_row / p.group + 1 : len;
+    }
 
     // this wave's rows
     RowPlace place[NT];
@@ -719,7 +877,8 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     float unit_of[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        place[n] = row_place(p, range, len, head, row0 + (wave * NT + n) * 16 + col, rows_all);
+        place[n] = SHARED && p.front ? shared_place(p, head, row0 + (wave * NT + n) * 16 + col, rows_all)
+                                     : row_place(p, range, len, head, row0 + (wave * NT + n) * 16 + col, rows_all);
         elems[n].request(p, place[n], range.first, dim, grp);
     }
 #pragma unroll
@@ -732,8 +891,15 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     const int wave_row = row0 + wave * NT * 16;
     const int wave_last = wave_row + NT * 16 < rows_all ? wave_row + NT * 16 - 1 : rows_all - 1;
     const int pos_first = pos0 + wave_row / p.group, pos_last = pos0 + wave_last / p.group;
-    const int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0, all_hi = p.causal ? pos_first : len - 1;
-    const int any_lo = p.window > 0 ? pos_first - p.window + 1 : 0, any_hi = wave_row < rows_all ? p.causal ? pos_last : len - 1 : -1;
+    int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0, all_hi = p.causal ? pos_first : len - 1;
+    int any_lo = p.window > 0 ? pos_first - p.window + 1 : 0, any_hi = wave_row < rows_all ? p.causal ? pos_last : len - 1 : -1;
+    if (SHARED && p.front) {
+        const SeenBy seen = seen_by(place);
+        all_lo = seen.all_lo;
+        all_hi = seen.all_hi;
+        any_lo = seen.any_lo;
+        any_hi = seen.any_hi;
+    }
 
     // this wave's part of a stage: of step wave / 4 the key rows of tile wave % 4 and the values of CH tiles of 16 elements
     const int my_step = wave >> 2, my_part = wave & 3;
@@ -871,6 +1037,14 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     for (int n = 0; n < NT; ++n) {
         const float total = sum_over_groups(l[n]);
         if (place[n].row < 0) continue;
+        if constexpr (SHARED) {
+            const long long at = partial_at(p, piece.split, place[n].row, place[n].head);
+#pragma unroll
+            for (int i = 0; i < VALUES; ++i)
+                if (begin < end && (FULL || i * 16 < dim)) *reinterpret_cast<f32x4*>(p.part + at * dim + i * 16 + grp * 4) = o[n][i] * scales.unit;
+            if (grp == 0) *reinterpret_cast<f32x2*>(p.stats + at * 2) = (f32x2){scales.reference(ref[n]), total};
+            continue;
+        }
         const float inv = total == 0.f ? 0.f : 1.f / total;
         const long long to = place[n].row * p.out.row_stride + place[n].head * p.out.head_stride + grp * 4;
 #pragma unroll
@@ -918,6 +1092,45 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendParams p, 
     const RowPlace place = row_place(p, work.range, work.len, head, tile * ROWS + rr, rows_all);
     store_row4<TYPE>(p.out, place.row * p.out.row_stride + place.head * p.out.head_stride + d, acc * (total == 0.f ? 0.f : 1.f / total));
     if (p.lse && threadIdx.x == 0) p.lse[place.row * p.q_heads + place.head] = log_sum(ref, total);
+}
+
+// Rows of sequences that share their first tokens, joined of `sets` partial results: a wave per row and head.
+template <int TYPE>
+__global__ __launch_bounds__(256) void attend_shared_join_kernel(const AttendParams p, int sets) {
+    const long long rows = static_cast<long long>(p.ragged.rows) * p.q_heads;
+    const long long at = static_cast<long long>(p.first + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (at >= rows) return;
+    const int lane = threadIdx.x & 63, row = static_cast<int>(at / p.q_heads), head = static_cast<int>(at - static_cast<long long>(row) * p.q_heads);
+    const int dim = p.cache.dim;
+    // the rows of no sequence are left as they are
+    const int seq = __builtin_amdgcn_readfirstlane(seq_of_row(p, row));
+    if (seq < 0) return;
+    const RowRange range = p.ragged.range(seq, p.cache.length(seq));
+    if (row < range.first || row - range.first >= range.count) return;
+    const f32x2* stats = reinterpret_cast<const f32x2*>(p.stats);
+    float ref = kNoRef;
+    for (int k = lane; k < sets; k += 64) ref = fmaxf(ref, stats[k * rows + at][0]);
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) ref = fmaxf(ref, __shfl_xor(ref, d));
+    // half a wave adds every other set
+    const int half = lane >> 5;
+    float total = 0.f;
+    for (int d0 = 0; d0 < dim; d0 += 128) {
+        const int d = d0 + (lane & 31) * 4;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+        for (int k = half; k < sets; k += 2) {
+            const f32x2 st = stats[k * rows + at];
+            const Factor f(st[0] - ref);
+            sum += f.of(st[1]);
+            if (st[1] != 0.f && d < dim) acc += *reinterpret_cast<const f32x4*>(p.part + (k * rows + at) * dim + d) * f.whole();
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], 32);
+        total = sum + __shfl_xor(sum, 32);
+        if (half == 0 && d < dim) store_row4<TYPE>(p.out, row * p.out.row_stride + head * p.out.head_stride + d, acc * (total == 0.f ? 0.f : 1.f / total));
+    }
+    if (p.lse && lane == 0) p.lse[at] = log_sum(ref, total);
 }
 
 }  // namespace biq

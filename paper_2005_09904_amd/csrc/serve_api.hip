@@ -140,6 +140,80 @@ AttendPlan attend_plan(const biq_attention_args& a) {
     return pl;
 }
 
+// ---- attention with a shared prefix: how a call is mapped --------------------------------------------------
+
+struct SharedPart {
+    bool tiles;              // the kernel for many rows
+    int nt, splits, split_steps;
+    long long row_tiles;
+};
+struct SharedPlan {
+    SharedPart front, back;
+    size_t workspace;
+};
+
+biq_status shared_check(const biq_attention_shared_args* a) {
+    if (!a) return BIQ_EINVAL;
+    if (biq_status s = attend_check(&a->attention); s != BIQ_OK) return s;
+    const biq_cache& c = a->attention.cache;
+    if (a->shared < 1 || a->shared % c.page_tokens || a->shared > static_cast<long long>(c.table_stride) * c.page_tokens) return BIQ_EINVAL;
+    return BIQ_OK;
+}
+
+SharedPlan shared_plan(const biq_attention_shared_args& args) {
+    const biq_attention_args& a = args.attention;
+    const biq_cache& c = a.cache;
+    const int group = a.q_heads / c.heads, ch = chunks_of(c.head_dim) - 1;
+    SharedPlan pl{};
+    // The shared tokens: all rows of the call over the same steps, in pieces so that there is a workgroup for every CU.
+    const long long rows = static_cast<long long>(a.ragged.rows) * group, steps = (args.shared + 63) / 64;
+    const int few = rows <= 16 || ch > 1 ? 16 : 32, many = ch <= 1 ? 128 : 64;
+    pl.front.tiles = rows > 4 * few;
+    pl.front.nt = few / 16;
+    const int tile = pl.front.tiles ? many : few;
+    pl.front.row_tiles = (rows + tile - 1) / tile;
+    const long long units = pl.front.row_tiles * c.heads;
+    long long splits = units >= kCus ? 1 : kCus / units;
+    splits = splits > (steps + 3) / 4 ? (steps + 3) / 4 : splits;
+    pl.front.splits = static_cast<int>(splits > 32 ? 32 : splits);
+    // The own tokens.
+    const long long own_rows = static_cast<long long>(a.ragged.max_rows) * group, room = static_cast<long long>(c.table_stride) * c.page_tokens;
+    long long span = (a.max_len > 0 && a.max_len < room ? a.max_len : room) - args.shared;
+    span = span < 64 ? 64 : span;
+    const long long own_steps = (span + 63) / 64;
+    const int own_few = own_rows <= 16 || ch > 1 ? 16 : 32;
+    pl.back.tiles = own_rows > 4 * own_few;
+    pl.back.nt = own_few / 16;
+    const int own_tile = pl.back.tiles ? many : own_few;
+    pl.back.row_tiles = (own_rows + own_tile - 1) / own_tile;
+    const long long own_units = pl.back.row_tiles * c.heads * c.seqs;
+    splits = own_units >= kCus ? 1 : kCus / own_units;
+    splits = splits > (own_steps + 3) / 4 ? (own_steps + 3) / 4 : splits;
+    splits = splits > 16 ? 16 : splits;
+    pl.back.splits = static_cast<int>(splits);
+    pl.back.split_steps = static_cast<int>((own_steps + splits - 1) / splits);
+    pl.workspace = static_cast<size_t>(pl.front.splits + pl.back.splits) * a.ragged.rows * a.q_heads * (c.head_dim + 2) * 4;
+    return pl;
+}
+
+AttendParams attend_params(const biq_attention_args* a) {
+    AttendParams p{};
+    p.cache = cache_of(a->cache);
+    p.ragged = {a->ragged.starts, a->ragged.rows, a->ragged.max_rows};
+    p.q = rows_of(a->q, a->type);
+    p.out = rows_of(a->out, a->type);
+    p.lse = a->lse;
+    p.q_heads = a->q_heads;
+    p.group = a->q_heads / a->cache.heads;
+    p.causal = a->causal != 0;
+    // (a window that no token is outside of is none)
+    p.window = a->window < static_cast<long long>(a->cache.table_stride) * a->cache.page_tokens ? a->window : 0;
+    p.seqs = a->cache.seqs;
+    p.negative = a->scale < 0.f;
+    p.scale = fabsf(a->scale) * 1.4426950408889634f;
+    return p;
+}
+
 }  // namespace
 }  // namespace biq
 
@@ -249,21 +323,8 @@ biq_status biq_attention(const biq_attention_args* a, void* workspace, size_t wo
     const AttendPlan pl = attend_plan(*a);
     if (pl.workspace > workspace_bytes) return BIQ_EWORKSPACE;
     if (pl.workspace && (!workspace || !aligned(workspace, 16))) return BIQ_EINVAL;
-    AttendParams p{};
-    p.cache = cache_of(a->cache);
-    p.ragged = {a->ragged.starts, a->ragged.rows, a->ragged.max_rows};
-    p.q = rows_of(a->q, a->type);
-    p.out = rows_of(a->out, a->type);
-    p.lse = a->lse;
-    p.q_heads = a->q_heads;
-    p.group = a->q_heads / a->cache.heads;
-    p.causal = a->causal != 0;
-    // (a window that no token is outside of is none)
-    p.window = a->window < static_cast<long long>(a->cache.table_stride) * a->cache.page_tokens ? a->window : 0;
-    p.seqs = a->cache.seqs;
+    AttendParams p = attend_params(a);
     p.shares = pl.shares;
-    p.negative = a->scale < 0.f;
-    p.scale = fabsf(a->scale) * 1.4426950408889634f;
     p.part = static_cast<float*>(workspace);
     p.stats = p.part + static_cast<size_t>(pl.shares) * 2 * 16 * pl.nt * a->cache.head_dim;
     p.owners = reinterpret_cast<int*>(p.stats + static_cast<size_t>(pl.shares) * 2 * 16 * pl.nt * 2);
@@ -275,6 +336,41 @@ biq_status biq_attention(const biq_attention_args* a, void* workspace, size_t wo
         case BIQ_BF16: return status(launch_attend_bf16(a->cache.format, pl.tiles, pl.nt, pl.waves, p, s));
         default: return status(launch_attend_f16(a->cache.format, pl.tiles, pl.nt, pl.waves, p, s));
     }
+}
+
+size_t biq_attention_shared_workspace_bytes(const biq_attention_shared_args* a) {
+    return shared_check(a) == BIQ_OK ? shared_plan(*a).workspace : 0;
+}
+
+biq_status biq_attention_shared(const biq_attention_shared_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    if (biq_status s = shared_check(args); s != BIQ_OK) return s;
+    const biq_attention_args* a = &args->attention;
+    if (!rows_ok(a->q, a->type) || !rows_ok(a->out, a->type) || !aligned(a->lse, 4)) return BIQ_EINVAL;
+    const SharedPlan pl = shared_plan(*args);
+    if (pl.workspace > workspace_bytes) return BIQ_EWORKSPACE;
+    if (!workspace || !aligned(workspace, 16)) return BIQ_EINVAL;
+    if (static_cast<long long>(a->cache.seqs) * a->cache.heads * pl.back.row_tiles * pl.back.splits > kMaxInt) return BIQ_EUNSUPPORTED;
+    AttendParams p = attend_params(a);
+    const int sets = pl.front.splits + pl.back.splits;
+    p.part = static_cast<float*>(workspace);
+    p.stats = p.part + static_cast<size_t>(sets) * a->ragged.rows * a->q_heads * a->cache.head_dim;
+    p.shared = args->shared;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    for (const bool front : {true, false}) {
+        const SharedPart& part = front ? pl.front : pl.back;
+        p.front = front;
+        p.row_tiles = static_cast<int>(part.row_tiles);
+        p.splits = part.splits;
+        p.split_steps = part.split_steps;
+        p.set = front ? 0 : pl.front.splits;
+        const hipError_t e = a->type == BIQ_F32    ? launch_attend_shared_f32(a->cache.format, part.tiles, part.nt, p, s)
+                             : a->type == BIQ_BF16 ? launch_attend_shared_bf16(a->cache.format, part.tiles, part.nt, p, s)
+                                                   : launch_attend_shared_f16(a->cache.format, part.tiles, part.nt, p, s);
+        if (e != hipSuccess) return BIQ_EHIP;
+    }
+    return status(a->type == BIQ_F32    ? launch_shared_join_f32(sets, p, s)
+                  : a->type == BIQ_BF16 ? launch_shared_join_bf16(sets, p, s)
+                                        : launch_shared_join_f16(sets, p, s));
 }
 
 size_t biq_verify_workspace_bytes(int seqs, int vocab) {

@@ -58,6 +58,10 @@ class _AttentionArgs(ctypes.Structure):
                 ("max_len", I), ("causal", I), ("window", I), ("scale", ctypes.c_float)]
 
 
+class _SharedArgs(ctypes.Structure):
+    _fields_ = [("attention", _AttentionArgs), ("shared", I)]
+
+
 class _VerifyArgs(ctypes.Structure):
     _fields_ = [("p", P), ("q", P), ("p_seq_stride", L), ("p_stride", L), ("q_seq_stride", L), ("q_stride", L),
                 ("draft_tokens", P), ("draft_lens", P), ("uniform", P), ("tokens", P), ("accepted", P), ("type", I), ("seqs", I),
@@ -261,6 +265,28 @@ class PreparedAttention(_Prepared):
 def biq_attention(cache, q, out, lse=None, scale=None, starts=None, max_rows=None, max_len=0, causal=True, window=0,
                   workspace=None, stream=None) -> None:
     PreparedAttention(cache, q, out, lse, scale, starts, max_rows, max_len, causal, window, workspace, stream)()
+
+
+def biq_attention_shared_workspace_bytes(cache, q, shared, scale=None, starts=None, max_rows=None, max_len=0, causal=True, window=0) -> int:
+    """Bytes for PreparedSharedAttention / biq_attention_shared with the same arguments."""
+    a = _SharedArgs(_attention_args(cache, q, scale, starts, max_rows, max_len, causal, window), shared)
+    return binding.load_library().biq_attention_shared_workspace_bytes(ctypes.addressof(a))
+
+
+class PreparedSharedAttention(_Prepared):
+    """biq_attention_shared: as PreparedAttention, where the first `shared` tokens of all sequences are those of the cache's sequence 0."""
+
+    def __init__(self, cache, q, out, shared, lse=None, scale=None, starts=None, max_rows=None, max_len=0, causal=True, window=0,
+                 workspace=None, stream=None):
+        a = _SharedArgs(_attention_args(cache, q, scale, starts, max_rows, max_len, causal, window), shared)
+        a.attention.out = _rows(out, "out", q, q.shape[1], q.shape[2], q.shape[0])
+        a.attention.lse = None if lse is None else _whole(lse, "lse", "float32", q.shape[:2], q.device)
+        super().__init__("biq_attention_shared", a, (cache, q, out, lse, starts), workspace, True, q.device, stream)
+
+
+def biq_attention_shared(cache, q, out, shared, lse=None, scale=None, starts=None, max_rows=None, max_len=0, causal=True, window=0,
+                         workspace=None, stream=None) -> None:
+    PreparedSharedAttention(cache, q, out, shared, lse, scale, starts, max_rows, max_len, causal, window, workspace, stream)()
 
 
 # ---- drafted tokens ----------------------------------------------------------------------------------------

@@ -47,6 +47,12 @@ def test_packed_bytes(biq):
         assert biq.biq_packed4_bytes(*bad) == 0
 
 
+def at(descriptor):
+    """Its address, which is good as long as the descriptor is kept."""
+    at.kept = descriptor
+    return ctypes.addressof(descriptor)
+
+
 def norm(**change):
     from paper_2005_09904_amd import step
 
@@ -63,9 +69,9 @@ def test_norm_refuses(biq):
                 dict(n=0), dict(group=16), dict(group=-32), dict(group=256), dict(format=2), dict(eps=-1.0), dict(eps=nan), dict(eps=inf), dict(weight_add=nan),
                 dict(x=A + 2), dict(y=A + 2), dict(y=A + 1, y_type=1), dict(residual=A + 1), dict(sum=A + 3), dict(weight=A + 2), dict(scales=A + 1),
                 dict(x_stride=-1), dict(residual_stride=-1), dict(sum_stride=63), dict(y_stride=0), dict(code_stride=63), dict(x_stride=(1 << 40) + 1)):
-        assert lib.biq_norm(ctypes.addressof(norm(**bad)), None) == EINVAL, bad
+        assert lib.biq_norm(at(norm(**bad)), None) == EINVAL, bad
     big = (1 << 24) + 1
-    assert lib.biq_norm(ctypes.addressof(norm(n=big, sum_stride=big, y_stride=big, code_stride=big)), None) == EUNSUPPORTED
+    assert lib.biq_norm(at(norm(n=big, sum_stride=big, y_stride=big, code_stride=big)), None) == EUNSUPPORTED
 
 
 def gemm4(**change):
@@ -79,7 +85,7 @@ def test_products_refuse(biq):
     lib = biq.load_library()
 
     def status(a, ws=A, size=1 << 40):
-        return lib.biq_gemm4(ctypes.addressof(a), ws, size, None)
+        return lib.biq_gemm4(at(a), ws, size, None)
 
     assert lib.biq_gemm4(None, A, 1 << 40, None) == EINVAL and lib.biq_gemm4_workspace_bytes(None) == 0
     for bad in (dict(weights=None), dict(x=None), dict(y=None), dict(x_scales=None), dict(m=0), dict(n=0), dict(batch=0), dict(group=0), dict(group=48),
@@ -88,12 +94,12 @@ def test_products_refuse(biq):
         assert status(gemm4(**bad)) == EINVAL, bad
     for bad in (dict(batch=65536), dict(n=(1 << 24) + 1), dict(m=(1 << 28) + 1, y_stride=1 << 29)):
         assert status(gemm4(**bad)) == EUNSUPPORTED, bad
-        assert lib.biq_gemm4_workspace_bytes(ctypes.addressof(gemm4(**bad))) == 0
-    need = lib.biq_gemm4_workspace_bytes(ctypes.addressof(gemm4()))
+        assert lib.biq_gemm4_workspace_bytes(at(gemm4(**bad))) == 0
+    need = lib.biq_gemm4_workspace_bytes(at(gemm4()))
     assert need > 40 * 300 * 2
     assert status(gemm4(), A, need - 1) == EWORKSPACE
     assert status(gemm4(), None, need) == EINVAL and status(gemm4(), A + 8, need) == EINVAL
-    assert lib.biq_gemm4_workspace_bytes(ctypes.addressof(gemm4(batch=1))) == 0
+    assert lib.biq_gemm4_workspace_bytes(at(gemm4(batch=1))) == 0
 
 
 def test_layout_refuses(biq):
@@ -126,7 +132,7 @@ def test_logits_refuse(biq):
     lib = biq.load_library()
 
     def status(a, ws=A, size=1 << 40):
-        return lib.biq_logits(ctypes.addressof(a), ws, size, None)
+        return lib.biq_logits(at(a), ws, size, None)
 
     assert lib.biq_logits(None, A, 1 << 40, None) == EINVAL
     fields = ("history", "lens", "prompt_lens", "drafts", "repetition", "presence", "frequency", "temperature", "bias_tokens", "bias_values", "mask")
@@ -190,3 +196,35 @@ def test_logits_tensors(biq):
             dict(history=t(3, 9, dtype=i32)), dict(lens=t(3, dtype=i32)), dict(drafts=t(2, 3, dtype=i32)), dict(drafts=t(2, 2)), dict(repetition=t(2, 1)),
             dict(temperature=t(2, dtype=torch.float64)), dict(bias_values=None), dict(bias_values=t(2, 4)), dict(mask=t(2, 3, 3, dtype=i32)), dict(mask=t(2, 3, 4)),
             dict(mask=t(2, 3, 8, dtype=i32)[..., ::2]))
+
+
+# ---- attention with a shared prefix --------------------------------------------------------------------------------
+
+def test_shared_attention_refuses(biq):
+    from paper_2005_09904_amd import serving
+    from test_serving_host import BAD_CACHES, BAD_RAGGED, BAD_ROWS, attention, cache, ragged, rows
+
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "biq.h")).read(), flags=re.S)
+    assert re.search(r"typedef struct \{\s*biq_attention_args attention;\s*int shared;\s*\} biq_attention_shared_args;", text)
+    assert list(serving._SharedArgs._fields_) == [("attention", serving._AttentionArgs), ("shared", ctypes.c_int)]
+    lib = biq.load_library()
+
+    def status(a, shared=64, ws=A, size=1 << 40):
+        return lib.biq_attention_shared(at(serving._SharedArgs(a, shared)), ws, size, None)
+
+    assert lib.biq_attention_shared(None, A, 1 << 40, None) == EINVAL and lib.biq_attention_shared_workspace_bytes(None) == 0
+    for shared in (0, -32, 16, 33, 160, 1 << 30):               # pages of 32, four of a sequence
+        assert status(attention(), shared) == EINVAL
+        assert lib.biq_attention_shared_workspace_bytes(at(serving._SharedArgs(attention(), shared))) == 0
+    for bad, code in BAD_CACHES:
+        assert status(attention(cache=cache(**bad)), 32) == code, bad
+    for bad in BAD_RAGGED:
+        assert status(attention(ragged=ragged(**bad))) == EINVAL, bad
+    for bad in BAD_ROWS:
+        assert status(attention(q=rows(**bad))) == EINVAL and status(attention(out=rows(**bad))) == EINVAL, bad
+    for bad in (dict(type=3), dict(q_heads=3), dict(q_heads=0), dict(max_len=-1), dict(window=-1), dict(lse=A + 2)):
+        assert status(attention(**bad)) == EINVAL, bad
+    need = lib.biq_attention_shared_workspace_bytes(at(serving._SharedArgs(attention(), 64)))
+    assert need >= 2 * 6 * 4 * 66 * 4                           # two sets of partial results at least
+    assert status(attention(), 64, A, need - 1) == EWORKSPACE
+    assert status(attention(), 64, None, need) == EINVAL and status(attention(), 64, A + 8, need) == EINVAL
