@@ -29,22 +29,27 @@ hipError_t norm_t(NormParams p, hipStream_t s) {
     });
 }
 
-template <int TYPE, int WHAT>
+template <int TYPE, int THREADS, int U, int WHAT>
 hipError_t logits_pass(LogitsParams p, hipStream_t s) {
-    const int lds = 4 * kLogitsSpan * ((p.history || p.drafts ? 1 : 0) + (p.biases > 0 ? 1 : 0));
-    return launch_parts(static_cast<long long>(p.seqs) * p.spans, 256, [&](unsigned first, unsigned grid) {
+    const int lds = 16 * (THREADS / 64) + 4 * THREADS * U * 8 * ((p.history || p.drafts ? 1 : 0) + (p.biases > 0 ? 1 : 0));
+    return launch_parts(static_cast<long long>(p.seqs) * p.spans, THREADS, [&](unsigned first, unsigned grid) {
         p.first = first;
-        hipLaunchKernelGGL((logits_kernel<TYPE, 256, kLogitsSpan / 2048, WHAT>), dim3(grid), dim3(256), lds, s, p);
-        return hipGetLastError();
+        return launch_large_lds<logits_kernel<TYPE, THREADS, U, WHAT>, false>(p, static_cast<int>(grid), THREADS, lds, s);
     });
 }
 
 template <int TYPE>
-hipError_t logits_t(bool probabilities, const LogitsParams& p, hipStream_t s) {
-    if (!probabilities) return logits_pass<TYPE, 0>(p, s);
-    if (p.spans == 1) return logits_pass<TYPE, 3>(p, s);
-    if (hipError_t e = logits_pass<TYPE, 1>(p, s); e != hipSuccess) return e;
-    return logits_pass<TYPE, 2>(p, s);
+hipError_t logits_t(bool probabilities, bool whole, LogitsParams p, hipStream_t s) {
+    if (!probabilities) return logits_pass<TYPE, 256, kLogitsSpan / 2048, 0>(p, s);
+    if (whole) {
+        p.spans = 1;
+        if (p.vocab <= 2048) return logits_pass<TYPE, 256, 1, 3>(p, s);
+        if (p.vocab <= 8192) return logits_pass<TYPE, 1024, 1, 3>(p, s);
+        if (p.vocab <= 16384) return logits_pass<TYPE, 1024, 2, 3>(p, s);
+        return logits_pass<TYPE, 1024, 4, 3>(p, s);
+    }
+    if (hipError_t e = logits_pass<TYPE, 256, kLogitsSpan / 2048, 1>(p, s); e != hipSuccess) return e;
+    return logits_pass<TYPE, 256, kLogitsSpan / 2048, 2>(p, s);
 }
 
 }  // namespace
@@ -58,11 +63,11 @@ hipError_t launch_norm(int type, const NormParams& p, hipStream_t s) {
     return hipErrorInvalidValue;
 }
 
-hipError_t launch_logits(int type, bool probabilities, const LogitsParams& p, hipStream_t s) {
+hipError_t launch_logits(int type, bool probabilities, bool whole, const LogitsParams& p, hipStream_t s) {
     switch (type) {
-        case BIQ_F32: return logits_t<BIQ_F32>(probabilities, p, s);
-        case BIQ_BF16: return logits_t<BIQ_BF16>(probabilities, p, s);
-        case BIQ_F16: return logits_t<BIQ_F16>(probabilities, p, s);
+        case BIQ_F32: return logits_t<BIQ_F32>(probabilities, whole, p, s);
+        case BIQ_BF16: return logits_t<BIQ_BF16>(probabilities, whole, p, s);
+        case BIQ_F16: return logits_t<BIQ_F16>(probabilities, whole, p, s);
     }
     return hipErrorInvalidValue;
 }

@@ -68,6 +68,9 @@ Gemm4Plan gemm4_plan(const biq_gemm4_args& a) {
     return pl;
 }
 
+// Rows that a workgroup holds: 1024 threads with 32 tokens each, whose counts and biases take 4 bytes of LDS each.
+bool logits_whole(int vocab, bool biases) { return vocab <= (biases ? 16384 : 32768); }
+
 }  // namespace
 }  // namespace biq
 
@@ -193,7 +196,7 @@ biq_status biq_gemm4(const biq_gemm4_args* a, void* workspace, size_t workspace_
 size_t biq_logits_workspace_bytes(int seqs, int rows, int vocab) {
     if (seqs < 1 || rows < 1 || vocab < 1 || vocab > (1 << 22) || static_cast<long long>(seqs) * rows > kMaxInt) return 0;
     const size_t spans = (vocab + kLogitsSpan - 1) / kLogitsSpan;
-    return spans == 1 ? 0 : static_cast<size_t>(seqs) * rows * spans * 8;
+    return logits_whole(vocab, true) ? 0 : static_cast<size_t>(seqs) * rows * spans * kLogitsWaves * 8;
 }
 
 biq_status biq_logits(const biq_logits_args* a, void* workspace, size_t workspace_bytes, void* stream) {
@@ -211,6 +214,7 @@ biq_status biq_logits(const biq_logits_args* a, void* workspace, size_t workspac
     if (!write_ok(a->out_stride, a->rows, a->vocab) || !write_ok(a->out_seq_stride, a->seqs, a->vocab)) return BIQ_EINVAL;
     if (a->x == a->out && (a->type != a->out_type || a->x_seq_stride != a->out_seq_stride || a->x_stride != a->out_stride)) return BIQ_EINVAL;
     if (a->vocab > (1 << 22) || a->biases > 4096 || static_cast<long long>(a->seqs) * a->rows > kMaxInt) return BIQ_EUNSUPPORTED;
+    const bool whole = logits_whole(a->vocab, a->biases > 0);
     const size_t need = a->probabilities ? biq_logits_workspace_bytes(a->seqs, a->rows, a->vocab) : 0;
     if (need > workspace_bytes) return BIQ_EWORKSPACE;
     if (need && (!workspace || !aligned(workspace, 16))) return BIQ_EINVAL;
@@ -243,7 +247,7 @@ biq_status biq_logits(const biq_logits_args* a, void* workspace, size_t workspac
     p.biases = a->biases;
     p.spans = (a->vocab + kLogitsSpan - 1) / kLogitsSpan;
     if (static_cast<long long>(p.seqs) * p.spans > 0xffffffffll) return BIQ_EUNSUPPORTED;
-    return status(launch_logits(a->type, a->probabilities != 0, p, static_cast<hipStream_t>(stream)));
+    return status(launch_logits(a->type, a->probabilities != 0, whole, p, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

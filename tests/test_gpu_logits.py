@@ -136,6 +136,20 @@ def test_the_first_of_several_largest(biq):
         assert p.argmax(dim=2)[:, 0].tolist() == [0, vocab // 2, vocab - 1] and (p.sum(dim=2) == 1).all()
 
 
+def test_temperatures_at_the_ends(biq):
+    """Very hot ones leave all tokens alike, but for masked ones; very cold ones take the likeliest, as do negative ones and NaN."""
+    x = torch.randn((6, 1, 20000), generator=torch.Generator().manual_seed(1))
+    mask = np.full((6, 1, 625), 0x55555555, np.int32)
+    p = su.back(call(biq, x, dict(mask=mask, temperature=np.array([np.inf, 1e38, 1e-35, 1e-28, -1, np.nan], np.float32)), "fp32", True))
+    seen = np.arange(20000) % 2 == 0
+    for s in range(6):
+        assert (p[s, 0, ~seen] == 0).all()
+        if s < 2:
+            assert np.allclose(p[s, 0, seen], 1e-4, rtol=1e-5)
+        else:
+            assert p[s, 0].max() == 1 and p[s, 0].sum() == 1 and p[s, 0].argmax() == np.where(seen, x[s, 0].numpy(), -9).argmax()
+
+
 def test_lengths_and_biases_beyond_their_bounds(biq):
     x, h = inputs(3, 2, 500, "fp32", 5)
     h["lens"] = np.array([-3, 1 << 30, 10], np.int32)

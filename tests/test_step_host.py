@@ -122,9 +122,9 @@ def test_layout_refuses(biq):
 def logits(**change):
     from paper_2005_09904_amd import step
 
-    a = dict(x=A, out=2 * A, x_seq_stride=30000, x_stride=10000, out_seq_stride=30000, out_stride=10000, mask_seq_stride=939, mask_stride=313, history=A, lens=A,
+    a = dict(x=A, out=2 * A, x_seq_stride=60000, x_stride=20000, out_seq_stride=60000, out_stride=20000, mask_seq_stride=1877, mask_stride=625, history=A, lens=A,
              prompt_lens=A, drafts=A, repetition=A, presence=A, frequency=A, temperature=A, bias_tokens=A, bias_values=A, mask=A, type=0, out_type=0, seqs=2,
-             rows=3, vocab=10000, width=50, biases=4, probabilities=1)
+             rows=3, vocab=20000, width=50, biases=4, probabilities=1)
     return step._LogitsArgs(**{**a, **change})
 
 
@@ -137,13 +137,13 @@ def test_logits_refuse(biq):
     assert lib.biq_logits(None, A, 1 << 40, None) == EINVAL
     fields = ("history", "lens", "prompt_lens", "drafts", "repetition", "presence", "frequency", "temperature", "bias_tokens", "bias_values", "mask")
     for bad in (dict(x=None), dict(out=None), dict(type=3), dict(out_type=-1), dict(seqs=0), dict(rows=0), dict(vocab=0), dict(x=A + 2), dict(out=A + 1),
-                dict(lens=None), dict(history=None), dict(width=0), dict(biases=-1), dict(bias_tokens=None), dict(bias_values=None), dict(out_stride=9999),
+                dict(lens=None), dict(history=None), dict(width=0), dict(biases=-1), dict(bias_tokens=None), dict(bias_values=None), dict(out_stride=19999),
                 dict(out_seq_stride=0), dict(x_stride=-1), dict(mask_stride=-1), dict(mask_seq_stride=-1), dict(out=A, out_type=1),
-                dict(out=A, out_stride=10001), *({f: A + 2} for f in fields)):
+                dict(out=A, out_stride=20001), *({f: A + 2} for f in fields)):
         assert status(logits(**bad)) == EINVAL, bad
     for bad in (dict(vocab=(1 << 22) + 1, out_stride=1 << 23, out_seq_stride=1 << 25), dict(biases=4097), dict(seqs=1 << 16, rows=1 << 15)):
         assert status(logits(**bad)) == EUNSUPPORTED, bad
-    need = biq.biq_logits_workspace_bytes(2, 3, 10000)
+    need = biq.biq_logits_workspace_bytes(2, 3, 20000)
     assert need >= 2 * 3 * 8 and biq.biq_logits_workspace_bytes(2, 3, 4000) == 0
     for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, (1 << 22) + 1)):
         assert biq.biq_logits_workspace_bytes(*bad) == 0
