@@ -25,7 +25,7 @@ struct LogitsParams {
     const int* bias_tokens;  // [seqs][biases]
     const float* bias_values;
     const uint32_t* mask;
-    f32x2* stats;            // [seqs][rows][spans * waves] largest logit, sum of exponentials (or the place of the largest as an integer)
+    f32x2* stats;            // [seqs][rows][spans] largest logit, sum of exponentials (or the place of the largest as an integer)
     int out_type, seqs, rows, vocab, width, biases, spans;
     unsigned first;
 };
@@ -55,10 +55,22 @@ __device__ __forceinline__ Penalties penalties_of(const LogitsParams& p, int seq
     return k;
 }
 
+// Entry i0 + lane of a sequence's list of biases.
+struct Bias { int token; float value; };
+__device__ __forceinline__ Bias bias_of(const LogitsParams& p, int seq, int i0) {
+    const int i = i0 + static_cast<int>(threadIdx.x & 63);
+    const long long at = static_cast<long long>(seq) * p.biases + (i < p.biases ? i : p.biases - 1);
+    return {p.bias_tokens[at], p.bias_values[at]};
+}
+
 // Counts and biases of a span of SPAN tokens in LDS.
 template <int THREADS, int SPAN>
 __device__ __forceinline__ void count_tokens(const LogitsParams& p, int seq, int t0, uint32_t* counts, float* biases) {
     constexpr int AHEAD = 4;                                    // times 4 tokens that a thread requests together
+    constexpr int WAVES = THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Bias mine = {-1, 0.f};
+    if (biases) mine = bias_of(p, seq, 0);
     typedef int Loose4 __attribute__((ext_vector_type(4), aligned(4)));
     int len = p.history ? p.lens[seq] : 0, prompt = p.prompt_lens ? p.prompt_lens[seq] : 0;
     len = len < 0 ? 0 : len > p.width ? p.width : len;
@@ -97,75 +109,90 @@ __device__ __forceinline__ void count_tokens(const LogitsParams& p, int seq, int
             }
     }
     if (biases) {
-        // a token's biases are added in the list's order by the thread of the first of them
-        const int* listed = p.bias_tokens + static_cast<long long>(seq) * p.biases;
-        const float* values = p.bias_values + static_cast<long long>(seq) * p.biases;
-        for (int i = threadIdx.x; i < p.biases; i += THREADS) {
-            const int token = listed[i];
-            const uint32_t at = static_cast<uint32_t>(token) - static_cast<uint32_t>(t0);
-            if (at >= static_cast<uint32_t>(SPAN)) continue;
-            bool first = true;
-            for (int j = 0; j < i; ++j) first = first && listed[j] != token;
-            if (!first) continue;
-            float sum = 0.f;
-            for (int j = i; j < p.biases; ++j)
-                if (listed[j] == token) sum += values[j];
-            biases[at] = sum;
+        // 64 of the list at a time, a lane each; the waves share those that lie in the span.  A token's biases are added in the list's order
+        // where the first of them is met, which looks at the rest of the list.
+        for (int i0 = 0; i0 < p.biases; i0 += 64) {
+            if (i0 > 0) mine = bias_of(p, seq, i0);
+            unsigned long long here = __ballot(i0 + lane < p.biases && mine.token >= t0 && mine.token < t0 + SPAN);
+            for (int n = 0; here; ++n) {
+                const int l = __ffsll(here) - 1, token = __builtin_amdgcn_readlane(mine.token, l);
+                here &= here - 1;
+                if (n % WAVES != wave) continue;
+                bool first = true;
+                float sum = 0.f;
+                for (int j0 = 0; j0 < p.biases && first; j0 += 64) {
+                    const Bias other = j0 == i0 ? mine : bias_of(p, seq, j0);
+                    unsigned long long same = __ballot(j0 + lane < p.biases && other.token == token);
+                    first = !same || j0 + __ffsll(same) - 1 >= i0 + l;
+                    while (first && same) {
+                        sum += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(other.value), __ffsll(same) - 1));
+                        same &= same - 1;
+                    }
+                }
+                if (first && lane == 0) biases[token - t0] = sum;
+            }
         }
     }
     __syncthreads();
 }
 
-__device__ __forceinline__ float largest_of_wave(float x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
+// Over a wave: within rows of 16 lanes, then over the rows' ends.
+template <int CONTROL, int ROWS, typename Join>
+__device__ __forceinline__ float moved(float x, float none, const Join& join) {
+    return join(x, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CONTROL, ROWS, 0xf, false)));
 }
-__device__ __forceinline__ float sum_of_wave(float x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    return x;
+template <typename Join>
+__device__ __forceinline__ float over_wave(float x, float none, const Join& join) {
+    x = moved<0x111, 0xf>(x, none, join);                       // row_shr:1, 2, 4, 8
+    x = moved<0x112, 0xf>(x, none, join);
+    x = moved<0x114, 0xf>(x, none, join);
+    x = moved<0x118, 0xf>(x, none, join);
+    x = moved<0x142, 0xa>(x, none, join);                       // row_bcast:15 to rows 1 and 3
+    x = moved<0x143, 0xc>(x, none, join);                       // row_bcast:31 to rows 2 and 3
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
+__device__ __forceinline__ float largest_of_wave(float x) { return over_wave(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float sum_of_wave(float x) { return over_wave(x, 0.f, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ Best best_of_wave(Best b) {
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) b = better(b, Best{__shfl_xor(b.z, d), __shfl_xor(b.at, d)});
     return b;
 }
 
-// What a row comes to: probabilities are exp2((z - top) scale) each, or for greedy sequences 1 at place `at`.  Numbers
-// that are no numbers come through `each`: a NaN among the exponentials is one in their sum.
+// What a row comes to: probabilities are exp2((z - top) scale) each, or for greedy sequences 1 at place `at`.  A NaN among the
+// exponentials is one in their sum, and so comes to all of them.
 struct RowSum {
-    float top, each;
+    float top, sum;
     int at;
 };
-// Of n pairs (largest logit, sum of exponentials or place), all threads of a wave for all of them.
-template <typename Pairs>
-__device__ __forceinline__ RowSum row_sum(const Pairs& pairs, int n, bool greedy, float scale) {
+// Of n pairs (largest logit, and the sum of exponentials or its place), all threads of a wave for all of them; `mine` is pair `lane`.
+__device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n, bool greedy, float scale) {
     const int lane = threadIdx.x & 63;
     RowSum r = {-INFINITY, 0.f, -1};
     if (greedy) {
         Best best = {-INFINITY, 0x7fffffff};
-        for (int i = lane; i < n; i += 64) best = better(best, Best{pairs[i][0], __float_as_int(pairs[i][1])});
+        if (lane < n) best = Best{mine[0], __float_as_int(mine[1])};
+        for (int i = lane + 64; i < n; i += 64) best = better(best, Best{pairs[i][0], __float_as_int(pairs[i][1])});
         best = best_of_wave(best);
         r.top = best.z;
         r.at = best.z == -INFINITY ? -1 : best.at;
         return r;
     }
-    for (int i = lane; i < n; i += 64) r.top = fmaxf(r.top, pairs[i][0]);
+    if (lane < n) r.top = mine[0];
+    for (int i = lane + 64; i < n; i += 64) r.top = fmaxf(r.top, pairs[i][0]);
     r.top = largest_of_wave(r.top);
-    float sum = 0.f;
-    for (int i = lane; i < n; i += 64) sum += pairs[i][0] == -INFINITY ? pairs[i][1] : pairs[i][1] * __builtin_amdgcn_exp2f((pairs[i][0] - r.top) * scale);
-    sum = sum_of_wave(sum);
-    r.each = sum == 0.f ? 0.f : 1.f / sum;
+    auto part = [&](f32x2 x) { return x[0] == -INFINITY ? x[1] : x[1] * __builtin_amdgcn_exp2f((x[0] - r.top) * scale); };
+    if (lane < n) r.sum = part(mine);
+    for (int i = lane + 64; i < n; i += 64) r.sum += part(pairs[i]);
+    r.sum = sum_of_wave(r.sum);
     return r;
 }
 
-// WHAT: 0 writes logits, 1 leaves a pair of every wave, 2 writes probabilities by these, 3 writes probabilities of rows that a workgroup
-// has whole.  A thread has U times 8 adjacent tokens, and their counts and biases are read by no other: a draft is counted by the thread
-// that has it.
+// WHAT: 0 writes logits, 1 leaves a pair of every span, 2 writes probabilities by these, 3 writes probabilities of rows that a workgroup
+// has whole.  A thread has U times 8 adjacent tokens for all rows, and holds what is taken from their logits (looks it up
+// in LDS for every row where there are 32).
 template <int TYPE, int THREADS, int U, int WHAT>
 __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
-#pragma clang fp contract(off)
     typedef typename Elem<TYPE>::T T;
     constexpr int SPAN = THREADS * U * 8, WAVES = THREADS / 64;
     constexpr bool EARLY = U <= 2;                              // the next row is requested before this one is used (32 tokens: no registers left)
@@ -175,13 +202,15 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
     const long long group = p.first + blockIdx.x;
     const int seq = static_cast<int>(group / p.spans), span = static_cast<int>(group - static_cast<long long>(seq) * p.spans), t0 = span * SPAN;
     int me = threadIdx.x;
-    const int wave = __builtin_amdgcn_readfirstlane(me >> 6);
+    const int lane = me & 63, wave = __builtin_amdgcn_readfirstlane(me >> 6);
     const bool counting = p.history || p.drafts;
     uint32_t* counts = counting ? reinterpret_cast<uint32_t*>(space) : nullptr;
     float* biases = p.biases > 0 ? space + (counting ? SPAN : 0) : nullptr;
     T raw[U][8];
     uint32_t allowed[U];
+    f32x2 pair = {0.f, 0.f};
     auto request = [&](int row) {
+        if (WHAT == 2) pair = p.stats[(static_cast<long long>(seq) * p.rows + row) * p.spans + (lane < p.spans ? lane : 0)];
         const T* x = static_cast<const T*>(p.x) + seq * p.x_seq_stride + row * p.x_stride;
         const uint32_t* mask = p.mask + seq * p.mask_seq_stride + row * p.mask_stride;
 #pragma unroll
@@ -193,17 +222,54 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
     };
     request(0);
     const Penalties k = penalties_of(p, seq);
+    const int* drafts = p.drafts + static_cast<long long>(seq) * (p.rows - 1);
+    int draft = p.drafts && lane < p.rows - 1 ? drafts[lane] : -1;      // of the row after lane `lane` (of the 64 that it is among)
     if (counting || biases) count_tokens<THREADS, SPAN>(p, seq, t0, counts, biases);
-    const float scale = k.heat * 1.4426950408889634f;
+    const float scale = k.heat * 1.4426950408889634f, inverse = 1.f / k.repetition;
+
+    // z becomes z by - less: by is 1 or that of a token said before, less its penalties without its biases
+    auto less_of = [&](uint32_t c) {
+        const uint32_t said = c & ~kInPrompt;
+        return said ? __builtin_fmaf(static_cast<float>(said), k.frequency, k.presence) : 0.f;
+    };
+    float less[U][8];
+    bool seen[U][8];
+    auto look_up = [&](int u) {
+        const int at = (u * THREADS + me) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t c = counting ? counts[at + i] : 0;
+            seen[u][i] = c != 0;
+            less[u][i] = less_of(c) - (biases ? biases[at + i] : 0.f);
+        }
+    };
+    if (EARLY) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) look_up(u);
+    }
+    const bool some = counting || biases;
 
     for (int row = 0; row < p.rows; ++row) {
         // (the tokens' places are worked out anew for each row: kept over the loop, they take the registers that the logits need)
         if (!EARLY) asm volatile("" : "+v"(me));
         if (!EARLY && row > 0) request(row);
         if (row > 0 && p.drafts) {
-            const uint32_t at = static_cast<uint32_t>(p.drafts[static_cast<long long>(seq) * (p.rows - 1) + row - 1]) - static_cast<uint32_t>(t0);
-            if (at < static_cast<uint32_t>(SPAN) && static_cast<int>((at >> 3) % THREADS) == me) counts[at] += 1;
+            if ((row & 63) == 0) draft = row + lane < p.rows - 1 ? drafts[row + lane] : -1;
+            const uint32_t at = static_cast<uint32_t>(__builtin_amdgcn_readlane(draft, (row - 1) & 63)) - static_cast<uint32_t>(t0);
+            const int mine = static_cast<int>((at >> 3) % THREADS);
+            if (at < static_cast<uint32_t>(SPAN) && mine >> 6 == wave) {       // (this wave's: the counts are read by nobody else)
+                if (mine == me) counts[at] += 1;
+#pragma unroll
+                for (int u = 0; u < (EARLY ? U : 0); ++u)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (mine == me && static_cast<int>(at) == (u * THREADS + mine) * 8 + i) {
+                            seen[u][i] = true;
+                            less[u][i] = less_of(counts[at]) - (biases ? biases[at] : 0.f);
+                        }
+            }
         }
+        const f32x2 my_pair = pair;
         float z[U][8];
         uint32_t keep[U];
 #pragma unroll
@@ -217,36 +283,28 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
         if (EARLY && row + 1 < p.rows) request(row + 1);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int at = (u * THREADS + me) * 8;
-            if (counting) {
-                const u32x4 c0 = *reinterpret_cast<const u32x4*>(counts + at), c1 = *reinterpret_cast<const u32x4*>(counts + at + 4);
-                const u32x4 any = c0 | c1;
-                if ((any[0] | any[1]) | (any[2] | any[3])) {
+            if (some) {
+                if (!EARLY) look_up(u);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint32_t c = i < 4 ? c0[i & 3] : c1[i & 3], said = c & ~kInPrompt;
-                        const float y = z[u][i] > 0.f ? z[u][i] / k.repetition : z[u][i] * k.repetition;
-                        const float less = y - static_cast<float>(said) * k.frequency - k.presence;
-                        z[u][i] = c == 0 ? z[u][i] : said ? less : y;
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const float by = z[u][i] > 0.f ? inverse : k.repetition;
+                    z[u][i] = __builtin_fmaf(z[u][i], seen[u][i] ? by : 1.f, -less[u][i]);
                 }
-            }
-            if (biases) {
-                const f32x4 b0 = *reinterpret_cast<const f32x4*>(biases + at), b1 = *reinterpret_cast<const f32x4*>(biases + at + 4);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) z[u][i] += i < 4 ? b0[i & 3] : b1[i & 3];
             }
             if (WHAT == 0) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[u][i] *= k.heat;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (!((keep[u] >> i) & 1u)) z[u][i] = -INFINITY;
-            if (!EARLY) __builtin_amdgcn_sched_barrier(0);      // (one part's counts and biases at a time)
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t bit = static_cast<uint32_t>(static_cast<int>(keep[u] << (31 - i)) >> 31);         // all ones or none
+                z[u][i] = __uint_as_float((__float_as_uint(z[u][i]) & bit) | (0xff800000u & ~bit));
+            }
+            if (!EARLY) __builtin_amdgcn_sched_barrier(0);
         }
         const long long r = static_cast<long long>(seq) * p.rows + row;
         RowSum sum = {0.f, 0.f, -1};
+        float by = 0.f;                                         // makes probabilities of z's exponentials
         if constexpr (WHAT == 1 || WHAT == 3) {
             f32x2 mine;
             if (k.greedy) {
@@ -265,25 +323,38 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) top = fmaxf(top, z[u][i]);
                 top = largest_of_wave(top);
-                // (all of them -infinity: each counts nothing, but for a NaN)
-                const float from = top == -INFINITY ? 0.f : top;
+                const float from = top == -INFINITY ? 0.f : top;        // (all -infinity: sum 0, but for a NaN)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) all += __builtin_amdgcn_exp2f((z[u][i] - from) * scale);
+                    for (int i = 0; i < 8; ++i) {
+                        z[u][i] = __builtin_amdgcn_exp2f((z[u][i] - from) * scale);
+                        all += z[u][i];
+                    }
                 mine = (f32x2){top, sum_of_wave(all)};
             }
+            f32x2* mine_at = pairs + (row & 1) * WAVES;         // (the other ones may still be read)
+            if (lane == 0) mine_at[wave] = mine;
+            __syncthreads();
+            if (WHAT == 1 && wave > 0) continue;
+            sum = row_sum(mine_at[lane < WAVES ? lane : 0], mine_at, WAVES, k.greedy, scale);
             if (WHAT == 1) {
-                if ((me & 63) == 0) p.stats[(r * p.spans + span) * WAVES + wave] = mine;
+                if (lane == 0) p.stats[r * p.spans + span] = (f32x2){sum.top, k.greedy ? __int_as_float(sum.at) : sum.sum};
                 continue;
             }
-            f32x2* mine_at = pairs + (row & 1) * WAVES;         // (the other ones may still be read)
-            if ((me & 63) == 0) mine_at[wave] = mine;
-            __syncthreads();
-            sum = row_sum(mine_at, WAVES, k.greedy, scale);
+            by = sum.sum == 0.f ? 0.f : (mine[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mine[0] - sum.top) * scale)) / sum.sum;
         }
-        if constexpr (WHAT == 2) sum = row_sum(p.stats + r * p.spans * WAVES, p.spans * WAVES, k.greedy, scale);
-        const float from = sum.top == -INFINITY ? 0.f : sum.top;
+        if constexpr (WHAT == 2) {
+            sum = row_sum(my_pair, p.stats + r * p.spans, p.spans, k.greedy, scale);
+            by = sum.sum == 0.f ? 0.f : 1.f / sum.sum;
+            const float from = sum.top == -INFINITY ? 0.f : sum.top;
+            if (!k.greedy) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[u][i] = __builtin_amdgcn_exp2f((z[u][i] - from) * scale);
+            }
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int e = t0 + (u * THREADS + me) * 8;
@@ -291,7 +362,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if (k.greedy) z[u][i] = sum.top != sum.top ? sum.top : sum.at - e == i ? 1.f : 0.f;
-                    else z[u][i] = __builtin_amdgcn_exp2f((z[u][i] - from) * scale) * sum.each;
+                    else z[u][i] *= by;
                 }
             }
             if (e < p.vocab) store8_type(p.out_type, p.out, seq * p.out_seq_stride + row * p.out_stride, e, p.vocab, z[u]);

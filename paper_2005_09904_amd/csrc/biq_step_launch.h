@@ -18,8 +18,8 @@ hipError_t launch_unpack4(const Pack4Params& p, long long records, hipStream_t s
 hipError_t launch_gemm4_few(int x_type, int f, int x_scales, int lds, const Gemm4Params& p, hipStream_t s);
 hipError_t launch_gemm4_many(int x_type, int f, int x_scales, long long group_bytes, const Gemm4Params& p, hipStream_t s);
 
-// Tokens of a span of the vocabulary, and the waves that it has a pair for each.
-constexpr int kLogitsSpan = 4096, kLogitsWaves = 4;
+// Tokens of a span of the vocabulary.
+constexpr int kLogitsSpan = 4096;
 // (whole: a workgroup for a row)
 hipError_t launch_logits(int type, bool probabilities, bool whole, const LogitsParams& p, hipStream_t s);
 

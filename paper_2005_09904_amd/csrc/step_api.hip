@@ -196,7 +196,7 @@ biq_status biq_gemm4(const biq_gemm4_args* a, void* workspace, size_t workspace_
 size_t biq_logits_workspace_bytes(int seqs, int rows, int vocab) {
     if (seqs < 1 || rows < 1 || vocab < 1 || vocab > (1 << 22) || static_cast<long long>(seqs) * rows > kMaxInt) return 0;
     const size_t spans = (vocab + kLogitsSpan - 1) / kLogitsSpan;
-    return logits_whole(vocab, true) ? 0 : static_cast<size_t>(seqs) * rows * spans * kLogitsWaves * 8;
+    return logits_whole(vocab, true) ? 0 : static_cast<size_t>(seqs) * rows * spans * 8;
 }
 
 biq_status biq_logits(const biq_logits_args* a, void* workspace, size_t workspace_bytes, void* stream) {
