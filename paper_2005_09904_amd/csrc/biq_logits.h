@@ -254,7 +254,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
         if (!EARLY) asm volatile("" : "+v"(me));
         if (!EARLY && row > 0) request(row);
         if (row > 0 && p.drafts) {
-            if ((row & 63) == 0) draft = row + lane < p.rows - 1 ? drafts[row + lane] : -1;
+            if (row > 1 && ((row - 1) & 63) == 0) draft = row - 1 + lane < p.rows - 1 ? drafts[row - 1 + lane] : -1;
             const uint32_t at = static_cast<uint32_t>(__builtin_amdgcn_readlane(draft, (row - 1) & 63)) - static_cast<uint32_t>(t0);
             const int mine = static_cast<int>((at >> 3) % THREADS);
             if (at < static_cast<uint32_t>(SPAN) && mine >> 6 == wave) {       // (this wave's: the counts are read by nobody else)

@@ -19,7 +19,7 @@ hipError_t launch_gemm4_few(int x_type, int f, int x_scales, int lds, const Gemm
 hipError_t launch_gemm4_many(int x_type, int f, int x_scales, long long group_bytes, const Gemm4Params& p, hipStream_t s);
 
 // Tokens of a span of the vocabulary.
-constexpr int kLogitsSpan = 4096;
+constexpr int kLogitsSpan = 2048;
 // (whole: a workgroup for a row)
 hipError_t launch_logits(int type, bool probabilities, bool whole, const LogitsParams& p, hipStream_t s);
 

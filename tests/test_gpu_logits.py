@@ -157,6 +157,14 @@ def test_lengths_and_biases_beyond_their_bounds(biq):
     check(x, h, call(biq, x, h, "fp32", False), "fp32", False)
 
 
+@pytest.mark.parametrize("probabilities", [False, True])
+def test_more_rows_than_a_wave_has_lanes(biq, probabilities):
+    for vocab in (300, 20000):
+        x, h = inputs(2, 140, vocab, "bf16", 6, mask=False)
+        h["drafts"][:] = np.random.default_rng(1).integers(-2, 60, size=h["drafts"].shape)
+        check(x, h, call(biq, x, h, "fp32", probabilities), "fp32", probabilities)
+
+
 def test_a_long_history_and_many_biases(biq):
     rng = np.random.default_rng(9)
     x = torch.from_numpy(rng.standard_normal((2, 2, 5000)).astype(np.float32))
