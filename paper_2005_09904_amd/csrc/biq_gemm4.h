@@ -22,15 +22,15 @@ struct Gemm4Params {
     const void* x;
     const float* x_scales;   // [batch][x_groups], codes only
     void* y;
-    uint8_t* operands;       // X as operands, where there are many vectors: groups of `columns` of them
+    float* part;             // [splits][batch][16 tiles] sums of shares of the blocks (many vectors)
     long long x_stride, y_stride;
     int m, n, batch, blocks, tiles;
     int record;              // bytes of a record
     int group;               // 32, 64 or 128
     int x_group, x_groups;   // elements of a group of X's scales (0: the row), groups of a row
     int y_type;
-    int splits;              // waves that share a tile's blocks
-    int columns;
+    int splits;              // waves (many vectors: workgroups) that share a tile's blocks
+    int columns;             // vectors of a workgroup
     unsigned first;
 };
 
@@ -344,45 +344,186 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
     if (tile < p.tiles && (lane & 15) < columns) store_y4(p, column0 + (lane & 15), tile * 16 + 4 * (lane >> 4), acc[0]);
 }
 
-// Many vectors: X as operands in memory first, groups of p.columns vectors one after the other, each [operands, units].
+// Many vectors: a workgroup takes kRows4 rows, 32 a wave, up to 64 vectors and a share of the blocks.  X becomes operands on the way to LDS, two
+// blocks at a time, while the two before are multiplied; the weights go from memory to registers two blocks ahead.  Operand (j, lane / 16) of a
+// vector lies `u` = 4 j + lane / 16 places further on among its 16 vectors: neither the threads that write a vector's operands nor
+// the lanes that read 16 vectors' meet on a bank.
+constexpr int kRows4 = 32 * kWaves4;
 template <int XT>
-__global__ __launch_bounds__(256) void gemm4_operands_kernel(const Gemm4Params p, int x_scales, long long group_bytes) {
-    // (a workgroup for 16 blocks of one vector)
-    const int column = blockIdx.y, g = column / p.columns, column0 = g * p.columns;
-    const int columns = p.batch - column0 < p.columns ? p.batch - column0 : p.columns;
-    f16x8* to = reinterpret_cast<f16x8*>(p.operands + g * group_bytes);
-    float* units = reinterpret_cast<float*>(to + static_cast<long long>(p.blocks) * 16 * kTerms4<XT> * columns);
-    const int block0 = blockIdx.x * 16, block1 = block0 + 16 < p.blocks ? block0 + 16 : p.blocks;
-    stage4<XT>(p, column0, columns, column - column0, column - column0 + 1, block0, block1, x_scales, to, units, threadIdx.x, 256);
+struct Raw4 {
+    typename X4<XT>::T v[8];
+    __device__ __forceinline__ void request(const Gemm4Params& p, long long column, int e) {
+        typedef typename X4<XT>::T T;
+        typedef T Loose __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+        const T* row = static_cast<const T*>(p.x) + column * p.x_stride;
+        if (e + 8 <= p.n) {
+            const Loose all = *reinterpret_cast<const Loose*>(row + e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = all[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = row[e + i < p.n ? e + i : p.n - 1];
+        }
+    }
+};
+
+// PER_BLOCK: X has one scale in a block of 128.
+template <int XT, int F, int NC, bool PER_BLOCK>
+__global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4Params p, int x_scales) {
+    constexpr int TERMS = kTerms4<XT>, FLUSHES = 4 / F, COLS = 16 * NC, AHEAD = 2;
+    constexpr int SIDE = 2 * 4 * TERMS * 4 * COLS;              // operands of two blocks
+    constexpr bool SUMS = PER_BLOCK && !(TERMS == 2 && F == 1 && NC == 4);      // X's scale once a block (there: no registers for the block's sums)
+    extern __shared__ float lds[];
+    f16x8* operands = reinterpret_cast<f16x8*>(lds);            // [2][block][j][term][lane / 16][column]
+    float* units = reinterpret_cast<float*>(operands + 2 * SIDE);       // [2][block][scale][column]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
+    const int row_groups = (p.tiles + 2 * kWaves4 - 1) / (2 * kWaves4), split = (p.first + blockIdx.x) / row_groups;
+    const int tile = ((p.first + blockIdx.x) - split * row_groups) * 2 * kWaves4 + 2 * wave;
+    const int column0 = blockIdx.y * p.columns, columns = p.batch - column0 < p.columns ? p.batch - column0 : p.columns;
+    const int block0 = static_cast<int>(static_cast<long long>(p.blocks) * split / p.splits);
+    const int block1 = static_cast<int>(static_cast<long long>(p.blocks) * (split + 1) / p.splits);
+
+    // this thread's 8 elements of every 16th vector: unit u of the two blocks
+    const int u = threadIdx.x & 31, own = threadIdx.x >> 5;
+    Raw4<XT> raw[NC];
+    float scale[NC];
+    auto request_x = [&](int block) {
+        const int e = block * kBlock4 + u * 8;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int column = column0 + (own + 16 * c < columns ? own + 16 * c : columns - 1);
+            raw[c].request(p, column, e);
+            if constexpr (XT == kInt8 || XT == kFp8) {
+                int g = p.x_group == 0 ? 0 : e / p.x_group;     // (behind the last element: one that there is)
+                g = g < p.x_groups ? g : p.x_groups - 1;
+                scale[c] = p.x_scales[static_cast<long long>(column) * p.x_groups + g];
+            }
+        }
+    };
+    auto lay_down = [&](int side, int block) {
+        f16x8* to = operands + side * SIDE;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            f16x8 out[TERMS];
+            float unit = operand8<XT>(raw[c].v, block * kBlock4 + u * 8, p.n, out);
+            const int place = 16 * c + ((own + u) & 15);
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) to[(((u >> 2) * TERMS + t) * 4 + (u & 3)) * COLS + place] = out[t];
+            if constexpr (XT == kInt8 || XT == kFp8) unit = scale[c];
+            const int every = 16 / x_scales;
+            if ((u & 15) % every == 0) units[((side * 2 + (u >> 4)) * x_scales + (u & 15) / every) * COLS + 16 * c + own] = unit;
+        }
+    };
+
+    const uint8_t* weights[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) weights[r] = p.weights + static_cast<long long>(tile + r < p.tiles ? tile + r : p.tiles - 1) * p.blocks * p.record;
+    u32x4 codes[AHEAD][2];
+    u32x2 scales[AHEAD][2][FLUSHES];
+    auto request_w = [&](int i, int block) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const uint8_t* at = weights[r] + static_cast<long long>(block < block1 ? block : block1 - 1) * p.record;
+            codes[i][r] = *reinterpret_cast<const u32x4*>(at + 16 * lane);
+#pragma unroll
+            for (int f = 0; f < FLUSHES; ++f) scales[i][r][f] = *reinterpret_cast<const u32x2*>(at + 1024 + 32 * f * F / p.group * 32 + 8 * grp);
+        }
+    };
+
+    f32x4 acc[2][NC];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) acc[r][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    request_x(block0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) request_w(i, block0 + i);
+    lay_down(0, block0);
+    __syncthreads();
+    for (int side = 0, pair = block0; pair < block1; pair += 2, side ^= 1) {
+        if (pair + 2 < block1) request_x(pair + 2);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (pair + b >= block1) continue;
+            const f16x8* from = operands + side * SIDE + b * (SIDE / 2);
+            const float* unit = units + (side * 2 + b) * x_scales * COLS;
+            f32x4 sum[2][NC];                                   // of the block
+#pragma unroll
+            for (int f = 0; f < FLUSHES; ++f) {
+                f32x4 part[2][NC];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) part[r][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = f * F; j < f * F + F; ++j) {
+                    const f16x8 w[2] = {weights_f16(codes[b][0][j]), weights_f16(codes[b][1][j])};
+                    const int place = (lane + 16 * b + 4 * j + grp) & 15;
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) {
+                            const f16x8 x = from[((j * TERMS + t) * 4 + grp) * COLS + 16 * c + place];
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[r], x, part[r][c], 0, 0, 0);
+                        }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const u32x2 s = scales[b][r][f];
+                    const f32x4 ws = {bf16_up(s[0] & 0xffffu), __uint_as_float(s[0] & 0xffff0000u), bf16_up(s[1] & 0xffffu), __uint_as_float(s[1] & 0xffff0000u)};
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        if constexpr (SUMS) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sum[r][c][e] = f == 0 ? part[r][c][e] * ws[e] : __builtin_fmaf(part[r][c][e], ws[e], sum[r][c][e]);
+                        } else {
+                            const float v = unit[f * x_scales / FLUSHES * COLS + 16 * c + (lane & 15)];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[r][c][e] = __builtin_fmaf(part[r][c][e] * v, ws[e], acc[r][c][e]);
+                        }
+                    }
+                }
+            }
+            if constexpr (SUMS) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const float v = unit[16 * c + (lane & 15)];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[r][c][e] = __builtin_fmaf(sum[r][c][e], v, acc[r][c][e]);
+                }
+            }
+            request_w(b, pair + b + AHEAD);
+        }
+        if (pair + 2 < block1) lay_down(side ^ 1, pair + 2);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int column = (lane & 15) + 16 * c, row = (tile + r) * 16 + 4 * grp;
+            if (column >= columns || row >= p.m) continue;
+            if (p.splits == 1) {
+                store_y4(p, column0 + column, row, acc[r][c]);
+            } else {
+                // (rows of partial sums are whole tiles)
+                *reinterpret_cast<f32x4*>(p.part + (static_cast<long long>(split) * p.batch + column0 + column) * (16ll * p.tiles) + row) = acc[r][c];
+            }
+        }
 }
 
-template <int TERMS, int F, int NC>
-__global__ __launch_bounds__(64 * kWaves4) void gemm4_many_kernel(const Gemm4Params p, int x_scales, long long group_bytes) {
-    __shared__ f32x4 sums[kWaves4][NC][64];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int column0 = blockIdx.y * p.columns, columns = p.batch - column0 < p.columns ? p.batch - column0 : p.columns;
-    const f16x8* operands = reinterpret_cast<const f16x8*>(p.operands + blockIdx.y * group_bytes);
-    const float* units = reinterpret_cast<const float*>(operands + static_cast<long long>(p.blocks) * 16 * TERMS * columns);
-    const int per = kWaves4 / p.splits, split = wave % p.splits, tile = (p.first + blockIdx.x) * per + wave / p.splits;
-    f32x4 acc[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    if (tile < p.tiles)
-        tile4<TERMS, F, NC, 2>(p.weights + static_cast<long long>(tile) * p.blocks * p.record, p.record, p.group, p.blocks, split, p.splits,
-                               {operands, units, columns}, x_scales, acc);
-    if (p.splits > 1) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c) sums[wave][c][lane] = acc[c];
-        __syncthreads();
-        if (split > 0) return;
-        for (int s = 1; s < p.splits; ++s)
-#pragma unroll
-            for (int c = 0; c < NC; ++c) acc[c] += sums[wave + s][c][lane];
-    }
-    if (tile >= p.tiles) return;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-        if ((lane & 15) + 16 * c < columns) store_y4(p, column0 + (lane & 15) + 16 * c, tile * 16 + 4 * (lane >> 4), acc[c]);
+// The sums of all shares of the blocks, in their order: a thread for 4 rows of a vector.
+static __global__ __launch_bounds__(256) void gemm4_join_kernel(const Gemm4Params p) {
+    const long long quads = 4ll * p.tiles, at = static_cast<long long>(p.first + blockIdx.x) * 256 + threadIdx.x;
+    if (at >= quads * p.batch) return;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = 0; s < p.splits; ++s) sum += *reinterpret_cast<const f32x4*>(p.part + 4 * (s * quads * p.batch + at));
+    const int column = static_cast<int>(at / quads), row = static_cast<int>(at - column * quads) * 4;
+    if (row < p.m) store_y4(p, column, row, sum);
 }
 
 }  // namespace biq

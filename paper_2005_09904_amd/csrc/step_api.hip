@@ -28,7 +28,6 @@ bool write_ok(long long stride, long long rows, int n) { return read_ok(stride) 
 struct Gemm4Plan {
     bool many;
     int x_scales, f, splits, columns, lds;
-    long long group_bytes;
     size_t workspace;
 };
 
@@ -51,20 +50,24 @@ Gemm4Plan gemm4_plan(const biq_gemm4_args& a) {
     pl.x_scales = codes && a.x_group != 0 ? kBlock4 / a.x_group : 1;
     const int spans = codes && a.x_group != 0 && a.x_group < a.group ? a.x_group : a.group;
     pl.f = spans / 32;
-    pl.splits = 1;
-    while (pl.splits < kWaves4 && static_cast<long long>(tiles) * pl.splits < 256 * kWaves4) pl.splits *= 2;
     const long long column = static_cast<long long>(blocks) * (256 * terms + 4 * pl.x_scales);      // bytes of a vector as operands
     pl.columns = a.batch < 16 ? a.batch : 16;
     pl.many = a.batch > 16 || column * pl.columns > kLdsFew4;
+    pl.splits = 1;
     if (!pl.many) {
+        while (pl.splits < kWaves4 && static_cast<long long>(tiles) * pl.splits < 256 * kWaves4) pl.splits *= 2;
         const long long lds = column * pl.columns, join = pl.splits > 1 ? kWaves4 * 64 * 16 : 0;
         pl.lds = static_cast<int>(lds > join ? lds : join);
         return pl;
     }
     const int groups = (a.batch + 63) / 64;
     pl.columns = (a.batch + groups - 1) / groups;
-    pl.group_bytes = (column * pl.columns + 15) / 16 * 16;
-    pl.workspace = static_cast<size_t>(pl.group_bytes) * ((a.batch + pl.columns - 1) / pl.columns);
+    // a workgroup for every CU, four blocks each at least
+    const long long units = static_cast<long long>((a.m + kRows4 - 1) / kRows4) * groups;
+    long long splits = units >= 256 ? 1 : 256 / units;
+    splits = splits > (blocks + 3) / 4 ? (blocks + 3) / 4 : splits;
+    pl.splits = static_cast<int>(splits);
+    pl.workspace = splits == 1 ? 0 : static_cast<size_t>(splits) * a.batch * tiles * 64;
     return pl;
 }
 
@@ -173,7 +176,7 @@ biq_status biq_gemm4(const biq_gemm4_args* a, void* workspace, size_t workspace_
     p.x = a->x;
     p.x_scales = a->x_scales;
     p.y = a->y;
-    p.operands = static_cast<uint8_t*>(workspace);
+    p.part = static_cast<float*>(workspace);
     p.x_stride = a->x_stride;
     p.y_stride = a->y_stride;
     p.m = a->m;
@@ -189,7 +192,7 @@ biq_status biq_gemm4(const biq_gemm4_args* a, void* workspace, size_t workspace_
     p.splits = pl.splits;
     p.columns = pl.columns;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return status(pl.many ? launch_gemm4_many(a->x_type, pl.f, pl.x_scales, pl.group_bytes, p, s)
+    return status(pl.many ? launch_gemm4_many(a->x_type, pl.f, pl.x_scales, p, s)
                           : launch_gemm4_few(a->x_type, pl.f, pl.x_scales, pl.lds, p, s));
 }
 
