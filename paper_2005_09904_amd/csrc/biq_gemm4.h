@@ -36,14 +36,28 @@ struct Gemm4Params {
 
 __device__ __forceinline__ float bf16_up(uint32_t bits) { return __uint_as_float(bits << 16); }
 
-// 8 codes as 16-bit floats (exact).
-__device__ __forceinline__ f16x8 weights_f16(uint32_t w) {
-    union { f16x8 v; f16x2 p[4]; uint32_t w[4]; } r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r.w[i] = ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u;
-        r.p[i] -= (f16x2){1032.0f16, 1032.0f16};
+// 8 codes as 16-bit floats (exact): 4 bits below the exponent of 1024 are 1024 + u, those above them 1024 + 16 u, both u = code + 8.
+// Masks are kept in registers, one of them a vector's, as an instruction takes one constant.
+struct Masks4 {
+    uint32_t low, high, exponent;
+    __device__ __forceinline__ Masks4() : low(0x000f000fu), high(0x00f000f0u), exponent(0x64006400u) {
+        asm("" : "+v"(low));
+        asm("" : "+v"(high));
+        asm("" : "+s"(exponent));
     }
+};
+__device__ __forceinline__ f16x8 weights_f16(uint32_t w, const Masks4& m) {
+    union { f16x8 v; f16x2 p[4]; uint32_t w[4]; } r;
+    const uint32_t w8 = w >> 8;
+    r.w[0] = (w & m.low) | m.exponent;
+    r.w[1] = (w & m.high) | m.exponent;
+    r.w[2] = (w8 & m.low) | m.exponent;
+    r.w[3] = (w8 & m.high) | m.exponent;
+    const f16x2 sixteenth = {0.0625f16, 0.0625f16}, less = {-72.0f16, -72.0f16};
+    r.p[0] -= (f16x2){1032.0f16, 1032.0f16};
+    r.p[2] -= (f16x2){1032.0f16, 1032.0f16};
+    r.p[1] = __builtin_elementwise_fma(r.p[1], sixteenth, less);
+    r.p[3] = __builtin_elementwise_fma(r.p[3], sixteenth, less);
     return r.v;
 }
 
@@ -158,6 +172,16 @@ template <int XT> struct X4 { typedef typename Elem<XT>::T T; };
 template <> struct X4<kInt8> { typedef int8_t T; };
 template <> struct X4<kFp8> { typedef uint8_t T; };
 
+// The largest of 16 lanes' numbers (not below 0), in all of them: over quads, halves, all.
+__device__ __forceinline__ float over_16_lanes(float x) {
+    auto with = [&](int y) { x = fmaxf(x, __int_as_float(y)); };
+    with(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xb1, 0xf, 0xf, true));         // quad_perm [1,0,3,2]
+    with(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4e, 0xf, 0xf, true));         // quad_perm [2,3,0,1]
+    with(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, 0xf, 0xf, true));        // row_half_mirror
+    with(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x140, 0xf, 0xf, true));        // row_mirror
+    return x;
+}
+
 // 8 elements of an input vector (zeros behind its end) as terms; unit: what a 1 stands for.  The 16 lanes of a block of 128
 // call this together: 32-bit and bf16 elements are scaled by a power of two, the block's largest magnitude to [2^14, 2^15).  Elements
 // keep 22 bits (8 of bf16), and none below 2^-39 of the block's largest.
@@ -172,29 +196,28 @@ __device__ __forceinline__ float operand8(const typename X4<XT>::T (&raw)[8], in
     }
     float unit = 1.f;
     if constexpr (XT == BIQ_F32 || XT == BIQ_BF16) {
-        uint32_t most = 0;
+        // (a NaN does not count here, and comes through the products)
+        float most = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t bits = __float_as_uint(x[i]) & 0x7fffffffu;
-            most = most > bits ? most : bits;
-        }
-#pragma unroll
-        for (int d = 1; d < 16; d *= 2) {
-            const uint32_t other = __shfl_xor(most, d);
-            most = most > other ? most : other;
-        }
-        int b = static_cast<int>(most >> 23);                   // biased exponent
-        b = most == 0 ? 127 + 14 : b < 27 ? 27 : b;
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[i]));
+        most = over_16_lanes(most);
+        int b = static_cast<int>(__float_as_uint(most) >> 23);  // biased exponent
+        b = most == 0.f ? 127 + 14 : b < 27 ? 27 : b;
         const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 + 127 - b) << 23);
         unit = __uint_as_float(static_cast<uint32_t>(b - 14) << 23);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= up;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[0][i] = static_cast<_Float16>(x[i]);
-    if constexpr (kTerms4<XT> == 2) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[1][i] = static_cast<_Float16>(x[i] - static_cast<float>(out[0][i]));
+    for (int i = 0; i < 8; i += 2) {
+        const f16x2 hi = __builtin_convertvector((f32x2){x[i], x[i + 1]}, f16x2);
+        out[0][i] = hi[0];
+        out[0][i + 1] = hi[1];
+        if constexpr (kTerms4<XT> == 2) {
+            const f16x2 lo = __builtin_convertvector((f32x2){x[i] - static_cast<float>(hi[0]), x[i + 1] - static_cast<float>(hi[1])}, f16x2);
+            out[1][i] = lo[0];
+            out[1][i + 1] = lo[1];
+        }
     }
     return unit;
 }
@@ -219,13 +242,14 @@ __device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group
     int col[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) col[c] = (lane & 15) + 16 * c < x.columns ? (lane & 15) + 16 * c : x.columns - 1;
+    const Masks4 masks;
     u32x4 codes[AHEAD];
     u32x2 scales[AHEAD][FLUSHES];
     auto request = [&](int i, int block) {
         const uint8_t* at = tile + static_cast<long long>(block < blocks ? block : blocks - 1) * record;
-        codes[i] = *reinterpret_cast<const u32x4*>(at + 16 * lane);
+        codes[i] = *reinterpret_cast<const u32x4*>(at + 16u * static_cast<uint32_t>(lane));
 #pragma unroll
-        for (int f = 0; f < FLUSHES; ++f) scales[i][f] = *reinterpret_cast<const u32x2*>(at + 1024 + 32 * f * F / group * 32 + 8 * grp);
+        for (int f = 0; f < FLUSHES; ++f) scales[i][f] = *reinterpret_cast<const u32x2*>(at + 1024 + 32 * f * F / group * 32 + 8u * static_cast<uint32_t>(grp));
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) request(i, from + i * step);
@@ -241,7 +265,7 @@ __device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group
                     for (int c = 0; c < NC; ++c) part[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int j = f * F; j < f * F + F; ++j) {
-                        const f16x8 w = weights_f16(codes[i][j]);
+                        const f16x8 w = weights_f16(codes[i][j], masks);
 #pragma unroll
                         for (int t = 0; t < TERMS; ++t)
 #pragma unroll
@@ -349,24 +373,6 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
 // vector lies `u` = 4 j + lane / 16 places further on among its 16 vectors: neither the threads that write a vector's operands nor
 // the lanes that read 16 vectors' meet on a bank.
 constexpr int kRows4 = 32 * kWaves4;
-template <int XT>
-struct Raw4 {
-    typename X4<XT>::T v[8];
-    __device__ __forceinline__ void request(const Gemm4Params& p, long long column, int e) {
-        typedef typename X4<XT>::T T;
-        typedef T Loose __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-        const T* row = static_cast<const T*>(p.x) + column * p.x_stride;
-        if (e + 8 <= p.n) {
-            const Loose all = *reinterpret_cast<const Loose*>(row + e);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = all[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = row[e + i < p.n ? e + i : p.n - 1];
-        }
-    }
-};
-
 // PER_BLOCK: X has one scale in a block of 128.
 template <int XT, int F, int NC, bool PER_BLOCK>
 __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4Params p, int x_scales) {
@@ -377,27 +383,46 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
     f16x8* operands = reinterpret_cast<f16x8*>(lds);            // [2][block][j][term][lane / 16][column]
     float* units = reinterpret_cast<float*>(operands + 2 * SIDE);       // [2][block][scale][column]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
-    const int row_groups = (p.tiles + 2 * kWaves4 - 1) / (2 * kWaves4), split = (p.first + blockIdx.x) / row_groups;
-    const int tile = ((p.first + blockIdx.x) - split * row_groups) * 2 * kWaves4 + 2 * wave;
+    // (workgroups that read the same of X are `splits` apart: mostly on one XCD)
+    const int split = blockIdx.x % p.splits, tile = blockIdx.x / p.splits * 2 * kWaves4 + 2 * wave;
     const int column0 = blockIdx.y * p.columns, columns = p.batch - column0 < p.columns ? p.batch - column0 : p.columns;
     const int block0 = static_cast<int>(static_cast<long long>(p.blocks) * split / p.splits);
     const int block1 = static_cast<int>(static_cast<long long>(p.blocks) * (split + 1) / p.splits);
 
     // this thread's 8 elements of every 16th vector: unit u of the two blocks
     const int u = threadIdx.x & 31, own = threadIdx.x >> 5;
-    Raw4<XT> raw[NC];
+    typedef typename X4<XT>::T T;
+    typedef T Loose __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    const T* rows[NC];
+    const float* row_scales[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const long long column = column0 + (own + 16 * c < columns ? own + 16 * c : columns - 1);
+        rows[c] = static_cast<const T*>(p.x) + column * p.x_stride;
+        row_scales[c] = p.x_scales + column * p.x_groups;
+    }
+    T raw[NC][8];
     float scale[NC];
     auto request_x = [&](int block) {
         const int e = block * kBlock4 + u * 8;
+        if ((block + 2) * kBlock4 <= p.n) {                     // (for all threads alike)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int column = column0 + (own + 16 * c < columns ? own + 16 * c : columns - 1);
-            raw[c].request(p, column, e);
-            if constexpr (XT == kInt8 || XT == kFp8) {
-                int g = p.x_group == 0 ? 0 : e / p.x_group;     // (behind the last element: one that there is)
-                g = g < p.x_groups ? g : p.x_groups - 1;
-                scale[c] = p.x_scales[static_cast<long long>(column) * p.x_groups + g];
+            for (int c = 0; c < NC; ++c) {
+                const Loose all = *reinterpret_cast<const Loose*>(rows[c] + e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) raw[c][i] = all[i];
             }
+        } else {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) raw[c][i] = rows[c][e + i < p.n ? e + i : p.n - 1];
+        }
+        if constexpr (XT == kInt8 || XT == kFp8) {
+            int g = p.x_group == 0 ? 0 : e / p.x_group;         // (behind the last element: one that there is)
+            g = g < p.x_groups ? g : p.x_groups - 1;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) scale[c] = row_scales[c][g];
         }
     };
     auto lay_down = [&](int side, int block) {
@@ -405,7 +430,7 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             f16x8 out[TERMS];
-            float unit = operand8<XT>(raw[c].v, block * kBlock4 + u * 8, p.n, out);
+            float unit = operand8<XT>(raw[c], block * kBlock4 + u * 8, p.n, out);
             const int place = 16 * c + ((own + u) & 15);
 #pragma unroll
             for (int t = 0; t < TERMS; ++t) to[(((u >> 2) * TERMS + t) * 4 + (u & 3)) * COLS + place] = out[t];
@@ -415,6 +440,7 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
         }
     };
 
+    const Masks4 masks;
     const uint8_t* weights[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) weights[r] = p.weights + static_cast<long long>(tile + r < p.tiles ? tile + r : p.tiles - 1) * p.blocks * p.record;
@@ -424,9 +450,9 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const uint8_t* at = weights[r] + static_cast<long long>(block < block1 ? block : block1 - 1) * p.record;
-            codes[i][r] = *reinterpret_cast<const u32x4*>(at + 16 * lane);
+            codes[i][r] = *reinterpret_cast<const u32x4*>(at + 16u * static_cast<uint32_t>(lane));
 #pragma unroll
-            for (int f = 0; f < FLUSHES; ++f) scales[i][r][f] = *reinterpret_cast<const u32x2*>(at + 1024 + 32 * f * F / p.group * 32 + 8 * grp);
+            for (int f = 0; f < FLUSHES; ++f) scales[i][r][f] = *reinterpret_cast<const u32x2*>(at + 1024 + 32 * f * F / p.group * 32 + 8u * static_cast<uint32_t>(grp));
         }
     };
 
@@ -457,7 +483,7 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
                     for (int c = 0; c < NC; ++c) part[r][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int j = f * F; j < f * F + F; ++j) {
-                    const f16x8 w[2] = {weights_f16(codes[b][0][j]), weights_f16(codes[b][1][j])};
+                    const f16x8 w[2] = {weights_f16(codes[b][0][j], masks), weights_f16(codes[b][1][j], masks)};
                     const int place = (lane + 16 * b + 4 * j + grp) & 15;
 #pragma unroll
                     for (int t = 0; t < TERMS; ++t)
