@@ -15,6 +15,7 @@
 namespace biq {
 
 constexpr int kBlock4 = 128;                         // elements of a record's rows
+constexpr int kWaves4 = 8;                           // waves of a workgroup
 constexpr int kInt8 = 3, kFp8 = 4;                   // types of X beside biq_type: codes
 
 struct Gemm4Params {
@@ -26,7 +27,7 @@ struct Gemm4Params {
     long long x_stride, y_stride;
     int m, n, batch, blocks, tiles;
     int record;              // bytes of a record
-    int group;               // 32, 64 or 128
+    int group_shift;         // of 32, 64 or 128 elements
     int x_group, x_groups;   // elements of a group of X's scales (0: the row), groups of a row
     int y_type;
     int splits;              // waves (many vectors: workgroups) that share a tile's blocks
@@ -182,17 +183,40 @@ __device__ __forceinline__ float over_16_lanes(float x) {
     return x;
 }
 
-// 8 elements of an input vector (zeros behind its end) as terms; unit: what a 1 stands for.  The 16 lanes of a block of 128
-// call this together: 32-bit and bf16 elements are scaled by a power of two, the block's largest magnitude to [2^14, 2^15).  Elements
-// keep 22 bits (8 of bf16), and none below 2^-39 of the block's largest.
+// 8 adjacent elements of an input vector from e on, as they are.  Those at its end come from the last 8 there are (n >= 8), further
+// on than they should be by `late`: a branch with loads of their own would make all loads in flight be waited for.
 template <int XT>
-__device__ __forceinline__ float operand8(const typename X4<XT>::T (&raw)[8], int e, int n, f16x8 (&out)[kTerms4<XT>]) {
+struct Raw8 {
+    typedef typename X4<XT>::T T;
+    typedef T Loose __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    T __attribute__((ext_vector_type(8))) v;
+    __device__ __forceinline__ void request(const T* row, int e, int n) { v = *reinterpret_cast<const Loose*>(row + (e < n - 8 ? e : n - 8)); }
+    __device__ __forceinline__ void request_few(const T* row, int e, int n) {          // (n < 8)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = row[e + i < n ? e + i : n - 1];
+    }
+};
+__device__ __forceinline__ int late8(int e, int n) { return n < 8 || e <= n - 8 ? 0 : e - (n - 8); }
+
+// As terms (zeros behind the vector's end); returned is what a 1 stands for.  The 16 lanes of a block of 128 call this together:
+// 32-bit and bf16 elements are scaled by a power of two, the block's largest magnitude to [2^14, 2^15).  Elements keep 22 bits (8 of bf16), and
+// none below 2^-39 of the block's largest.
+template <int XT>
+__device__ __forceinline__ float operand8(const Raw8<XT>& raw, int e, int n, f16x8 (&out)[kTerms4<XT>]) {
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        if constexpr (XT == kFp8) x[i] = __builtin_amdgcn_cvt_f32_fp8(raw[i], 0);
-        else x[i] = static_cast<float>(raw[i]);
-        if (e + i >= n) x[i] = 0.f;
+        if constexpr (XT == kFp8) x[i] = __builtin_amdgcn_cvt_f32_fp8(raw.v[i], 0);
+        else x[i] = static_cast<float>(raw.v[i]);
+    }
+    if (__any(e + 8 > n)) {
+        const int late = late8(e, n);
+#pragma unroll
+        for (int d = 4; d > 0; d /= 2)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = !(late & d) ? x[i] : i + d < 8 ? x[i + d] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = e + i < n ? x[i] : 0.f;
     }
     float unit = 1.f;
     if constexpr (XT == BIQ_F32 || XT == BIQ_BF16) {
@@ -235,7 +259,7 @@ struct Operands4 {
 // A wave's share of a tile of 16 rows: blocks `from`, from + step, ..., of NC times 16 columns.  F spans of 32 share both scales.
 // AHEAD records are requested before the first of them is used.
 template <int TERMS, int F, int NC, int AHEAD>
-__device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group, int blocks, int from, int step, const Operands4& x, int x_scales,
+__device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group_shift, int blocks, int from, int step, const Operands4& x, int x_scales,
                                       f32x4 (&acc)[NC]) {
     constexpr int FLUSHES = 4 / F;
     const int lane = threadIdx.x & 63, grp = lane >> 4;
@@ -249,7 +273,7 @@ __device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group
         const uint8_t* at = tile + static_cast<long long>(block < blocks ? block : blocks - 1) * record;
         codes[i] = *reinterpret_cast<const u32x4*>(at + 16u * static_cast<uint32_t>(lane));
 #pragma unroll
-        for (int f = 0; f < FLUSHES; ++f) scales[i][f] = *reinterpret_cast<const u32x2*>(at + 1024 + 32 * f * F / group * 32 + 8u * static_cast<uint32_t>(grp));
+        for (int f = 0; f < FLUSHES; ++f) scales[i][f] = *reinterpret_cast<const u32x2*>(at + 1024 + (32 * f * F >> group_shift) * 32 + 8u * static_cast<uint32_t>(grp));
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) request(i, from + i * step);
@@ -287,41 +311,49 @@ __device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group
     }
 }
 
-// X's operands from its elements: blocks block0 .. block1 of the vectors from .. upto of `columns` ones that begin at column0.  `threads`
-// threads together (16 units of 8 elements are a block, so lanes that exchange magnitudes are all there).
+// X's operands from its elements, all threads of a workgroup; AHEAD units of 8 elements are requested together (a block has 16 units, so
+// lanes that exchange magnitudes are all there).
 template <int XT>
-__device__ __forceinline__ void stage4(const Gemm4Params& p, int column0, int columns, int from, int upto, int block0, int block1, int x_scales, f16x8* to,
-                                       float* units, int thread, int threads) {
+__device__ __forceinline__ void stage4(const Gemm4Params& p, int column0, int columns, int x_scales, f16x8* to, float* units) {
+    constexpr int THREADS = 64 * kWaves4, AHEAD = XT == BIQ_F32 ? 4 : 8;
     typedef typename X4<XT>::T T;
-    const int per = (block1 - block0) * 16;
-    for (int at = thread; at < per * (upto - from); at += threads) {
-        const int c = from + at / per, u = block0 * 16 + at % per, block = u >> 4, e = u * 8;
-        const T* row = static_cast<const T*>(p.x) + (column0 + c) * p.x_stride;
-        T raw[8];
-        typedef T Loose __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-        if (e + 8 <= p.n) {
-            const Loose all = *reinterpret_cast<const Loose*>(row + e);
+    const int per = p.blocks * 16, total = per * columns, every = 16 / x_scales;
+    for (int first = threadIdx.x; first < total; first += AHEAD * THREADS) {
+        Raw8<XT> raw[AHEAD];
+        float scale[AHEAD];
+        auto place = [&](int a, int& column, int& unit) {
+            const int at = first + a * THREADS < total ? first + a * THREADS : first;           // (again: all loads are requested)
+            column = at / per;
+            unit = at - column * per;
+        };
+        auto request = [&](bool few) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) raw[i] = all[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) raw[i] = row[e + i < p.n ? e + i : p.n - 1];
-        }
-        f16x8 out[kTerms4<XT>];
-        const float unit = operand8<XT>(raw, e, p.n, out);
-        const int j = (u >> 2) & 3, grp = u & 3;
-#pragma unroll
-        for (int t = 0; t < kTerms4<XT>; ++t) to[(((block * 4 + j) * kTerms4<XT> + t) * 4 + grp) * columns + c] = out[t];
-        if constexpr (XT == kInt8 || XT == kFp8) {
-            // (a scale of a group behind the last element is one that there is)
-            const int every = 16 / x_scales;
-            if ((u & 15) % every == 0) {
-                int g = p.x_group == 0 ? 0 : e / p.x_group;
-                g = g < p.x_groups ? g : p.x_groups - 1;
-                units[(block * x_scales + (u & 15) / every) * columns + c] = p.x_scales[static_cast<long long>(column0 + c) * p.x_groups + g];
+            for (int a = 0; a < AHEAD; ++a) {
+                int c, u;
+                place(a, c, u);
+                const T* row = static_cast<const T*>(p.x) + (column0 + c) * p.x_stride;
+                if (few) raw[a].request_few(row, u * 8, p.n);
+                else raw[a].request(row, u * 8, p.n);
+                if constexpr (XT == kInt8 || XT == kFp8) {
+                    int g = p.x_group == 0 ? 0 : u * 8 / p.x_group;     // (behind the last element: one that there is)
+                    g = g < p.x_groups ? g : p.x_groups - 1;
+                    scale[a] = p.x_scales[static_cast<long long>(column0 + c) * p.x_groups + g];
+                }
             }
-        } else if ((u & 15) == 0) {
-            units[block * columns + c] = unit;
+        };
+        if (p.n < 8) request(true);
+        else request(false);
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            if (first + a * THREADS >= total) break;
+            int c, u;
+            place(a, c, u);
+            f16x8 out[kTerms4<XT>];
+            float unit = operand8<XT>(raw[a], u * 8, p.n, out);
+#pragma unroll
+            for (int t = 0; t < kTerms4<XT>; ++t) to[(((u >> 2) * kTerms4<XT> + t) * 4 + (u & 3)) * columns + c] = out[t];
+            if constexpr (XT == kInt8 || XT == kFp8) unit = scale[a];
+            if ((u & 15) % every == 0) units[((u >> 4) * x_scales + (u & 15) / every) * columns + c] = unit;
         }
     }
 }
@@ -342,7 +374,6 @@ __device__ __forceinline__ void store_y4(const Gemm4Params& p, int column, int r
 
 // A few vectors: all of them as operands in LDS.  The WAVES waves of a workgroup take WAVES / splits tiles; waves of a tile
 // share its blocks and are joined through LDS.
-constexpr int kWaves4 = 8;
 template <int XT, int F>
 __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Params p, int x_scales) {
     extern __shared__ float lds[];
@@ -350,12 +381,12 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
     const int column0 = blockIdx.y * 16, columns = p.batch - column0 < 16 ? p.batch - column0 : 16;
     f16x8* operands = reinterpret_cast<f16x8*>(lds);
     float* units = reinterpret_cast<float*>(operands + p.blocks * 16 * kTerms4<XT> * columns);
-    stage4<XT>(p, column0, columns, 0, columns, 0, p.blocks, x_scales, operands, units, threadIdx.x, 64 * kWaves4);
+    stage4<XT>(p, column0, columns, x_scales, operands, units);
     __syncthreads();
     const int per = kWaves4 / p.splits, split = wave % p.splits, tile = (p.first + blockIdx.x) * per + wave / p.splits;
     f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
     if (tile < p.tiles)
-        tile4<kTerms4<XT>, F, 1, 4>(p.weights + static_cast<long long>(tile) * p.blocks * p.record, p.record, p.group, p.blocks, split, p.splits,
+        tile4<kTerms4<XT>, F, 1, 4>(p.weights + static_cast<long long>(tile) * p.blocks * p.record, p.record, p.group_shift, p.blocks, split, p.splits,
                                     {operands, units, columns}, x_scales, acc);
     if (p.splits > 1) {
         __syncthreads();                                        // (the operands are read)
@@ -368,7 +399,7 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
     if (tile < p.tiles && (lane & 15) < columns) store_y4(p, column0 + (lane & 15), tile * 16 + 4 * (lane >> 4), acc[0]);
 }
 
-// Many vectors: a workgroup takes kRows4 rows, 32 a wave, up to 64 vectors and a share of the blocks.  X becomes operands on the way to LDS, two
+// Many vectors (of 8 elements at least): a workgroup takes kRows4 rows, 32 a wave, up to 64 vectors and a share of the blocks.  X becomes operands on the way to LDS, two
 // blocks at a time, while the two before are multiplied; the weights go from memory to registers two blocks ahead.  Operand (j, lane / 16) of a
 // vector lies `u` = 4 j + lane / 16 places further on among its 16 vectors: neither the threads that write a vector's operands nor
 // the lanes that read 16 vectors' meet on a bank.
@@ -392,7 +423,6 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
     // this thread's 8 elements of every 16th vector: unit u of the two blocks
     const int u = threadIdx.x & 31, own = threadIdx.x >> 5;
     typedef typename X4<XT>::T T;
-    typedef T Loose __attribute__((ext_vector_type(8), aligned(sizeof(T))));
     const T* rows[NC];
     const float* row_scales[NC];
 #pragma unroll
@@ -401,23 +431,12 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
         rows[c] = static_cast<const T*>(p.x) + column * p.x_stride;
         row_scales[c] = p.x_scales + column * p.x_groups;
     }
-    T raw[NC][8];
+    Raw8<XT> raw[NC];
     float scale[NC];
     auto request_x = [&](int block) {
         const int e = block * kBlock4 + u * 8;
-        if ((block + 2) * kBlock4 <= p.n) {                     // (for all threads alike)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const Loose all = *reinterpret_cast<const Loose*>(rows[c] + e);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) raw[c][i] = all[i];
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) raw[c][i] = rows[c][e + i < p.n ? e + i : p.n - 1];
-        }
+        for (int c = 0; c < NC; ++c) raw[c].request(rows[c], e, p.n);
         if constexpr (XT == kInt8 || XT == kFp8) {
             int g = p.x_group == 0 ? 0 : e / p.x_group;         // (behind the last element: one that there is)
             g = g < p.x_groups ? g : p.x_groups - 1;
@@ -452,7 +471,7 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
             const uint8_t* at = weights[r] + static_cast<long long>(block < block1 ? block : block1 - 1) * p.record;
             codes[i][r] = *reinterpret_cast<const u32x4*>(at + 16u * static_cast<uint32_t>(lane));
 #pragma unroll
-            for (int f = 0; f < FLUSHES; ++f) scales[i][r][f] = *reinterpret_cast<const u32x2*>(at + 1024 + 32 * f * F / p.group * 32 + 8u * static_cast<uint32_t>(grp));
+            for (int f = 0; f < FLUSHES; ++f) scales[i][r][f] = *reinterpret_cast<const u32x2*>(at + 1024 + (32 * f * F >> p.group_shift) * 32 + 8u * static_cast<uint32_t>(grp));
         }
     };
 
@@ -467,50 +486,45 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
     lay_down(0, block0);
     __syncthreads();
     for (int side = 0, pair = block0; pair < block1; pair += 2, side ^= 1) {
-        if (pair + 2 < block1) request_x(pair + 2);
+        request_x(pair + 2 < block1 ? pair + 2 : pair);         // (always: a branch would make the loads before it be waited for)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             if (pair + b >= block1) continue;
             const f16x8* from = operands + side * SIDE + b * (SIDE / 2);
             const float* unit = units + (side * 2 + b) * x_scales * COLS;
-            f32x4 sum[2][NC];                                   // of the block
-#pragma unroll
-            for (int f = 0; f < FLUSHES; ++f) {
-                f32x4 part[2][NC];
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) part[r][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = f * F; j < f * F + F; ++j) {
-                    const f16x8 w[2] = {weights_f16(codes[b][0][j], masks), weights_f16(codes[b][1][j], masks)};
-                    const int place = (lane + 16 * b + 4 * j + grp) & 15;
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-                        for (int c = 0; c < NC; ++c) {
-                            const f16x8 x = from[((j * TERMS + t) * 4 + grp) * COLS + 16 * c + place];
-#pragma unroll
-                            for (int r = 0; r < 2; ++r) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[r], x, part[r][c], 0, 0, 0);
-                        }
+            f32x4 sum[2][NC], part[2][NC];                      // of the block, of the spans that share scales
+            f16x8 w[2];
+            // operand (j, term, column tile) of X and its two products
+            read_ahead<4 * TERMS * NC, 2, false>([&](int i) {
+                const int j = i / (TERMS * NC), t = i / NC % TERMS, c = i % NC;
+                return from[((j * TERMS + t) * 4 + grp) * COLS + 16 * c + ((lane + 4 * j + grp) & 15)];
+            }, [&](int i, f16x8 x) {
+                const int j = i / (TERMS * NC), t = i / NC % TERMS, c = i % NC, f = j / F;
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                if (t == 0 && c == 0) {
+                    w[0] = weights_f16(codes[b][0][j], masks);
+                    w[1] = weights_f16(codes[b][1][j], masks);
                 }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[r], x, t == 0 && j % F == 0 ? zero : part[r][c], 0, 0, 0);
+                if (t < TERMS - 1 || j % F != F - 1 || c < NC - 1) return;
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const u32x2 s = scales[b][r][f];
                     const f32x4 ws = {bf16_up(s[0] & 0xffffu), __uint_as_float(s[0] & 0xffff0000u), bf16_up(s[1] & 0xffffu), __uint_as_float(s[1] & 0xffff0000u)};
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) {
+                    for (int k = 0; k < NC; ++k) {
                         if constexpr (SUMS) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) sum[r][c][e] = f == 0 ? part[r][c][e] * ws[e] : __builtin_fmaf(part[r][c][e], ws[e], sum[r][c][e]);
+                            for (int e = 0; e < 4; ++e) sum[r][k][e] = f == 0 ? part[r][k][e] * ws[e] : __builtin_fmaf(part[r][k][e], ws[e], sum[r][k][e]);
                         } else {
-                            const float v = unit[f * x_scales / FLUSHES * COLS + 16 * c + (lane & 15)];
+                            const float v = unit[f * x_scales / FLUSHES * COLS + 16 * k + (lane & 15)];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[r][c][e] = __builtin_fmaf(part[r][c][e] * v, ws[e], acc[r][c][e]);
+                            for (int e = 0; e < 4; ++e) acc[r][k][e] = __builtin_fmaf(part[r][k][e] * v, ws[e], acc[r][k][e]);
                         }
                     }
                 }
-            }
+            });
             if constexpr (SUMS) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {

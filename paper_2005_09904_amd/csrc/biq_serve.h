@@ -180,4 +180,37 @@ __device__ __forceinline__ float sum_over_groups(float x) {
     return x + __shfl_xor(x, 32);
 }
 
+// READS operands from LDS and the EACH products of every one of them: read(i) four ahead of use(i, operand).  (Left alone, the compiler
+// reads each operand right before its products and waits for it.)  Either the scheduler is asked for this order, which leaves it
+// free to place what else there is to do (two prompts with heads of 128: 806 us instead of 812), or, FENCED, the reads stand where they
+// are meant to be and only other vector and scalar instructions pass: with heads above 128 the scheduler gives up its own order now and
+// then (heads of 256 in bf16: 365 us instead of 288).
+template <int READS, int EACH, bool FENCED, typename Read, typename Use>
+__device__ __forceinline__ void read_ahead(const Read& read, const Use& use) {
+    constexpr int kAhead = 4;
+    if constexpr (FENCED) {
+        constexpr int kVectorAndScalar = 0x6;
+        f16x8 ring[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) ring[i] = read(i);
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            use(i, ring[i % kAhead]);
+            if (i + kAhead < READS) ring[i % kAhead] = read(i + kAhead);
+            __builtin_amdgcn_sched_barrier(kVectorAndScalar);
+        }
+    } else {
+        constexpr int kReads = 0x100, kProducts = 0x8;
+#pragma unroll
+        for (int i = 0; i < READS; ++i) use(i, read(i));
+        __builtin_amdgcn_sched_group_barrier(kReads, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < READS - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kProducts, EACH, 0);
+            __builtin_amdgcn_sched_group_barrier(kReads, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kProducts, kAhead * EACH, 0);
+    }
+}
+
 }  // namespace biq

@@ -52,7 +52,7 @@ Gemm4Plan gemm4_plan(const biq_gemm4_args& a) {
     pl.f = spans / 32;
     const long long column = static_cast<long long>(blocks) * (256 * terms + 4 * pl.x_scales);      // bytes of a vector as operands
     pl.columns = a.batch < 16 ? a.batch : 16;
-    pl.many = a.batch > 16 || column * pl.columns > kLdsFew4;
+    pl.many = a.n >= 8 && (a.batch > 16 || column * pl.columns > kLdsFew4);
     pl.splits = 1;
     if (!pl.many) {
         while (pl.splits < kWaves4 && static_cast<long long>(tiles) * pl.splits < 256 * kWaves4) pl.splits *= 2;
@@ -185,7 +185,7 @@ biq_status biq_gemm4(const biq_gemm4_args* a, void* workspace, size_t workspace_
     p.blocks = (a->n + kBlock4 - 1) / kBlock4;
     p.tiles = (a->m + 15) / 16;
     p.record = record_bytes(a->group);
-    p.group = a->group;
+    p.group_shift = a->group == 32 ? 5 : a->group == 64 ? 6 : 7;
     p.x_group = codes ? a->x_group : 0;
     p.x_groups = groups_of(a->n, p.x_group);
     p.y_type = a->y_type;

@@ -98,7 +98,7 @@ def test_quantizer(biq, typ, group, m, n):
 @pytest.mark.parametrize("kind,x_group", [("fp32", 0), ("bf16", 0), ("fp16", 0), ("int8", 0), ("int8", 32), ("int8", 128), ("fp8", 64), ("fp8", 0)])
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("m,n,batch", [(1, 1, 1), (16, 128, 1), (17, 127, 2), (50, 129, 3), (100, 1000, 15), (130, 700, 16), (64, 500, 17), (35, 4100, 33),
-                                       (20, 260, 64), (19, 300, 65), (48, 140, 130), (3000, 513, 5), (40000, 130, 2)])
+                                       (20, 260, 64), (19, 300, 65), (9, 3, 40), (30, 7, 2), (31, 8, 33), (33, 13, 20), (5, 263, 18), (48, 140, 130), (3000, 513, 5), (40000, 130, 2)])
 def test_products(biq, kind, x_group, group, m, n, batch):
     codes, scales = weights(m, n, group, m + n)
     x, x_scales, values = inputs(batch, n, kind, x_group, batch)
