@@ -3,7 +3,7 @@
 //   Y[b][i] = sum over groups g of scale[i][g] * sum over the group's j of code[i][j] X[b][j]
 //
 // Layout: records of 16 rows and 128 elements of each, all records of 16 rows one after the other.  A record holds 64 x 16 bytes
-// of codes, then the bfloat16 scales [128 / group][16].  Lane l of a wave takes the l-th 16 bytes: row l % 16, and of each of
+// of codes, then the bfloat16 scales [rows / 4][128 / group][4].  Lane l of a wave takes the l-th 16 bytes: row l % 16, and of each of
 // the four spans of 32 elements the 8 from 8 (l / 16) on (a dword): the left operand of one 16 x 16 x 32 product per dword, whose
 // 32 elements belong to one group.  A dword holds code + 8 of element 2 i in its bits 4 i and of element 2 i + 1 in its bits
 // 16 + 4 i: ((w >> 4 i) & 0x000f000f) | 0x64006400 is two 16-bit floats 1024 + code + 8.
@@ -27,7 +27,6 @@ struct Gemm4Params {
     long long x_stride, y_stride;
     int m, n, batch, blocks, tiles;
     int record;              // bytes of a record
-    int group_shift;         // of 32, 64 or 128 elements
     int x_group, x_groups;   // elements of a group of X's scales (0: the row), groups of a row
     int y_type;
     int splits;              // waves (many vectors: workgroups) that share a tile's blocks
@@ -77,7 +76,7 @@ __device__ __forceinline__ void lay_out4(uint8_t* record, int tile, int block, i
     reinterpret_cast<uint32_t*>(record)[dword] = w;
     const int per = kBlock4 / group;                            // scales of a row in a record
     if (dword < 16 * per) {
-        const int r = tile * 16 + (dword & 15), g = block * per + (dword >> 4);
+        const int r = tile * 16 + dword / (4 * per) * 4 + (dword & 3), g = block * per + dword / 4 % per;
         const bool there = r < m && g * group < n;
         reinterpret_cast<uint16_t*>(record + 1024)[dword] = there ? scale(r, g) : 0;
     }
@@ -157,7 +156,8 @@ static __global__ __launch_bounds__(256) void unpack4_kernel(const Pack4Params p
     const int lane = threadIdx.x >> 2, j = threadIdx.x & 3, row = tile * 16 + (lane & 15), e0 = block * kBlock4 + 32 * j + 8 * (lane >> 4);
     const uint8_t* record = p.packed + at * p.record;
     const uint32_t w = reinterpret_cast<const uint32_t*>(record)[threadIdx.x];
-    const float scale = bf16_up(reinterpret_cast<const uint16_t*>(record + 1024)[32 * j / p.group * 16 + (lane & 15)]);
+    const int per = kBlock4 / p.group, r = lane & 15;
+    const float scale = bf16_up(reinterpret_cast<const uint16_t*>(record + 1024)[((r >> 2) * per + 32 * j / p.group) * 4 + (r & 3)]);
     if (row >= p.m) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -256,10 +256,28 @@ struct Operands4 {
     int columns;
 };
 
-// A wave's share of a tile of 16 rows: blocks `from`, from + step, ..., of NC times 16 columns.  F spans of 32 share both scales.
-// AHEAD records are requested before the first of them is used.
-template <int TERMS, int F, int NC, int AHEAD>
-__device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group_shift, int blocks, int from, int step, const Operands4& x, int x_scales,
+// A lane's part of a record: 16 bytes of codes, and the scales of its 4 rows of products, G spans of 32 elements each.
+template <int G>
+struct Part4 {
+    typedef uint32_t Scales __attribute__((ext_vector_type(8 / G)));
+    u32x4 codes;
+    Scales scales;
+    __device__ __forceinline__ void request(const uint8_t* record, int lane) {
+        codes = *reinterpret_cast<const u32x4*>(record + 16u * static_cast<uint32_t>(lane));
+        typedef uint32_t Loose __attribute__((ext_vector_type(8 / G), aligned(8)));
+        scales = *reinterpret_cast<const Loose*>(record + 1024 + 32u / G * static_cast<uint32_t>(lane >> 4));
+    }
+    // Of span j.
+    __device__ __forceinline__ f32x4 of(int j) const {
+        const uint32_t a = scales[j / G * 2], b = scales[j / G * 2 + 1];
+        return (f32x4){bf16_up(a), __uint_as_float(a & 0xffff0000u), bf16_up(b), __uint_as_float(b & 0xffff0000u)};
+    }
+};
+
+// A wave's share of a tile of 16 rows: blocks `from`, from + step, ..., of NC times 16 columns.  F spans of 32 share both scales, G the
+// weights'.  AHEAD records are requested before the first of them is used.
+template <int TERMS, int F, int G, int NC, int AHEAD>
+__device__ __forceinline__ void tile4(const uint8_t* tile, int record, int blocks, int from, int step, const Operands4& x, int x_scales,
                                       f32x4 (&acc)[NC]) {
     constexpr int FLUSHES = 4 / F;
     const int lane = threadIdx.x & 63, grp = lane >> 4;
@@ -267,14 +285,8 @@ __device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group
 #pragma unroll
     for (int c = 0; c < NC; ++c) col[c] = (lane & 15) + 16 * c < x.columns ? (lane & 15) + 16 * c : x.columns - 1;
     const Masks4 masks;
-    u32x4 codes[AHEAD];
-    u32x2 scales[AHEAD][FLUSHES];
-    auto request = [&](int i, int block) {
-        const uint8_t* at = tile + static_cast<long long>(block < blocks ? block : blocks - 1) * record;
-        codes[i] = *reinterpret_cast<const u32x4*>(at + 16u * static_cast<uint32_t>(lane));
-#pragma unroll
-        for (int f = 0; f < FLUSHES; ++f) scales[i][f] = *reinterpret_cast<const u32x2*>(at + 1024 + (32 * f * F >> group_shift) * 32 + 8u * static_cast<uint32_t>(grp));
-    };
+    Part4<G> parts[AHEAD];
+    auto request = [&](int i, int block) { parts[i].request(tile + static_cast<long long>(block < blocks ? block : blocks - 1) * record, lane); };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) request(i, from + i * step);
     for (int b0 = from; b0 < blocks; b0 += AHEAD * step) {
@@ -289,15 +301,14 @@ __device__ __forceinline__ void tile4(const uint8_t* tile, int record, int group
                     for (int c = 0; c < NC; ++c) part[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int j = f * F; j < f * F + F; ++j) {
-                        const f16x8 w = weights_f16(codes[i][j], masks);
+                        const f16x8 w = weights_f16(parts[i].codes[j], masks);
 #pragma unroll
                         for (int t = 0; t < TERMS; ++t)
 #pragma unroll
                             for (int c = 0; c < NC; ++c)
                                 part[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w, x.x[(((block * 4 + j) * TERMS + t) * 4 + grp) * x.columns + col[c]], part[c], 0, 0, 0);
                     }
-                    const f32x4 ws = {bf16_up(scales[i][f][0] & 0xffffu), __uint_as_float(scales[i][f][0] & 0xffff0000u),
-                                      bf16_up(scales[i][f][1] & 0xffffu), __uint_as_float(scales[i][f][1] & 0xffff0000u)};
+                    const f32x4 ws = parts[i].of(f * F);
 #pragma unroll
                     for (int c = 0; c < NC; ++c) {
                         const float unit = x.units[(block * x_scales + f * x_scales / FLUSHES) * x.columns + col[c]];
@@ -374,7 +385,7 @@ __device__ __forceinline__ void store_y4(const Gemm4Params& p, int column, int r
 
 // A few vectors: all of them as operands in LDS.  The WAVES waves of a workgroup take WAVES / splits tiles; waves of a tile
 // share its blocks and are joined through LDS.
-template <int XT, int F>
+template <int XT, int F, int G>
 __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Params p, int x_scales) {
     extern __shared__ float lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -386,7 +397,7 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
     const int per = kWaves4 / p.splits, split = wave % p.splits, tile = (p.first + blockIdx.x) * per + wave / p.splits;
     f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
     if (tile < p.tiles)
-        tile4<kTerms4<XT>, F, 1, 4>(p.weights + static_cast<long long>(tile) * p.blocks * p.record, p.record, p.group_shift, p.blocks, split, p.splits,
+        tile4<kTerms4<XT>, F, G, 1, 4>(p.weights + static_cast<long long>(tile) * p.blocks * p.record, p.record, p.blocks, split, p.splits,
                                     {operands, units, columns}, x_scales, acc);
     if (p.splits > 1) {
         __syncthreads();                                        // (the operands are read)
@@ -405,7 +416,7 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
 // the lanes that read 16 vectors' meet on a bank.
 constexpr int kRows4 = 32 * kWaves4;
 // PER_BLOCK: X has one scale in a block of 128.
-template <int XT, int F, int NC, bool PER_BLOCK>
+template <int XT, int F, int G, int NC, bool PER_BLOCK>
 __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4Params p, int x_scales) {
     constexpr int TERMS = kTerms4<XT>, FLUSHES = 4 / F, COLS = 16 * NC, AHEAD = 2;
     constexpr int SIDE = 2 * 4 * TERMS * 4 * COLS;              // operands of two blocks
@@ -463,16 +474,10 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
     const uint8_t* weights[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) weights[r] = p.weights + static_cast<long long>(tile + r < p.tiles ? tile + r : p.tiles - 1) * p.blocks * p.record;
-    u32x4 codes[AHEAD][2];
-    u32x2 scales[AHEAD][2][FLUSHES];
+    Part4<G> parts[AHEAD][2];
     auto request_w = [&](int i, int block) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const uint8_t* at = weights[r] + static_cast<long long>(block < block1 ? block : block1 - 1) * p.record;
-            codes[i][r] = *reinterpret_cast<const u32x4*>(at + 16u * static_cast<uint32_t>(lane));
-#pragma unroll
-            for (int f = 0; f < FLUSHES; ++f) scales[i][r][f] = *reinterpret_cast<const u32x2*>(at + 1024 + (32 * f * F >> p.group_shift) * 32 + 8u * static_cast<uint32_t>(grp));
-        }
+        for (int r = 0; r < 2; ++r) parts[i][r].request(weights[r] + static_cast<long long>(block < block1 ? block : block1 - 1) * p.record, lane);
     };
 
     f32x4 acc[2][NC];
@@ -502,16 +507,15 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
                 const int j = i / (TERMS * NC), t = i / NC % TERMS, c = i % NC, f = j / F;
                 const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
                 if (t == 0 && c == 0) {
-                    w[0] = weights_f16(codes[b][0][j], masks);
-                    w[1] = weights_f16(codes[b][1][j], masks);
+                    w[0] = weights_f16(parts[b][0].codes[j], masks);
+                    w[1] = weights_f16(parts[b][1].codes[j], masks);
                 }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) part[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[r], x, t == 0 && j % F == 0 ? zero : part[r][c], 0, 0, 0);
                 if (t < TERMS - 1 || j % F != F - 1 || c < NC - 1) return;
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const u32x2 s = scales[b][r][f];
-                    const f32x4 ws = {bf16_up(s[0] & 0xffffu), __uint_as_float(s[0] & 0xffff0000u), bf16_up(s[1] & 0xffffu), __uint_as_float(s[1] & 0xffff0000u)};
+                    const f32x4 ws = parts[b][r].of(f * F);
 #pragma unroll
                     for (int k = 0; k < NC; ++k) {
                         if constexpr (SUMS) {

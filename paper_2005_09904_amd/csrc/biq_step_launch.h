@@ -14,9 +14,9 @@ hipError_t launch_norm(int type, const NormParams& p, hipStream_t s);
 hipError_t launch_pack4(const Pack4Params& p, long long records, hipStream_t s);
 hipError_t launch_quantize4(int type, const Pack4Params& p, long long records, hipStream_t s);
 hipError_t launch_unpack4(const Pack4Params& p, long long records, hipStream_t s);
-// (x_scales: scales of X in 128 elements; f: spans of 32 elements that share both scales)
-hipError_t launch_gemm4_few(int x_type, int f, int x_scales, int lds, const Gemm4Params& p, hipStream_t s);
-hipError_t launch_gemm4_many(int x_type, int f, int x_scales, const Gemm4Params& p, hipStream_t s);
+// (x_scales: scales of X in 128 elements; f: spans of 32 elements that share both scales, g: the weights')
+hipError_t launch_gemm4_few(int x_type, int f, int g, int x_scales, int lds, const Gemm4Params& p, hipStream_t s);
+hipError_t launch_gemm4_many(int x_type, int f, int g, int x_scales, const Gemm4Params& p, hipStream_t s);
 
 // Tokens of a span of the vocabulary.
 constexpr int kLogitsSpan = 2048;

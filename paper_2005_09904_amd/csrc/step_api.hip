@@ -27,7 +27,7 @@ bool write_ok(long long stride, long long rows, int n) { return read_ok(stride) 
 
 struct Gemm4Plan {
     bool many;
-    int x_scales, f, splits, columns, lds;
+    int x_scales, f, g, splits, columns, lds;
     size_t workspace;
 };
 
@@ -50,6 +50,7 @@ Gemm4Plan gemm4_plan(const biq_gemm4_args& a) {
     pl.x_scales = codes && a.x_group != 0 ? kBlock4 / a.x_group : 1;
     const int spans = codes && a.x_group != 0 && a.x_group < a.group ? a.x_group : a.group;
     pl.f = spans / 32;
+    pl.g = a.group / 32;
     const long long column = static_cast<long long>(blocks) * (256 * terms + 4 * pl.x_scales);      // bytes of a vector as operands
     pl.columns = a.batch < 16 ? a.batch : 16;
     pl.many = a.n >= 8 && (a.batch > 16 || column * pl.columns > kLdsFew4);
@@ -185,15 +186,14 @@ biq_status biq_gemm4(const biq_gemm4_args* a, void* workspace, size_t workspace_
     p.blocks = (a->n + kBlock4 - 1) / kBlock4;
     p.tiles = (a->m + 15) / 16;
     p.record = record_bytes(a->group);
-    p.group_shift = a->group == 32 ? 5 : a->group == 64 ? 6 : 7;
     p.x_group = codes ? a->x_group : 0;
     p.x_groups = groups_of(a->n, p.x_group);
     p.y_type = a->y_type;
     p.splits = pl.splits;
     p.columns = pl.columns;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return status(pl.many ? launch_gemm4_many(a->x_type, pl.f, pl.x_scales, p, s)
-                          : launch_gemm4_few(a->x_type, pl.f, pl.x_scales, pl.lds, p, s));
+    return status(pl.many ? launch_gemm4_many(a->x_type, pl.f, pl.g, pl.x_scales, p, s)
+                          : launch_gemm4_few(a->x_type, pl.f, pl.g, pl.x_scales, pl.lds, p, s));
 }
 
 size_t biq_logits_workspace_bytes(int seqs, int rows, int vocab) {
