@@ -17,6 +17,13 @@
 
 namespace biq {
 
+// How the units of sequences that share their first tokens are dealt to workgroups.
+struct SharedMap {
+    int row_tiles;
+    int splits, split_steps; // pieces of a unit's steps; of own tokens the steps of each but the last, which has what is left
+    int set;                 // set of partial results of the first piece
+};
+
 struct AttendParams {
     Cache cache;
     Ragged ragged;
@@ -33,9 +40,8 @@ struct AttendParams {
     float scale;             // |scale| * log2(e)
     // Of a call whose sequences share their first tokens (SharedUnit):
     int shared;              // these tokens
-    int front;               // this launch: the shared tokens for all rows of the call, else each sequence's own ones
-    int splits, split_steps; // pieces of a unit's steps; of own tokens the steps of each but the last, which has what is left
-    int set;                 // set of partial results of the first piece
+    int front_groups;        // workgroups of this launch that have shared tokens; those behind them have own ones
+    SharedMap map[2];        // of the shared tokens, of the own ones
 };
 
 // What a workgroup spends on a unit beside its steps (rows, first keys, joining its waves, results), in steps: 32 sequences of 410 ..
@@ -251,25 +257,29 @@ __device__ __forceinline__ SeenBy seen_by(const RowPlace (&place)[NT]) {
 // A workgroup's tile of ROWS rows and its piece of the tokens, begin .. end.  Tiles that read the same tokens are splits * heads
 // workgroups apart, mostly on one XCD.
 struct SharedUnit {
-    int seq, head, tile, split, len, rows_all, begin, end;
+    int seq, head, tile, len, rows_all, begin, end;
+    int set;
     RowRange range;
-    bool none;               // no rows
+    bool front, none;        // of the shared tokens; without rows
 };
 template <int ROWS>
 __device__ __forceinline__ SharedUnit shared_unit(const AttendParams& p) {
     SharedUnit u;
-    const int group = p.first + blockIdx.x, pairs = p.cache.heads * p.splits;
-    const int at = group % pairs;
+    int group = p.first + blockIdx.x;
+    u.front = group < p.front_groups;
+    if (!u.front) group -= p.front_groups;
+    const SharedMap m = u.front ? p.map[0] : p.map[1];
+    const int pairs = p.cache.heads * m.splits, at = group % pairs, split = at / p.cache.heads;
     u.head = at % p.cache.heads;
-    u.split = at / p.cache.heads;
-    u.seq = group / pairs / p.row_tiles;
-    u.tile = group / pairs - u.seq * p.row_tiles;
-    if (p.front) {
+    u.seq = group / pairs / m.row_tiles;
+    u.tile = group / pairs - u.seq * m.row_tiles;
+    u.set = m.set + split;
+    if (u.front) {
         const long long steps = (p.shared + 63) >> 6;
         u.len = p.shared;
         u.range = {0, p.ragged.rows, 0};
-        u.begin = static_cast<int>(steps * u.split / p.splits) * 64;
-        u.end = static_cast<int>(steps * (u.split + 1) / p.splits) * 64;
+        u.begin = static_cast<int>(steps * split / m.splits) * 64;
+        u.end = static_cast<int>(steps * (split + 1) / m.splits) * 64;
     } else {
         u.len = p.cache.length(u.seq);
         u.range = p.ragged.range(u.seq, u.len);
@@ -277,8 +287,8 @@ __device__ __forceinline__ SharedUnit shared_unit(const AttendParams& p) {
         lo = lo < 0 ? 0 : lo & ~63;
         lo = lo < p.shared ? p.shared : lo;
         const int steps = u.len > lo ? (u.len - lo + 63) >> 6 : 0;
-        const int from = u.split * p.split_steps;               // (the host has checked the product)
-        const int upto = u.split == p.splits - 1 ? steps : from + p.split_steps < steps ? from + p.split_steps : steps;
+        const int from = split * m.split_steps;                 // (the host has checked the product)
+        const int upto = split == m.splits - 1 ? steps : from + m.split_steps < steps ? from + m.split_steps : steps;
         u.begin = lo + (from < upto ? from : upto) * 64;
         u.end = lo + upto * 64;
     }
@@ -288,8 +298,8 @@ __device__ __forceinline__ SharedUnit shared_unit(const AttendParams& p) {
 }
 
 // Where the partial result of a row lies, in rows of a set's sums.
-__device__ __forceinline__ long long partial_at(const AttendParams& p, int split, long long row, int head) {
-    return (static_cast<long long>(p.set + split) * p.ragged.rows + row) * p.q_heads + head;
+__device__ __forceinline__ long long partial_at(const AttendParams& p, int set, long long row, int head) {
+    return (static_cast<long long>(set) * p.ragged.rows + row) * p.q_heads + head;
 }
 
 // Elements of the row of a lane's column: part (c, h) holds elements 64 c + 16 (lane / 16) + 8 h ..  Lanes without a row and parts
@@ -602,7 +612,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     RowElems<TYPE, CH, false> elems[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        place[n] = SHARED && p.front ? shared_place(p, head, row0 + n * 16 + col, rows_all) : row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
+        place[n] = SHARED && piece.front ? shared_place(p, head, row0 + n * 16 + col, rows_all) : row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
         elems[n].request(p, place[n], range.first, dim, grp);
     }
     u32x4 kc[4][CH];                                            // token 4 t + col % 4 of that block
@@ -642,7 +652,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     // tokens that every row of the tile sees
     int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0;
     int all_hi = p.causal ? pos_first : len - 1;
-    if (SHARED && p.front) {
+    if (SHARED && piece.front) {
         const SeenBy seen = seen_by(place);
         all_lo = seen.all_lo;
         all_hi = seen.all_hi;
@@ -758,7 +768,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
         }
         if constexpr (SHARED) {
             const int r = row0 + rr, i = r / p.group;
-            const long long to = partial_at(p, piece.split, range.first + i, head * p.group + (r - i * p.group));
+            const long long to = partial_at(p, piece.set, range.first + i, head * p.group + (r - i * p.group));
             if (stop > 0) *reinterpret_cast<f32x4*>(p.part + to * dim + 4 * d) = acc;
             if (d == 0) *reinterpret_cast<f32x2*>(p.stats + to * 2) = (f32x2){now, total};
             continue;
@@ -844,7 +854,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     float unit_of[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        place[n] = SHARED && p.front ? shared_place(p, head, row0 + (wave * NT + n) * 16 + col, rows_all)
+        place[n] = SHARED && piece.front ? shared_place(p, head, row0 + (wave * NT + n) * 16 + col, rows_all)
                                      : row_place(p, range, len, head, row0 + (wave * NT + n) * 16 + col, rows_all);
         elems[n].request(p, place[n], range.first, dim, grp);
     }
@@ -860,7 +870,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     const int pos_first = pos0 + wave_row / p.group, pos_last = pos0 + wave_last / p.group;
     int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0, all_hi = p.causal ? pos_first : len - 1;
     int any_lo = p.window > 0 ? pos_first - p.window + 1 : 0, any_hi = wave_row < rows_all ? p.causal ? pos_last : len - 1 : -1;
-    if (SHARED && p.front) {
+    if (SHARED && piece.front) {
         const SeenBy seen = seen_by(place);
         all_lo = seen.all_lo;
         all_hi = seen.all_hi;
@@ -1005,7 +1015,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
         const float total = sum_over_groups(l[n]);
         if (place[n].row < 0) continue;
         if constexpr (SHARED) {
-            const long long at = partial_at(p, piece.split, place[n].row, place[n].head);
+            const long long at = partial_at(p, piece.set, place[n].row, place[n].head);
 #pragma unroll
             for (int i = 0; i < VALUES; ++i)
                 if (begin < end && (FULL || i * 16 < dim)) *reinterpret_cast<f32x4*>(p.part + at * dim + i * 16 + grp * 4) = o[n][i] * scales.unit;
@@ -1061,7 +1071,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendParams p, 
     if (p.lse && threadIdx.x == 0) p.lse[place.row * p.q_heads + place.head] = log_sum(ref, total);
 }
 
-// Rows of sequences that share their first tokens, joined of `sets` partial results: a wave per row and head.
+// Rows of sequences that share their first tokens, joined of up to 64 partial results: a wave per row and head.  Lane k has the k-th
+// result's reference and sum of weights; half a wave adds every other one's sums, four elements a lane.
 template <int TYPE>
 __global__ __launch_bounds__(256) void attend_shared_join_kernel(const AttendParams p, int sets) {
     const long long rows = static_cast<long long>(p.ragged.rows) * p.q_heads;
@@ -1069,33 +1080,34 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(const AttendPar
     if (at >= rows) return;
     const int lane = threadIdx.x & 63, row = static_cast<int>(at / p.q_heads), head = static_cast<int>(at - static_cast<long long>(row) * p.q_heads);
     const int dim = p.cache.dim;
+    f32x2 mine = reinterpret_cast<const f32x2*>(p.stats)[(lane < sets ? lane : 0) * rows + at];
     // the rows of no sequence are left as they are
     const int seq = __builtin_amdgcn_readfirstlane(seq_of_row(p, row));
     if (seq < 0) return;
     const RowRange range = p.ragged.range(seq, p.cache.length(seq));
     if (row < range.first || row - range.first >= range.count) return;
-    const f32x2* stats = reinterpret_cast<const f32x2*>(p.stats);
-    float ref = kNoRef;
-    for (int k = lane; k < sets; k += 64) ref = fmaxf(ref, stats[k * rows + at][0]);
+    if (lane >= sets) mine = (f32x2){kNoRef, 0.f};
+    float ref = mine[0];
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) ref = fmaxf(ref, __shfl_xor(ref, d));
-    // half a wave adds every other set
+    const Factor f(mine[0] - ref);
+    float total = f.of(mine[1]);
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) total += __shfl_xor(total, d);
+    // (a result without weight may have no sums)
+    const float by = mine[1] != 0.f ? f.whole() : -1.f, inverse = total == 0.f ? 0.f : 1.f / total;
     const int half = lane >> 5;
-    float total = 0.f;
     for (int d0 = 0; d0 < dim; d0 += 128) {
         const int d = d0 + (lane & 31) * 4;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        float sum = 0.f;
+#pragma unroll 4
         for (int k = half; k < sets; k += 2) {
-            const f32x2 st = stats[k * rows + at];
-            const Factor f(st[0] - ref);
-            sum += f.of(st[1]);
-            if (st[1] != 0.f && d < dim) acc += *reinterpret_cast<const f32x4*>(p.part + (k * rows + at) * dim + d) * f.whole();
+            const float w = __shfl(by, k);
+            if (w >= 0.f && d < dim) acc += *reinterpret_cast<const f32x4*>(p.part + (k * rows + at) * dim + d) * w;
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], 32);
-        total = sum + __shfl_xor(sum, 32);
-        if (half == 0 && d < dim) store_row4<TYPE>(p.out, row * p.out.row_stride + head * p.out.head_stride + d, acc * (total == 0.f ? 0.f : 1.f / total));
+        if (half == 0 && d < dim) store_row4<TYPE>(p.out, row * p.out.row_stride + head * p.out.head_stride + d, acc * inverse);
     }
     if (p.lse && lane == 0) p.lse[at] = log_sum(ref, total);
 }

@@ -25,10 +25,10 @@ hipError_t launch_attend_f32(int fmt, bool tiles, int nt, int waves, const Atten
 hipError_t launch_attend_bf16(int fmt, bool tiles, int nt, int waves, const AttendParams& p, hipStream_t s);
 hipError_t launch_attend_f16(int fmt, bool tiles, int nt, int waves, const AttendParams& p, hipStream_t s);
 
-// Pieces of the shared tokens or of the sequences' own ones (p.front), and the results joined of `sets` partial ones.
-hipError_t launch_attend_shared_f32(int fmt, bool tiles, int nt, const AttendParams& p, hipStream_t s);
-hipError_t launch_attend_shared_bf16(int fmt, bool tiles, int nt, const AttendParams& p, hipStream_t s);
-hipError_t launch_attend_shared_f16(int fmt, bool tiles, int nt, const AttendParams& p, hipStream_t s);
+// `groups` workgroups with pieces of the shared tokens and of the sequences' own ones, and the results joined of `sets` partial ones.
+hipError_t launch_attend_shared_f32(int fmt, bool tiles, int nt, long long groups, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_shared_bf16(int fmt, bool tiles, int nt, long long groups, const AttendParams& p, hipStream_t s);
+hipError_t launch_attend_shared_f16(int fmt, bool tiles, int nt, long long groups, const AttendParams& p, hipStream_t s);
 hipError_t launch_shared_join_f32(int sets, AttendParams p, hipStream_t s);
 hipError_t launch_shared_join_bf16(int sets, AttendParams p, hipStream_t s);
 hipError_t launch_shared_join_f16(int sets, AttendParams p, hipStream_t s);

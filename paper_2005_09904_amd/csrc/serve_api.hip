@@ -165,17 +165,20 @@ SharedPlan shared_plan(const biq_attention_shared_args& args) {
     const biq_cache& c = a.cache;
     const int group = a.q_heads / c.heads, ch = chunks_of(c.head_dim) - 1;
     SharedPlan pl{};
-    // The shared tokens: all rows of the call over the same steps, in pieces so that there is a workgroup for every CU.
+    // The shared tokens: all rows of the call over the same steps, in pieces so that there is a workgroup for every place of a CU (two for the
+    // kernel for many rows with heads up to 128).
     const long long rows = static_cast<long long>(a.ragged.rows) * group, steps = (args.shared + 63) / 64;
     const int few = rows <= 16 || ch > 1 ? 16 : 32, many = ch <= 1 ? 128 : 64;
+    auto pieces = [](long long units, long long places, long long steps, long long least, long long most) {
+        long long n = units >= places ? 1 : places / units;
+        n = n > (steps + least - 1) / least ? (steps + least - 1) / least : n;
+        return static_cast<int>(n > most ? most : n);
+    };
     pl.front.tiles = rows > 4 * few;
     pl.front.nt = few / 16;
     const int tile = pl.front.tiles ? many : few;
     pl.front.row_tiles = (rows + tile - 1) / tile;
-    const long long units = pl.front.row_tiles * c.heads;
-    long long splits = units >= kCus ? 1 : kCus / units;
-    splits = splits > (steps + 3) / 4 ? (steps + 3) / 4 : splits;
-    pl.front.splits = static_cast<int>(splits > 32 ? 32 : splits);
+    pl.front.splits = pieces(pl.front.row_tiles * c.heads, pl.front.tiles && ch <= 1 ? 2 * kCus : kCus, steps, pl.front.tiles ? 8 : 4, 32);
     // The own tokens.
     const long long own_rows = static_cast<long long>(a.ragged.max_rows) * group, room = static_cast<long long>(c.table_stride) * c.page_tokens;
     long long span = (a.max_len > 0 && a.max_len < room ? a.max_len : room) - args.shared;
@@ -186,12 +189,8 @@ SharedPlan shared_plan(const biq_attention_shared_args& args) {
     pl.back.nt = own_few / 16;
     const int own_tile = pl.back.tiles ? many : own_few;
     pl.back.row_tiles = (own_rows + own_tile - 1) / own_tile;
-    const long long own_units = pl.back.row_tiles * c.heads * c.seqs;
-    splits = own_units >= kCus ? 1 : kCus / own_units;
-    splits = splits > (own_steps + 3) / 4 ? (own_steps + 3) / 4 : splits;
-    splits = splits > 16 ? 16 : splits;
-    pl.back.splits = static_cast<int>(splits);
-    pl.back.split_steps = static_cast<int>((own_steps + splits - 1) / splits);
+    pl.back.splits = pieces(pl.back.row_tiles * c.heads * c.seqs, !pl.back.tiles && (ch + 1) * pl.back.nt <= 2 ? 2 * kCus : kCus, own_steps, pl.back.tiles ? 8 : 4, 16);
+    pl.back.split_steps = static_cast<int>((own_steps + pl.back.splits - 1) / pl.back.splits);
     pl.workspace = static_cast<size_t>(pl.front.splits + pl.back.splits) * a.ragged.rows * a.q_heads * (c.head_dim + 2) * 4;
     return pl;
 }
@@ -349,24 +348,30 @@ biq_status biq_attention_shared(const biq_attention_shared_args* args, void* wor
     const SharedPlan pl = shared_plan(*args);
     if (pl.workspace > workspace_bytes) return BIQ_EWORKSPACE;
     if (!workspace || !aligned(workspace, 16)) return BIQ_EINVAL;
-    if (static_cast<long long>(a->cache.seqs) * a->cache.heads * pl.back.row_tiles * pl.back.splits > kMaxInt) return BIQ_EUNSUPPORTED;
+    if (a->cache.heads * (pl.front.row_tiles * pl.front.splits + pl.back.row_tiles * pl.back.splits * a->cache.seqs) > kMaxInt) return BIQ_EUNSUPPORTED;
     AttendParams p = attend_params(a);
     const int sets = pl.front.splits + pl.back.splits;
     p.part = static_cast<float*>(workspace);
     p.stats = p.part + static_cast<size_t>(sets) * a->ragged.rows * a->q_heads * a->cache.head_dim;
     p.shared = args->shared;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    for (const bool front : {true, false}) {
-        const SharedPart& part = front ? pl.front : pl.back;
-        p.front = front;
-        p.row_tiles = static_cast<int>(part.row_tiles);
-        p.splits = part.splits;
-        p.split_steps = part.split_steps;
-        p.set = front ? 0 : pl.front.splits;
-        const hipError_t e = a->type == BIQ_F32    ? launch_attend_shared_f32(a->cache.format, part.tiles, part.nt, p, s)
-                             : a->type == BIQ_BF16 ? launch_attend_shared_bf16(a->cache.format, part.tiles, part.nt, p, s)
-                                                   : launch_attend_shared_f16(a->cache.format, part.tiles, part.nt, p, s);
-        if (e != hipSuccess) return BIQ_EHIP;
+    long long groups[2];
+    for (int i = 0; i < 2; ++i) {
+        const SharedPart& part = i == 0 ? pl.front : pl.back;
+        p.map[i] = {static_cast<int>(part.row_tiles), part.splits, part.split_steps, i == 0 ? 0 : pl.front.splits};
+        groups[i] = part.row_tiles * part.splits * a->cache.heads * (i == 0 ? 1 : a->cache.seqs);
+    }
+    auto launch = [&](const SharedPart& part, long long front_groups, long long all) {
+        p.front_groups = static_cast<int>(front_groups);
+        return a->type == BIQ_F32    ? launch_attend_shared_f32(a->cache.format, part.tiles, part.nt, all, p, s)
+               : a->type == BIQ_BF16 ? launch_attend_shared_bf16(a->cache.format, part.tiles, part.nt, all, p, s)
+                                     : launch_attend_shared_f16(a->cache.format, part.tiles, part.nt, all, p, s);
+    };
+    // one launch where both have the same kernel
+    if (pl.front.tiles == pl.back.tiles && (pl.front.tiles || pl.front.nt == pl.back.nt)) {
+        if (launch(pl.front, groups[0], groups[0] + groups[1]) != hipSuccess) return BIQ_EHIP;
+    } else {
+        if (launch(pl.front, groups[0], groups[0]) != hipSuccess || launch(pl.back, 0, groups[1]) != hipSuccess) return BIQ_EHIP;
     }
     return status(a->type == BIQ_F32    ? launch_shared_join_f32(sets, p, s)
                   : a->type == BIQ_BF16 ? launch_shared_join_bf16(sets, p, s)
