@@ -229,6 +229,12 @@ __device__ __forceinline__ RowPlace shared_place(const AttendParams& p, int head
     return place;
 }
 
+// The row alone, which no load tells: its elements can be requested before it is known whether it is one.
+__device__ __forceinline__ RowPlace shared_row(const AttendParams& p, int head, int rr, int rows_all) {
+    const int r = rr / p.group;
+    return {rr < rows_all ? r : -1, head * p.group + (rr - r * p.group), 0, -1};
+}
+
 // What all rows of a wave's tiles see and what some of them do, by exchange between the lanes that hold them.
 struct SeenBy { int all_lo, all_hi, any_lo, any_hi; };
 template <int NT>
@@ -612,7 +618,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     RowElems<TYPE, CH, false> elems[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        place[n] = SHARED && piece.front ? shared_place(p, head, row0 + n * 16 + col, rows_all) : row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
+        place[n] = SHARED && piece.front ? shared_row(p, head, row0 + n * 16 + col, rows_all) : row_place(p, range, len, head, row0 + n * 16 + col, rows_all);
         elems[n].request(p, place[n], range.first, dim, grp);
     }
     u32x4 kc[4][CH];                                            // token 4 t + col % 4 of that block
@@ -639,6 +645,10 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
     };
     int t0 = begin + __builtin_amdgcn_readfirstlane(wave) * 64;
     if (t0 < end) request_keys(t0);
+    if (SHARED && piece.front) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) place[n] = shared_place(p, head, row0 + n * 16 + col, rows_all);
+    }
 
     f16x8 q[NT][CH][2][QT];
     float unit_of[NT];
@@ -854,28 +864,9 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
     float unit_of[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        place[n] = SHARED && piece.front ? shared_place(p, head, row0 + (wave * NT + n) * 16 + col, rows_all)
+        place[n] = SHARED && piece.front ? shared_row(p, head, row0 + (wave * NT + n) * 16 + col, rows_all)
                                      : row_place(p, range, len, head, row0 + (wave * NT + n) * 16 + col, rows_all);
         elems[n].request(p, place[n], range.first, dim, grp);
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        float x[CH][2][8];
-        elems[n].get(place[n], dim, grp, x);
-        unit_of[n] = row_terms<TYPE, CH>(p.negative, x, q[n]) * p.scale;
-    }
-    // what all and what some of them see
-    const int wave_row = row0 + wave * NT * 16;
-    const int wave_last = wave_row + NT * 16 < rows_all ? wave_row + NT * 16 - 1 : rows_all - 1;
-    const int pos_first = pos0 + wave_row / p.group, pos_last = pos0 + wave_last / p.group;
-    int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0, all_hi = p.causal ? pos_first : len - 1;
-    int any_lo = p.window > 0 ? pos_first - p.window + 1 : 0, any_hi = wave_row < rows_all ? p.causal ? pos_last : len - 1 : -1;
-    if (SHARED && piece.front) {
-        const SeenBy seen = seen_by(place);
-        all_lo = seen.all_lo;
-        all_hi = seen.all_hi;
-        any_lo = seen.any_lo;
-        any_hi = seen.any_hi;
     }
 
     // this wave's part of a stage: of step wave / 4 the key rows of tile wave % 4 and the values of CH tiles of 16 elements
@@ -912,6 +903,34 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
             }
         }
     };
+    if constexpr (SHARED) {
+        // pieces may be short: their first tokens are requested before anything is waited for
+        if (begin < end) request(begin);
+        if (piece.front) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) place[n] = shared_place(p, head, row0 + (wave * NT + n) * 16 + col, rows_all);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float x[CH][2][8];
+        elems[n].get(place[n], dim, grp, x);
+        unit_of[n] = row_terms<TYPE, CH>(p.negative, x, q[n]) * p.scale;
+    }
+    // what all and what some of them see
+    const int wave_row = row0 + wave * NT * 16;
+    const int wave_last = wave_row + NT * 16 < rows_all ? wave_row + NT * 16 - 1 : rows_all - 1;
+    const int pos_first = pos0 + wave_row / p.group, pos_last = pos0 + wave_last / p.group;
+    int all_lo = p.window > 0 ? pos_last - p.window + 1 : 0, all_hi = p.causal ? pos_first : len - 1;
+    int any_lo = p.window > 0 ? pos_first - p.window + 1 : 0, any_hi = wave_row < rows_all ? p.causal ? pos_last : len - 1 : -1;
+    if (SHARED && piece.front) {
+        const SeenBy seen = seen_by(place);
+        all_lo = seen.all_lo;
+        all_hi = seen.all_hi;
+        any_lo = seen.any_lo;
+        any_hi = seen.any_hi;
+    }
+
     auto lay_down = [&](f16x8* to) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
@@ -945,7 +964,7 @@ __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kerne
         for (int i = 0; i < STEPS; ++i) scales.see(vs[i], valid[i], l);
     };
     if (begin < end) {
-        request(begin);
+        if constexpr (!SHARED) request(begin);
         lay_down(buffers);
         __syncthreads();
         see_scales();

@@ -178,7 +178,7 @@ SharedPlan shared_plan(const biq_attention_shared_args& args) {
     pl.front.nt = few / 16;
     const int tile = pl.front.tiles ? many : few;
     pl.front.row_tiles = (rows + tile - 1) / tile;
-    pl.front.splits = pieces(pl.front.row_tiles * c.heads, pl.front.tiles && ch <= 1 ? 2 * kCus : kCus, steps, pl.front.tiles ? 8 : 4, 32);
+    pl.front.splits = pieces(pl.front.row_tiles * c.heads, pl.front.tiles && ch <= 1 ? 2 * kCus : kCus, steps, 4, 32);
     // The own tokens.
     const long long own_rows = static_cast<long long>(a.ragged.max_rows) * group, room = static_cast<long long>(c.table_stride) * c.page_tokens;
     long long span = (a.max_len > 0 && a.max_len < room ? a.max_len : room) - args.shared;
