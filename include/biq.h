@@ -644,7 +644,7 @@ biq_status biq_gemm4(const biq_gemm4_args* args, void* workspace, size_t workspa
  *      prompt's; drafts int32 [seqs][rows - 1] (NULL: none): the first i of a sequence's have been said before its row i.
  *      If v is among them: z > 0 ? z / repetition[s] : z * repetition[s].  If v was said c > 0 times other than in the prompt:
  *      z - c frequency[s] - presence[s].  Each of the three NULL: left out.  Tokens outside [0, vocab) count nowhere.
- *   2. biases: of the bias_tokens [seqs][biases] that are v the bias_values are added, in the list's order.
+ *   2. biases: of the bias_tokens [seqs][biases] that are v the bias_values are summed in the list's order and added.
  *   3. temperature[s] (NULL: 1): z * (1 / temperature).  One that is not above 2^-100 leaves z; none counts as more than 2^100.
  *   4. mask: bit v % 32 of the 32-bit word v / 32 of a row is 0: z = -infinity, whatever it was.
  * out: z, or with `probabilities` exp(z) / sum exp(z) over the row (temperature not above 2^-100: 1 at the largest z, the first of

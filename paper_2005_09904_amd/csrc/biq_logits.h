@@ -159,14 +159,14 @@ __device__ __forceinline__ Best best_of_wave(Best b) {
     return b;
 }
 
-// What a row comes to: probabilities are exp2((z - top) scale) each, or for greedy sequences 1 at place `at`.  A NaN among the
+// What a row comes to: probabilities are exp2(z - top) each, or for greedy sequences 1 at place `at`.  A NaN among the
 // exponentials is one in their sum, and so comes to all of them.
 struct RowSum {
     float top, sum;
     int at;
 };
 // Of n pairs (largest logit, and the sum of exponentials or its place), all threads of a wave for all of them; `mine` is pair `lane`.
-__device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n, bool greedy, float scale) {
+__device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n, bool greedy) {
     const int lane = threadIdx.x & 63;
     RowSum r = {-INFINITY, 0.f, -1};
     if (greedy) {
@@ -181,7 +181,7 @@ __device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n,
     if (lane < n) r.top = mine[0];
     for (int i = lane + 64; i < n; i += 64) r.top = fmaxf(r.top, pairs[i][0]);
     r.top = largest_of_wave(r.top);
-    auto part = [&](f32x2 x) { return x[0] == -INFINITY ? x[1] : x[1] * __builtin_amdgcn_exp2f((x[0] - r.top) * scale); };
+    auto part = [&](f32x2 x) { return x[0] == -INFINITY ? x[1] : x[1] * __builtin_amdgcn_exp2f(x[0] - r.top); };
     if (lane < n) r.sum = part(mine);
     for (int i = lane + 64; i < n; i += 64) r.sum += part(pairs[i]);
     r.sum = sum_of_wave(r.sum);
@@ -225,12 +225,13 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
     const int* drafts = p.drafts + static_cast<long long>(seq) * (p.rows - 1);
     int draft = p.drafts && lane < p.rows - 1 ? drafts[lane] : -1;      // of the row after lane `lane` (of the 64 that it is among)
     if (counting || biases) count_tokens<THREADS, SPAN>(p, seq, t0, counts, biases);
-    const float scale = k.heat * 1.4426950408889634f, inverse = 1.f / k.repetition;
-
-    // z becomes z by - less: by is 1 or that of a token said before, less its penalties without its biases
-    auto less_of = [&](uint32_t c) {
+    // Logits times the temperature's reciprocal, for exponentials (but for greedy sequences) times log2 e too.  z becomes z by - less: by is that
+    // factor, for a token said before with its repetition's, less its penalties without its biases.
+    const float scale = WHAT == 0 || k.greedy ? k.heat : k.heat * 1.4426950408889634f;
+    const float again = k.repetition * scale, inverse = 1.f / k.repetition * scale;
+    auto less_of = [&](uint32_t c, float bias) {
         const uint32_t said = c & ~kInPrompt;
-        return said ? __builtin_fmaf(static_cast<float>(said), k.frequency, k.presence) : 0.f;
+        return ((said ? __builtin_fmaf(static_cast<float>(said), k.frequency, k.presence) : 0.f) - bias) * scale;
     };
     float less[U][8];
     bool seen[U][8];
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
         for (int i = 0; i < 8; ++i) {
             const uint32_t c = counting ? counts[at + i] : 0;
             seen[u][i] = c != 0;
-            less[u][i] = less_of(c) - (biases ? biases[at + i] : 0.f);
+            less[u][i] = less_of(c, biases ? biases[at + i] : 0.f);
         }
     };
     if (EARLY) {
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
                     for (int i = 0; i < 8; ++i)
                         if (mine == me && static_cast<int>(at) == (u * THREADS + mine) * 8 + i) {
                             seen[u][i] = true;
-                            less[u][i] = less_of(counts[at]) - (biases ? biases[at] : 0.f);
+                            less[u][i] = less_of(counts[at], biases ? biases[at] : 0.f);
                         }
             }
         }
@@ -287,13 +288,12 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
                 if (!EARLY) look_up(u);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float by = z[u][i] > 0.f ? inverse : k.repetition;
-                    z[u][i] = __builtin_fmaf(z[u][i], seen[u][i] ? by : 1.f, -less[u][i]);
+                    const float by = z[u][i] > 0.f ? inverse : again;
+                    z[u][i] = __builtin_fmaf(z[u][i], seen[u][i] ? by : scale, -less[u][i]);
                 }
-            }
-            if (WHAT == 0) {
+            } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z[u][i] *= k.heat;
+                for (int i = 0; i < 8; ++i) z[u][i] *= scale;
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        z[u][i] = __builtin_amdgcn_exp2f((z[u][i] - from) * scale);
+                        z[u][i] = __builtin_amdgcn_exp2f(z[u][i] - from);
                         all += z[u][i];
                     }
                 mine = (f32x2){top, sum_of_wave(all)};
@@ -337,22 +337,22 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
             if (lane == 0) mine_at[wave] = mine;
             __syncthreads();
             if (WHAT == 1 && wave > 0) continue;
-            sum = row_sum(mine_at[lane < WAVES ? lane : 0], mine_at, WAVES, k.greedy, scale);
+            sum = row_sum(mine_at[lane < WAVES ? lane : 0], mine_at, WAVES, k.greedy);
             if (WHAT == 1) {
                 if (lane == 0) p.stats[r * p.spans + span] = (f32x2){sum.top, k.greedy ? __int_as_float(sum.at) : sum.sum};
                 continue;
             }
-            by = sum.sum == 0.f ? 0.f : (mine[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mine[0] - sum.top) * scale)) / sum.sum;
+            by = sum.sum == 0.f ? 0.f : (mine[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mine[0] - sum.top)) / sum.sum;
         }
         if constexpr (WHAT == 2) {
-            sum = row_sum(my_pair, p.stats + r * p.spans, p.spans, k.greedy, scale);
+            sum = row_sum(my_pair, p.stats + r * p.spans, p.spans, k.greedy);
             by = sum.sum == 0.f ? 0.f : 1.f / sum.sum;
             const float from = sum.top == -INFINITY ? 0.f : sum.top;
             if (!k.greedy) {
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) z[u][i] = __builtin_amdgcn_exp2f((z[u][i] - from) * scale);
+                    for (int i = 0; i < 8; ++i) z[u][i] = __builtin_amdgcn_exp2f(z[u][i] - from);
             }
         }
 #pragma unroll
