@@ -32,13 +32,6 @@ struct LogitsParams {
 
 constexpr uint32_t kInPrompt = 0x80000000u;          // beside the count of a token: it is among the prompt's
 
-// The largest logit and its lowest place; a NaN is larger than all.
-struct Best { float z; int at; };
-__device__ __forceinline__ Best better(Best a, Best b) {
-    if (a.z != a.z || b.z != b.z) return a.z != a.z ? a : b;
-    return b.z > a.z || (b.z == a.z && b.at < a.at) ? b : a;
-}
-
 // What happens to a sequence's logits, but for what LDS holds.
 struct Penalties {
     float repetition, presence, frequency, heat;                // heat: 1 / temperature
@@ -151,14 +144,30 @@ __device__ __forceinline__ float over_wave(float x, float none, const Join& join
     x = moved<0x143, 0xc>(x, none, join);                       // row_bcast:31 to rows 2 and 3
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
-__device__ __forceinline__ float largest_of_wave(float x) { return over_wave(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ __forceinline__ float sum_of_wave(float x) { return over_wave(x, 0.f, [](float a, float b) { return a + b; }); }
-__device__ __forceinline__ Best best_of_wave(Best b) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) b = better(b, Best{__shfl_xor(b.z, d), __shfl_xor(b.at, d)});
-    return b;
+// (lanes without another keep their own)
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(x, x, CONTROL, ROWS, 0xf, false); }
+template <typename T, typename Join>
+__device__ __forceinline__ T best_of_wave(T x, const Join& join) {
+    x = join(x, from_lane<0x111, 0xf>(x));
+    x = join(x, from_lane<0x112, 0xf>(x));
+    x = join(x, from_lane<0x114, 0xf>(x));
+    x = join(x, from_lane<0x118, 0xf>(x));
+    x = join(x, from_lane<0x142, 0xa>(x));
+    x = join(x, from_lane<0x143, 0xc>(x));
+    return __builtin_amdgcn_readlane(x, 63);
 }
-
+// A float's order as an integer's: of negative ones the lower bits are turned over.
+__device__ __forceinline__ int ordered(float x) {
+    const int i = __float_as_int(x);
+    return i ^ ((i >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float largest_of_wave(float x) {
+    const int i = best_of_wave(ordered(x), [](int a, int b) { return a > b ? a : b; });
+    return __int_as_float(i ^ ((i >> 31) & 0x7fffffff));
+}
+__device__ __forceinline__ int lowest_of_wave(int x) { return best_of_wave(x, [](int a, int b) { return a < b ? a : b; }); }
+__device__ __forceinline__ float sum_of_wave(float x) { return over_wave(x, 0.f, [](float a, float b) { return a + b; }); }
 // What a row comes to: probabilities are exp2(z - top) each, or for greedy sequences 1 at place `at`.  A NaN among the
 // exponentials is one in their sum, and so comes to all of them.
 struct RowSum {
@@ -170,12 +179,19 @@ __device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n,
     const int lane = threadIdx.x & 63;
     RowSum r = {-INFINITY, 0.f, -1};
     if (greedy) {
-        Best best = {-INFINITY, 0x7fffffff};
-        if (lane < n) best = Best{mine[0], __float_as_int(mine[1])};
-        for (int i = lane + 64; i < n; i += 64) best = better(best, Best{pairs[i][0], __float_as_int(pairs[i][1])});
-        best = best_of_wave(best);
-        r.top = best.z;
-        r.at = best.z == -INFINITY ? -1 : best.at;
+        // (a NaN among the largest: one is the row's)
+        bool bad = lane < n && mine[0] != mine[0];
+        if (lane < n) r.top = mine[0];
+        for (int i = lane + 64; i < n; i += 64) {
+            bad |= pairs[i][0] != pairs[i][0];
+            r.top = fmaxf(r.top, pairs[i][0]);
+        }
+        r.top = largest_of_wave(r.top);
+        r.at = lane < n && mine[0] == r.top ? __float_as_int(mine[1]) : 0x7fffffff;
+        for (int i = lane + 64; i < n; i += 64)
+            if (pairs[i][0] == r.top && __float_as_int(pairs[i][1]) < r.at) r.at = __float_as_int(pairs[i][1]);
+        r.at = r.top == -INFINITY ? -1 : lowest_of_wave(r.at);
+        if (__any(bad)) r.top = __uint_as_float(0x7fc00000u);
         return r;
     }
     if (lane < n) r.top = mine[0];
@@ -307,22 +323,27 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
         float by = 0.f;                                         // makes probabilities of z's exponentials
         if constexpr (WHAT == 1 || WHAT == 3) {
             f32x2 mine;
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, z[u][i]);
+            top = largest_of_wave(top);
             if (k.greedy) {
-                Best best = {-INFINITY, U * 8};
+                // the lowest place with the largest logit, among this thread's (constants) and the wave's
+                int at = U * 8;
+                bool bad = false;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (int u = U - 1; u >= 0; --u)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) best = better(best, Best{z[u][i], u * 8 + i});     // (this thread's places: constants)
-                best.at = t0 + ((best.at >> 3) * THREADS + me) * 8 + (best.at & 7);
-                best = best_of_wave(best);
-                mine = (f32x2){best.z, __int_as_float(best.at)};
+                    for (int i = 7; i >= 0; --i) {
+                        at = z[u][i] == top ? u * 8 + i : at;
+                        bad |= z[u][i] != z[u][i];
+                    }
+                at = at == U * 8 ? 0x7fffffff : t0 + ((at >> 3) * THREADS + me) * 8 + (at & 7);
+                mine = (f32x2){__any(bad) ? __uint_as_float(0x7fc00000u) : top, __int_as_float(lowest_of_wave(at))};
             } else {
-                float top = -INFINITY, all = 0.f;
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, z[u][i]);
-                top = largest_of_wave(top);
+                float all = 0.f;
                 const float from = top == -INFINITY ? 0.f : top;        // (all -infinity: sum 0, but for a NaN)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
