@@ -72,8 +72,11 @@ Gemm4Plan gemm4_plan(const biq_gemm4_args& a) {
     return pl;
 }
 
-// Rows that a workgroup holds: 1024 threads with 32 tokens each, whose counts and biases take 4 bytes of LDS each.
-bool logits_whole(int vocab, bool biases) { return vocab <= (biases ? 16384 : 32768); }
+// Whether workgroups hold whole rows (1024 threads with up to 32 tokens each, whose counts and biases take 4 bytes of LDS each) in one launch,
+// or spans in two.  Up to 16384 tokens a workgroup is quicker: one row of 8000 6.6 us instead of 9.6, of 16000 9.2 and 10.0 with
+// the second launch's own time not counted.  Beyond, one row of 32000 takes 13.1 us and 10.4, so that it is left to spans until the
+// sequences fill half of the CUs (256 of them: 22.7 and 36.6; 64 with four rows each 44.8 and 27).
+bool logits_whole(int vocab, bool biases, int seqs) { return vocab <= 16384 || (vocab <= 32768 && !biases && seqs >= 128); }
 
 }  // namespace
 }  // namespace biq
@@ -199,7 +202,7 @@ biq_status biq_gemm4(const biq_gemm4_args* a, void* workspace, size_t workspace_
 size_t biq_logits_workspace_bytes(int seqs, int rows, int vocab) {
     if (seqs < 1 || rows < 1 || vocab < 1 || vocab > (1 << 22) || static_cast<long long>(seqs) * rows > kMaxInt) return 0;
     const size_t spans = (vocab + kLogitsSpan - 1) / kLogitsSpan;
-    return logits_whole(vocab, true) ? 0 : static_cast<size_t>(seqs) * rows * spans * 8;
+    return logits_whole(vocab, true, seqs) ? 0 : static_cast<size_t>(seqs) * rows * spans * 8;
 }
 
 biq_status biq_logits(const biq_logits_args* a, void* workspace, size_t workspace_bytes, void* stream) {
@@ -217,7 +220,7 @@ biq_status biq_logits(const biq_logits_args* a, void* workspace, size_t workspac
     if (!write_ok(a->out_stride, a->rows, a->vocab) || !write_ok(a->out_seq_stride, a->seqs, a->vocab)) return BIQ_EINVAL;
     if (a->x == a->out && (a->type != a->out_type || a->x_seq_stride != a->out_seq_stride || a->x_stride != a->out_stride)) return BIQ_EINVAL;
     if (a->vocab > (1 << 22) || a->biases > 4096 || static_cast<long long>(a->seqs) * a->rows > kMaxInt) return BIQ_EUNSUPPORTED;
-    const bool whole = logits_whole(a->vocab, a->biases > 0);
+    const bool whole = logits_whole(a->vocab, a->biases > 0, a->seqs);
     const size_t need = a->probabilities ? biq_logits_workspace_bytes(a->seqs, a->rows, a->vocab) : 0;
     if (need > workspace_bytes) return BIQ_EWORKSPACE;
     if (need && (!workspace || !aligned(workspace, 16))) return BIQ_EINVAL;

@@ -78,7 +78,7 @@ def check(x, h, got, out_type, probabilities):
 
 @pytest.mark.parametrize("typ,out_type", [("fp32", "fp32"), ("bf16", "fp32"), ("fp16", "fp16"), ("bf16", "bf16")])
 @pytest.mark.parametrize("seqs,rows,vocab", [(1, 1, 1), (2, 3, 5), (3, 1, 31), (2, 2, 33), (4, 3, 1000), (3, 4, 4095), (3, 2, 4096), (3, 2, 4097), (5, 3, 9001),
-                                             (1, 1, 32000), (1, 2, 70001)])
+                                             (1, 1, 32000), (1, 2, 70001), (130, 2, 17000)])
 @pytest.mark.parametrize("probabilities", [False, True])
 def test_all_together(biq, typ, out_type, seqs, rows, vocab, probabilities):
     x, h = inputs(seqs, rows, vocab, typ, seqs + vocab)
