@@ -166,26 +166,30 @@ SharedPlan shared_plan(const biq_attention_shared_args& args) {
     const int group = a.q_heads / c.heads, ch = chunks_of(c.head_dim) - 1;
     SharedPlan pl{};
     // The shared tokens: all rows of the call over the same steps, in pieces so that there is a workgroup for every place of a CU (two for the
-    // kernel for many rows with heads up to 128).
+    // kernel for many rows with heads up to 128).  One launch for both parts saves one part's start and end, a chain of loads of 9 us, and
+    // needs the same tiles: of 16 rows where the own rows are few.  That pays until the twice as many tiles cost as much: 32
+    // sequences of 4 rows and 8 heads behind 8192 tokens 25.1 us instead of 29.8, behind 16384 36.9 instead of 39.2, behind 32768 more.
     const long long rows = static_cast<long long>(a.ragged.rows) * group, steps = (args.shared + 63) / 64;
-    const int few = rows <= 16 || ch > 1 ? 16 : 32, many = ch <= 1 ? 128 : 64;
+    const long long own_rows = static_cast<long long>(a.ragged.max_rows) * group;
+    const bool joint = own_rows <= 16 && rows <= 128 && c.heads * ((rows + 31) / 32) * steps <= 40 * kCus;
+    const int few = rows <= 16 || ch > 1 || joint ? 16 : 32, many = ch <= 1 ? 128 : 64;
     auto pieces = [](long long units, long long places, long long steps, long long least, long long most) {
         long long n = units >= places ? 1 : places / units;
         n = n > (steps + least - 1) / least ? (steps + least - 1) / least : n;
         return static_cast<int>(n > most ? most : n);
     };
-    pl.front.tiles = rows > 4 * few;
+    pl.front.tiles = rows > many;
     pl.front.nt = few / 16;
     const int tile = pl.front.tiles ? many : few;
     pl.front.row_tiles = (rows + tile - 1) / tile;
-    pl.front.splits = pieces(pl.front.row_tiles * c.heads, pl.front.tiles && ch <= 1 ? 2 * kCus : kCus, steps, 4, 32);
+    pl.front.splits = pieces(pl.front.row_tiles * c.heads, pl.front.tiles && ch <= 1 ? 2 * kCus : kCus, steps, pl.front.tiles ? 8 : 4, 32);
     // The own tokens.
-    const long long own_rows = static_cast<long long>(a.ragged.max_rows) * group, room = static_cast<long long>(c.table_stride) * c.page_tokens;
+    const long long room = static_cast<long long>(c.table_stride) * c.page_tokens;
     long long span = (a.max_len > 0 && a.max_len < room ? a.max_len : room) - args.shared;
     span = span < 64 ? 64 : span;
     const long long own_steps = (span + 63) / 64;
     const int own_few = own_rows <= 16 || ch > 1 ? 16 : 32;
-    pl.back.tiles = own_rows > 4 * own_few;
+    pl.back.tiles = own_rows > many;
     pl.back.nt = own_few / 16;
     const int own_tile = pl.back.tiles ? many : own_few;
     pl.back.row_tiles = (own_rows + own_tile - 1) / own_tile;
