@@ -519,7 +519,7 @@ biq_status biq_attention(const biq_attention_args* args, void* workspace, size_t
 /*
  * The same for a batch whose sequences begin with the same tokens (an instruction, a document): the first `shared` tokens of every
  * sequence are those of sequence 0, in the pages table[0][0 .. shared / page_tokens), which are read once for all rows of the call; the entries
- * of the other sequences for them are not looked at.  shared: a multiple of page_tokens, at least one page and at most
+ * of the other sequences for them are not looked at.  These pages hold `shared` tokens, whatever lens says.  shared: a multiple of page_tokens, at least one page and at most
  * table_stride * page_tokens (BIQ_EINVAL).  lens count the shared tokens; a sequence may also be shorter than them.  Everything
  * else, and what it costs in bits, is as with biq_attention; results differ from its in the order of additions.
  * workspace: biq_attention_shared_workspace_bytes(), 16-byte aligned (never 0).
@@ -580,8 +580,8 @@ biq_status biq_verify_drafts(const biq_verify_args* args, void* workspace, size_
  *   BIQ_CACHE_INT8: u = (largest |t| of the group) * (1 / 127 in 32 bits), codes rn(t * (1 / u)) in [-127, 127];
  *   BIQ_CACHE_FP8 : u = the least power of two that makes every |t| at most 448 u, codes t / u rounded to nearest (E4M3);
  * scale = u r.  Groups whose largest |t| is below 2^-100 are zeros with scale 0; with an infinity or a NaN: codes 0, scale NaN.
- * x, residual and sum have one type.  sum may be x or residual, y may be x (same data, type and stride); otherwise outputs overlap
- * nothing.  One of y and codes at least.  n <= 2^24 (BIQ_EUNSUPPORTED beyond).
+ * x, residual and sum have one type.  sum and y may be x or residual, but not the same one (same data, type and stride, or BIQ_EINVAL);
+ * otherwise outputs overlap nothing.  One of y and codes at least.  n <= 2^24 (BIQ_EUNSUPPORTED beyond).
  * Squares whose sum leaves the range of 32 bits are summed in 64.
  */
 typedef struct {

@@ -1120,9 +1120,10 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(const AttendPar
         const int d = d0 + (lane & 31) * 4;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int k = half; k < sets; k += 2) {
+        for (int k0 = 0; k0 < sets; k0 += 2) {                  // (all lanes to the end: a lane that has left has nothing to give)
+            const int k = k0 + half;
             const float w = __shfl(by, k);
-            if (w >= 0.f && d < dim) acc += *reinterpret_cast<const f32x4*>(p.part + (k * rows + at) * dim + d) * w;
+            if (k < sets && w >= 0.f && d < dim) acc += *reinterpret_cast<const f32x4*>(p.part + (k * rows + at) * dim + d) * w;
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], 32);

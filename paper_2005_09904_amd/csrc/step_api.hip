@@ -96,6 +96,12 @@ biq_status biq_norm(const biq_norm_args* a, void* stream) {
     if (!read_ok(a->x_stride) || (a->residual && !read_ok(a->residual_stride)) || (a->sum && !write_ok(a->sum_stride, a->rows, a->n)) ||
         (a->y && !write_ok(a->y_stride, a->rows, a->n)) || (a->codes && !write_ok(a->code_stride, a->rows, a->n)))
         return BIQ_EINVAL;
+    // a row is read before it is written, which only the same place of the same row may rely on
+    if (a->sum == a->x && a->sum_stride != a->x_stride) return BIQ_EINVAL;
+    if (a->sum && a->sum == a->residual && a->sum_stride != a->residual_stride) return BIQ_EINVAL;
+    if (a->y == a->x && (a->y_type != a->type || a->y_stride != a->x_stride)) return BIQ_EINVAL;
+    if (a->y && a->y == a->residual && (a->y_type != a->type || a->y_stride != a->residual_stride)) return BIQ_EINVAL;
+    if (a->y && a->y == a->sum) return BIQ_EINVAL;
     if (a->n > kMaxRow) return BIQ_EUNSUPPORTED;
     NormParams p{};
     p.x = a->x;

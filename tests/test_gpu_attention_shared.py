@@ -167,6 +167,14 @@ def test_long_prefix(biq, dim, typ, fmt):
     check(biq, pages, 6016, [40] * 4, au.rows_like([40] * 4, 8, dim, typ, 1), typ, uniform=True, max_len=6500, causal=False, window=444)
 
 
+@pytest.mark.parametrize("dim,own", [(64, 1), (64, 300), (160, 70)])
+def test_more_pieces_than_half_a_wave_has_lanes(biq, dim, own):
+    """32 pieces of the prefix and an odd or even number of others."""
+    pages = held(8192, (8192 + own, 8193), 1, dim, 256, "fp8")
+    for window in (0, 40):
+        check(biq, pages, 8192, [1, 1], au.rows_like([1, 1], 2, dim, "fp32", own), "fp32", uniform=True, max_len=8192 + own, window=window)
+
+
 @pytest.mark.parametrize("new", [1, 130])
 def test_what_is_hidden_does_not_show(biq, new):
     """NaN blocks outside a row's window and beyond a sequence's length; a page of the prefix that does not exist has no tokens."""

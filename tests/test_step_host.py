@@ -56,7 +56,7 @@ def at(descriptor):
 def norm(**change):
     from paper_2005_09904_amd import step
 
-    a = dict(x=A, residual=A, sum=A, weight=A, y=A, codes=A, scales=A, x_stride=64, residual_stride=64, sum_stride=64, y_stride=64, code_stride=64, type=0,
+    a = dict(x=A, residual=2 * A, sum=3 * A, weight=A, y=4 * A, codes=A, scales=A, x_stride=64, residual_stride=64, sum_stride=64, y_stride=64, code_stride=64, type=0,
              y_type=0, rows=3, n=64, group=32, format=0, eps=1e-6, weight_add=0.0)
     return step._NormArgs(**{**a, **change})
 
@@ -68,6 +68,8 @@ def test_norm_refuses(biq):
     for bad in (dict(x=None), dict(y=None, codes=None), dict(residual=None), dict(scales=None), dict(type=3), dict(type=-1), dict(y_type=3), dict(rows=0),
                 dict(n=0), dict(group=16), dict(group=-32), dict(group=256), dict(format=2), dict(eps=-1.0), dict(eps=nan), dict(eps=inf), dict(weight_add=nan),
                 dict(x=A + 2), dict(y=A + 2), dict(y=A + 1, y_type=1), dict(residual=A + 1), dict(sum=A + 3), dict(weight=A + 2), dict(scales=A + 1),
+                dict(y=A, y_type=1), dict(y=A, y_stride=65), dict(y=2 * A, y_stride=65), dict(y=2 * A, y_type=2), dict(y=3 * A), dict(sum=A, sum_stride=65),
+                dict(sum=2 * A, sum_stride=65),
                 dict(x_stride=-1), dict(residual_stride=-1), dict(sum_stride=63), dict(y_stride=0), dict(code_stride=63), dict(x_stride=(1 << 40) + 1)):
         assert lib.biq_norm(at(norm(**bad)), None) == EINVAL, bad
     big = (1 << 24) + 1
