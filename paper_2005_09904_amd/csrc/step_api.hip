@@ -10,7 +10,11 @@ namespace {
 constexpr long long kMaxInt = 0x7fffffff;
 constexpr long long kMaxStride = 1ll << 40;
 constexpr int kMaxRow = 1 << 24;                     // elements of a row
-constexpr int kLdsFew4 = 128 * 1024;                 // most that the operands of a few vectors take in LDS
+// Up to 16 vectors are `few` if their operands take this much of LDS at most, so that two workgroups share a CU; more of them, and those
+// of larger operands, are `many`.  32000 x 4096, bfloat16: 8 vectors (64 KB) 19.4 us and 16.7 + 4.7 for the join, in a launch of its
+// own, 10 vectors 26.8 and 16.5 + 4.7; 4096 x 4096: 8.4 and 6.7 + 3.0, 9.8 and 6.6 + 2.2; 16384 x 2048, 16 vectors (64 KB): 11.0 and 8.2 + 3.7;
+// 4096 x 16384, 3 vectors (96 KB): 16.8 and 13.0 + 3.9.
+constexpr int kLdsFew4 = 80 * 1024;
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool type_ok(int type) { return type == BIQ_F32 || type == BIQ_BF16 || type == BIQ_F16; }
