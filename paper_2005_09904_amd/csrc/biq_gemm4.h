@@ -384,7 +384,13 @@ __device__ __forceinline__ void store_y4(const Gemm4Params& p, int column, int r
 }
 
 // A few vectors: all of them as operands in LDS.  The WAVES waves of a workgroup take WAVES / splits tiles; waves of a tile
-// share its blocks and are joined through LDS.
+// share its blocks and are joined through LDS.  Splitting blocks over waves costs a round through LDS, and pays as long as the chip is not full
+// of waves: there are twice as many splits until tiles x splits fill 2048 waves.
+//
+// The weights bound large products: 32000 x 4096 with groups of 64 (70 MB) and one vector of bfloat16 16.7 us, 4.4 TB/s as the workgroups' start (X is
+// the operand that all of it waits for) is not covered by loads; 16384 x 4096 with five vectors of codes (35 MB) 11.4 us.  4096 x 4096 with one vector
+// takes 6.3 us, X, weights and join one after the other.  AHEAD records of weights are in flight: with 8 the head takes 23 us, with 2 17.4, with
+// the weights asked for before X becomes operands 19.7 (registers).
 template <int XT, int F, int G>
 __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Params p, int x_scales) {
     extern __shared__ float lds[];
@@ -410,10 +416,15 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
     if (tile < p.tiles && (lane & 15) < columns) store_y4(p, column0 + (lane & 15), tile * 16 + 4 * (lane >> 4), acc[0]);
 }
 
-// Many vectors (of 8 elements at least): a workgroup takes kRows4 rows, 32 a wave, up to 64 vectors and a share of the blocks.  X becomes operands on the way to LDS, two
-// blocks at a time, while the two before are multiplied; the weights go from memory to registers two blocks ahead.  Operand (j, lane / 16) of a
-// vector lies `u` = 4 j + lane / 16 places further on among its 16 vectors: neither the threads that write a vector's operands nor
-// the lanes that read 16 vectors' meet on a bank.
+// Many vectors (of 8 elements at least): a workgroup takes kRows4 rows, 32 a wave, up to 64 vectors and a share of the blocks.  X becomes operands
+// on the way to LDS, two blocks at a time, while the two before are multiplied; the weights go from memory to registers two blocks ahead.  Operand
+// (j, lane / 16) of a vector lies `u` = 4 j + lane / 16 places further on among its 16 vectors: neither the threads that write a vector's operands
+// nor the lanes that read 16 vectors' meet on a bank.
+//
+// 256 rows share the conversion of X, and 32 rows a wave the reads of its operands: that costs as many instructions as unpacking the weights.  48
+// vectors of 32 bits, 4096 x 16384 with groups of 32 (37 MB, 6.4 GFLOP counted once): 23 us and 4.8 for the join, 95 with the kernel of few vectors.
+// A SIMD's vector instructions (3300 a wave: unpacking, X's terms, both scales every 32 elements) and its products (6100 cycles a wave, two
+// terms) add up; memory waits 30 % of the time.  Requests fenced against the compiler's order gave nothing and spilt registers at groups of 32.
 constexpr int kRows4 = 32 * kWaves4;
 // PER_BLOCK: X has one scale in a block of 128.
 template <int XT, int F, int G, int NC, bool PER_BLOCK>

@@ -67,7 +67,7 @@ Gemm4Plan gemm4_plan(const biq_gemm4_args& a) {
     }
     const int groups = (a.batch + 63) / 64;
     pl.columns = (a.batch + groups - 1) / groups;
-    // a workgroup for every CU, four blocks each at least
+    // a workgroup for every CU, four blocks each at least (fewer do not pay for the join: 2 to 5 us in a launch of its own)
     const long long units = static_cast<long long>((a.m + kRows4 - 1) / kRows4) * groups;
     long long splits = units >= 256 ? 1 : 256 / units;
     splits = splits > (blocks + 3) / 4 ? (blocks + 3) / 4 : splits;
