@@ -648,7 +648,9 @@ biq_status biq_gemm4(const biq_gemm4_args* args, void* workspace, size_t workspa
  *   3. temperature[s] (NULL: 1): z * (1 / temperature).  One that is not above 2^-100 leaves z; none counts as more than 2^100.
  *   4. mask: bit v % 32 of the 32-bit word v / 32 of a row is 0: z = -infinity, whatever it was.
  * out: z, or with `probabilities` exp(z) / sum exp(z) over the row (temperature not above 2^-100: 1 at the largest z, the first of
- * several, 0 elsewhere).  A row whose every z is -infinity has probabilities 0.  A NaN that is not masked makes its row's probabilities NaN.
+ * several, 0 elsewhere).  A row whose every z is -infinity has probabilities 0.  (On the way to
+ * probabilities finite numbers up to 2^143 are held: a row all of its type's lowest value is no row of infinities.)
+ * A NaN that is not masked makes its row's probabilities NaN.
  * out may be x (same data, type and strides).  vocab <= 2^22, biases <= 4096 (BIQ_EUNSUPPORTED beyond).  Deterministic.
  * workspace: biq_logits_workspace_bytes(), 16-byte aligned (may be 0; none is needed without probabilities).
  */

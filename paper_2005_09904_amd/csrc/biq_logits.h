@@ -175,12 +175,32 @@ __device__ __forceinline__ float largest_of_wave(float x) {
 }
 __device__ __forceinline__ int lowest_of_wave(int x) { return best_of_wave(x, [](int a, int b) { return a < b ? a : b; }); }
 __device__ __forceinline__ float sum_of_wave(float x) { return over_wave(x, 0.f, [](float a, float b) { return a + b; }); }
-// What a row comes to: probabilities are exp2(z - top) each, or for greedy sequences 1 at place `at`.  A NaN among the
+// What a row comes to: probabilities are exp2((z - top) unit) each, or for greedy sequences 1 at place `at`.  A NaN among the
 // exponentials is one in their sum, and so comes to all of them.
 struct RowSum {
     float top, sum;
     int at;
 };
+// Logits of probabilities are held in units of 2^16, so that what stays within 2^143 loses nothing: rows that are all of the type's lowest
+// value are (times log2 e, a repetition, a low temperature).  (Powers of two round nothing; what lies below 2^-133 is gone.)
+constexpr float kLogitUnit = 0x1p16f;
+__device__ __forceinline__ float exp_of(float z, float top) { return __builtin_amdgcn_exp2f((z - top) * kLogitUnit); }
+// Of all of a thread's: in one instruction each where the largest is in range by itself (the product with the unit is exact).
+template <int U>
+__device__ __forceinline__ void exps_of(float (&z)[U][8], float top) {
+    const float from = top == -INFINITY ? 0.f : top, there = from * kLogitUnit;
+    if (fabsf(there) < INFINITY) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][i], kLogitUnit, -there));
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[u][i] = exp_of(z[u][i], from);
+    }
+}
 // Of n pairs (largest logit, and the sum of exponentials or its place), all threads of a wave for all of them; `mine` is pair `lane`.
 __device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n, bool greedy) {
     const int lane = threadIdx.x & 63;
@@ -204,7 +224,7 @@ __device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n,
     if (lane < n) r.top = mine[0];
     for (int i = lane + 64; i < n; i += 64) r.top = fmaxf(r.top, pairs[i][0]);
     r.top = largest_of_wave(r.top);
-    auto part = [&](f32x2 x) { return x[0] == -INFINITY ? x[1] : x[1] * __builtin_amdgcn_exp2f(x[0] - r.top); };
+    auto part = [&](f32x2 x) { return x[0] == -INFINITY ? x[1] : x[1] * exp_of(x[0], r.top); };
     if (lane < n) r.sum = part(mine);
     for (int i = lane + 64; i < n; i += 64) r.sum += part(pairs[i]);
     r.sum = sum_of_wave(r.sum);
@@ -249,8 +269,8 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
     int draft = p.drafts && lane < p.rows - 1 ? drafts[lane] : -1;      // of the row after lane `lane` (of the 64 that it is among)
     if (counting || biases) count_tokens<THREADS, SPAN>(p, seq, t0, counts, biases);
     // Logits times the temperature's reciprocal, for exponentials (but for greedy sequences) times log2 e too.  z becomes z by - less: by is that
-    // factor, for a token said before with its repetition's, less its penalties without its biases.
-    const float scale = WHAT == 0 || k.greedy ? k.heat : k.heat * 1.4426950408889634f;
+    // factor (and the unit's), for a token said before with its repetition's, less its penalties without its biases.
+    const float scale = WHAT == 0 || k.greedy ? k.heat : k.heat * (1.4426950408889634f / kLogitUnit);
     const float again = k.repetition * scale, inverse = 1.f / k.repetition * scale;
     auto less_of = [&](uint32_t c, float bias) {
         const uint32_t said = c & ~kInPrompt;
@@ -351,14 +371,11 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
                 mine = (f32x2){__any(bad) ? __uint_as_float(0x7fc00000u) : top, __int_as_float(lowest_of_wave(at))};
             } else {
                 float all = 0.f;
-                const float from = top == -INFINITY ? 0.f : top;        // (all -infinity: sum 0, but for a NaN)
+                exps_of(z, top);                                // (all -infinity: sum 0, but for a NaN)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        z[u][i] = __builtin_amdgcn_exp2f(z[u][i] - from);
-                        all += z[u][i];
-                    }
+                    for (int i = 0; i < 8; ++i) all += z[u][i];
                 mine = (f32x2){top, sum_of_wave(all)};
             }
             f32x2* mine_at = pairs + (row & 1) * WAVES;         // (the other ones may still be read)
@@ -370,18 +387,12 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
                 if (lane == 0) p.stats[r * p.spans + span] = (f32x2){sum.top, k.greedy ? __int_as_float(sum.at) : sum.sum};
                 continue;
             }
-            by = sum.sum == 0.f ? 0.f : (mine[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mine[0] - sum.top)) / sum.sum;
+            by = sum.sum == 0.f ? 0.f : (mine[0] == -INFINITY ? 1.f : exp_of(mine[0], sum.top)) / sum.sum;
         }
         if constexpr (WHAT == 2) {
             sum = row_sum(my_pair, p.stats + r * p.spans, p.spans, k.greedy);
             by = sum.sum == 0.f ? 0.f : 1.f / sum.sum;
-            const float from = sum.top == -INFINITY ? 0.f : sum.top;
-            if (!k.greedy) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) z[u][i] = __builtin_amdgcn_exp2f(z[u][i] - from);
-            }
+            if (!k.greedy) exps_of(z, sum.top);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {

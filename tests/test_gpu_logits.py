@@ -127,6 +127,45 @@ def test_rows_without_tokens_infinities_and_nan(biq, vocab, heat):
     check(x, sub, torch.from_numpy(z), "fp32", False)
 
 
+@pytest.mark.parametrize("typ", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("vocab", [90, 5001, 16000, 20001])
+@pytest.mark.parametrize("heat", [1.0, 0.5, 2.0, 0.0])
+def test_the_ends_of_the_type(biq, typ, vocab, heat):
+    """Rows all of the type's lowest value, some of it masked, some -infinity; such beside ordinary ones; forced tokens; those banned by a bias."""
+    low = torch.finfo(su.TYPES[typ]).min
+    x = torch.full((6, 1, vocab), low, dtype=su.TYPES[typ])
+    mask = np.full((6, 1, -(-vocab // 32)), -1, np.int32)
+    mask[1, 0, 0] = 0x0ffffff0
+    x[2, 0, ::3] = float("-inf")
+    x[3, 0, vocab - 2] = 1.0
+    x[4, 0], x[4, 0, [1, vocab - 1]] = 3.0, -low
+    biases = np.full((6, 2), 0.0, np.float32)
+    biases[5] = float("-inf")
+    h = dict(mask=mask, temperature=np.full(6, heat, np.float32), bias_tokens=np.tile(np.array([0, vocab - 1], np.int32), (6, 1)), bias_values=biases,
+             repetition=np.full(6, 1.5, np.float32), history=np.arange(6, dtype=np.int32)[:, None] * 0 + 7, lens=np.ones(6, np.int32))
+    h["repetition"][[0, 1]] = 1
+    p = su.back(call(biq, x, h, "fp32", True))[:, 0].astype(np.float64)
+    want = np.ones((6, vocab))
+    want[1, :4] = want[1, 28:32] = 0
+    want[2, ::3] = 0
+    want[3], want[4] = np.arange(vocab) == vocab - 2, np.isin(np.arange(vocab), [1, vocab - 1])
+    want[5, [0, vocab - 1]] = 0
+    if heat == 0:
+        want = np.arange(vocab) == want.argmax(axis=1)[:, None]
+    else:
+        want[[2, 5], 7] = 0                                         # (times 1.5 it is far below the others)
+    want = want / want.sum(axis=1, keepdims=True)
+    # the sum has equal terms (whole numbers, exact), the reciprocal and the product round once each
+    assert (np.abs(p - want) <= 2.0 ** -22 * want).all()
+
+
+def test_the_ends_of_the_type_in_many_whole_rows(biq):
+    x = torch.full((128, 1, 20001), torch.finfo(torch.bfloat16).min, dtype=torch.bfloat16)
+    x[::2, 0, 5:] = float("-inf")
+    p = su.back(call(biq, x, {}, "fp32", True))[:, 0].astype(np.float64)
+    assert (np.abs(p[::2] - 0.2 * (np.arange(20001) < 5)) <= 2.0 ** -22).all() and (np.abs(p[1::2] * 20001 - 1) <= 2.0 ** -22).all()
+
+
 def test_the_first_of_several_largest(biq):
     for vocab in (50, 5000, 20000):
         x = torch.zeros((3, 1, vocab))
