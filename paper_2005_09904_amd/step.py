@@ -169,6 +169,8 @@ class PreparedLogits(_Prepared):
             _need(history.dim() == 2, "history: [seqs, tokens] expected")
             a.width = history.shape[1]
             a.history = _whole(history, "history", "int32", [seqs, a.width], x.device)
+            if a.width == 0:                                        # nothing said yet
+                history = lens = prompt_lens = None
         for name, t, kind, shape in (("lens", lens, "int32", [seqs]), ("prompt_lens", prompt_lens, "int32", [seqs]),
                                      ("drafts", drafts, "int32", [seqs, rows - 1]), ("repetition", repetition, "float32", [seqs]),
                                      ("presence", presence, "float32", [seqs]), ("frequency", frequency, "float32", [seqs]),

@@ -166,6 +166,13 @@ def test_the_ends_of_the_type_in_many_whole_rows(biq):
     assert (np.abs(p[::2] - 0.2 * (np.arange(20001) < 5)) <= 2.0 ** -22).all() and (np.abs(p[1::2] * 20001 - 1) <= 2.0 ** -22).all()
 
 
+def test_nothing_said_yet_and_no_biases(biq):
+    x, h = inputs(2, 2, 700, "fp32", 8)
+    none = dict(h, history=np.zeros((2, 0), np.int32), bias_tokens=np.zeros((2, 0), np.int32), bias_values=np.zeros((2, 0), np.float32))
+    without = {k: v for k, v in h.items() if k not in ("history", "lens", "prompt_lens", "bias_tokens", "bias_values")}
+    assert torch.equal(call(biq, x, none, "fp32", True), call(biq, x, without, "fp32", True))
+
+
 def test_the_first_of_several_largest(biq):
     for vocab in (50, 5000, 20000):
         x = torch.zeros((3, 1, vocab))
