@@ -323,9 +323,9 @@ __device__ __forceinline__ void tile4(const uint8_t* tile, int record, int block
 }
 
 // X's operands from its elements, all threads of a workgroup; AHEAD units of 8 elements are requested together (a block has 16 units, so
-// lanes that exchange magnitudes are all there).
-template <int XT>
-__device__ __forceinline__ void stage4(const Gemm4Params& p, int column0, int columns, int x_scales, f16x8* to, float* units) {
+// lanes that exchange magnitudes are all there).  between: called once, with the first units requested.
+template <int XT, typename Between>
+__device__ __forceinline__ void stage4(const Gemm4Params& p, int column0, int columns, int x_scales, f16x8* to, float* units, const Between& between) {
     constexpr int THREADS = 64 * kWaves4, AHEAD = XT == BIQ_F32 ? 4 : 8;
     typedef typename X4<XT>::T T;
     const int per = p.blocks * 16, total = per * columns, every = 16 / x_scales;
@@ -354,6 +354,7 @@ __device__ __forceinline__ void stage4(const Gemm4Params& p, int column0, int co
         };
         if (p.n < 8) request(true);
         else request(false);
+        if (first == static_cast<int>(threadIdx.x)) between();
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
             if (first + a * THREADS >= total) break;
@@ -388,7 +389,9 @@ __device__ __forceinline__ void store_y4(const Gemm4Params& p, int column, int r
 // of waves: there are twice as many splits until tiles x splits fill 2048 waves.
 //
 // The weights bound large products: 32000 x 4096 with groups of 64 (70 MB) and one vector of bfloat16 16.7 us, 4.4 TB/s as the workgroups' start (X is
-// the operand that all of it waits for) is not covered by loads; 16384 x 4096 with five vectors of codes (35 MB) 11.4 us.  4096 x 4096 with one vector
+// the operand that all of it waits for) is not covered by loads; 16384 x 4096 with five vectors of codes (35 MB) 11.4 us.  One load a wave touches the
+// lines of its first four records while X is converted: a pass among others takes 15.2 us instead of 15.7, 10.4 instead of 10.8, and 5.6
+// instead of 5.5 for 4096 x 4096, whose weights the caches hold.  4096 x 4096 with one vector
 // takes 6.3 us, X, weights and join one after the other.  AHEAD records of weights are in flight: with 8 the head takes 23 us, with 2 17.4, with
 // the weights asked for before X becomes operands 19.7 (registers).
 template <int XT, int F, int G>
@@ -398,13 +401,19 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
     const int column0 = blockIdx.y * 16, columns = p.batch - column0 < 16 ? p.batch - column0 : 16;
     f16x8* operands = reinterpret_cast<f16x8*>(lds);
     float* units = reinterpret_cast<float*>(operands + p.blocks * 16 * kTerms4<XT> * columns);
-    stage4<XT>(p, column0, columns, x_scales, operands, units);
-    __syncthreads();
     const int per = kWaves4 / p.splits, split = wave % p.splits, tile = (p.first + blockIdx.x) * per + wave / p.splits;
+    const uint8_t* weights = p.weights + static_cast<long long>(tile < p.tiles ? tile : p.tiles - 1) * p.blocks * p.record;
+    int touched = 0;
+    stage4<XT>(p, column0, columns, x_scales, operands, units, [&]() {
+        const int block = split + (lane >> 4) * p.splits, at = (lane & 15) * 128;
+        touched = *reinterpret_cast<const int*>(weights + (block < p.blocks ? block : p.blocks - 1) * static_cast<long long>(p.record) + (at < p.record ? at : 0));
+    });
+    __syncthreads();
     f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
     if (tile < p.tiles)
-        tile4<kTerms4<XT>, F, G, 1, 4>(p.weights + static_cast<long long>(tile) * p.blocks * p.record, p.record, p.blocks, split, p.splits,
+        tile4<kTerms4<XT>, F, G, 1, 4>(weights, p.record, p.blocks, split, p.splits,
                                     {operands, units, columns}, x_scales, acc);
+    asm volatile("" : : "v"(touched));
     if (p.splits > 1) {
         __syncthreads();                                        // (the operands are read)
         f32x4* sums = reinterpret_cast<f32x4*>(lds);
