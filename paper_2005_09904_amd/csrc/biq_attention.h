@@ -197,7 +197,7 @@ __device__ __forceinline__ RowPlace row_place(const AttendParams& p, RowRange ra
 //
 // Sharing divides the cache's reads by the sequences, and makes one large product of their small ones, which bounds it: 24 sequences of 5 rows,
 // 32 / 8 heads of 128, fp32, behind 32768 shared tokens take 128 us for the shared part (matrix cores busy 42 % of it, in two terms, vector
-// instructions 39 %), 15.5 for the own, 8.7 for the join.  32 single rows in bfloat16 behind 8192 tokens (52 MB) take 25.3 + 4.9 us: 3072 waves,
+// instructions 39 %), 15.5 for the own, 8.7 for the join.  32 single rows in bfloat16 behind 8192 tokens (52 MB) take 25.3 + 4.9 us: 12 waves a CU,
 // each with a chain of loads (page, codes, rows) of 9 us around its steps.
 // The kernels are those of other calls, in a second form: registers of the first stay what they were.
 
