@@ -521,7 +521,8 @@ biq_status biq_attention(const biq_attention_args* args, void* workspace, size_t
  * sequence are those of sequence 0, in the pages table[0][0 .. shared / page_tokens), which are read once for all rows of the call; the entries
  * of the other sequences for them are not looked at.  These pages hold `shared` tokens, whatever lens says.  shared: a multiple of page_tokens, at least one page and at most
  * table_stride * page_tokens (BIQ_EINVAL).  lens count the shared tokens; a sequence may also be shorter than them.  Everything
- * else, and what it costs in bits, is as with biq_attention; results differ from its in the order of additions.
+ * else, and what it costs in bits, is as with biq_attention, but that the weights of bf16 outputs keep 22 bits like the others; results differ
+ * from its in the order of additions.
  * workspace: biq_attention_shared_workspace_bytes(), 16-byte aligned (never 0).
  */
 typedef struct {

@@ -147,8 +147,11 @@ struct Factor {
 // once it is scaled into their range.  Terms of q: two for 32-bit elements, one otherwise (bf16 values have 8 bits).
 template <int TYPE> struct RowTerms { static constexpr int value = TYPE == BIQ_F32 ? 2 : 1; };
 // Terms of the weights: one (11 bits) where the output has 8 bits, two otherwise.  (Prompts of 4096 rows in bf16 are off by 1.67e-3 from
-// 64 bits with one, 1.66e-3 with 32-bit weights: the output's own rounding.)
-template <int TYPE> struct WeightTerms { static constexpr int value = TYPE == BIQ_BF16 ? 1 : 2; };
+// 64 bits with one, 1.66e-3 with 32-bit weights: the output's own rounding.)  Behind shared tokens there are
+// two for every output: with one, those in bf16 that lie near the middle of two numbers round to the farther one (2 to 7 % of them, which is
+// a difference of 7.7e-4 from 32-bit weights over 9000 tokens).  That costs 1.5 us where rows are few (32 behind 8192 tokens 25.4 > 26.9) and a third
+// of the tile kernel's products (24 x 5 behind 32768 in bf16 89 > 117, four prompts of 70 behind 4096 46 > 53.5).
+template <int TYPE, bool SHARED> struct WeightTerms { static constexpr int value = TYPE == BIQ_BF16 && !SHARED ? 1 : 2; };
 
 template <int TERMS>
 __device__ __forceinline__ void f16_terms(const float (&x)[8], f16x8 (&out)[TERMS]) {
@@ -551,7 +554,7 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 w, int valid) {
 // CH: 64 elements of a head each; FULL: the head has all of them; NT: tiles of 16 rows.
 template <int TYPE, int FMT, int CH, bool FULL, int NT, int WAVES, bool SHARED = false>
 __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1) void attend_rows_kernel(const AttendParams p) {
-    constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE>::value;
+    constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE, SHARED>::value;
     constexpr int ROWS = 16 * NT;
     extern __shared__ float lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -813,7 +816,7 @@ __global__ __launch_bounds__(64 * WAVES, CH * NT == 1 ? 3 : CH * NT == 2 ? 2 : 1
 // are 20 % faster a flop here and their layout gives a lane one scale.
 template <int TYPE, int FMT, int CH, bool FULL, bool HALF, int NT, int WAVES, bool SHARED = false>
 __global__ __launch_bounds__(64 * WAVES, CH <= 2 ? 2 : 1) void attend_tile_kernel(const AttendParams p) {
-    constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE>::value;
+    constexpr int QT = RowTerms<TYPE>::value, PT = WeightTerms<TYPE, SHARED>::value;
     constexpr int STEPS = WAVES / 4, ROWS = 16 * NT * WAVES;
     constexpr int SIDE = 8 * CH * 64;                           // places for a step's keys as operands; as many for its values
     constexpr int KEYS = 2 * CH - HALF, VALUES = 4 * CH - 2 * HALF;      // operands of 32 elements; of 16
