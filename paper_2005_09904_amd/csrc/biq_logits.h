@@ -175,34 +175,38 @@ __device__ __forceinline__ float largest_of_wave(float x) {
 }
 __device__ __forceinline__ int lowest_of_wave(int x) { return best_of_wave(x, [](int a, int b) { return a < b ? a : b; }); }
 __device__ __forceinline__ float sum_of_wave(float x) { return over_wave(x, 0.f, [](float a, float b) { return a + b; }); }
-// What a row comes to: probabilities are exp2((z - top) unit) each, or for greedy sequences 1 at place `at`.  A NaN among the
+// What a row comes to: probabilities are 2^((z - top) heat) / sum each, or for greedy sequences 1 at place `at`.  A NaN among the
 // exponentials is one in their sum, and so comes to all of them.
 struct RowSum {
     float top, sum;
     int at;
 };
-// Logits of probabilities are held in units of 2^16, so that what stays within 2^143 loses nothing: rows that are all of the type's lowest
-// value are (times log2 e, a repetition, a low temperature).  (Powers of two round nothing; what lies below 2^-133 is gone.)
+// Logits of probabilities are held in units of 2^16, before the temperature's factor, so that what stays within 2^143 loses nothing: rows that are
+// all of the type's lowest value are (times a repetition).  (Powers of two round nothing; what lies below 2^-133 is gone.)  heat: that
+// factor, log2 e and the unit, at most 2^117.
 constexpr float kLogitUnit = 0x1p16f;
-__device__ __forceinline__ float exp_of(float z, float top) { return __builtin_amdgcn_exp2f((z - top) * kLogitUnit); }
-// Of all of a thread's: in one instruction each where the largest is in range by itself (the product with the unit is exact).
+__device__ __forceinline__ float exp_of(float z, float top, float heat) { return __builtin_amdgcn_exp2f((z - top) * heat); }
+// Of all of a thread's, 2^(z heat - near), near = top heat rounded; returned is what makes 2^((z - top) heat) of them, so that what is lost goes with
+// z - top and not with z (logits around 1000: 1.8e-5 of the row where the factor was part of z, 1e-7 so).  One instruction each, where
+// near is small enough for its rounding to be a factor close to 1; the difference first where it is not.
 template <int U>
-__device__ __forceinline__ void exps_of(float (&z)[U][8], float top) {
-    const float from = top == -INFINITY ? 0.f : top, there = from * kLogitUnit;
-    if (fabsf(there) < INFINITY) {
+__device__ __forceinline__ float exps_of(float (&z)[U][8], float top, float heat) {
+    const float from = top == -INFINITY ? 0.f : top, near = from * heat;
+    if (fabsf(near) < 0x1p20f) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][i], kLogitUnit, -there));
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[u][i] = exp_of(z[u][i], from);
+            for (int i = 0; i < 8; ++i) z[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][i], heat, -near));
+        return __builtin_amdgcn_exp2f(-__builtin_fmaf(from, heat, -near));
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[u][i] = exp_of(z[u][i], from, heat);
+    return 1.f;
 }
 // Of n pairs (largest logit, and the sum of exponentials or its place), all threads of a wave for all of them; `mine` is pair `lane`.
-__device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n, bool greedy) {
+__device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n, bool greedy, float heat) {
     const int lane = threadIdx.x & 63;
     RowSum r = {-INFINITY, 0.f, -1};
     if (greedy) {
@@ -224,7 +228,7 @@ __device__ __forceinline__ RowSum row_sum(f32x2 mine, const f32x2* pairs, int n,
     if (lane < n) r.top = mine[0];
     for (int i = lane + 64; i < n; i += 64) r.top = fmaxf(r.top, pairs[i][0]);
     r.top = largest_of_wave(r.top);
-    auto part = [&](f32x2 x) { return x[0] == -INFINITY ? x[1] : x[1] * exp_of(x[0], r.top); };
+    auto part = [&](f32x2 x) { return x[0] == -INFINITY ? x[1] : x[1] * exp_of(x[0], r.top, heat); };
     if (lane < n) r.sum = part(mine);
     for (int i = lane + 64; i < n; i += 64) r.sum += part(pairs[i]);
     r.sum = sum_of_wave(r.sum);
@@ -268,9 +272,9 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
     const int* drafts = p.drafts + static_cast<long long>(seq) * (p.rows - 1);
     int draft = p.drafts && lane < p.rows - 1 ? drafts[lane] : -1;      // of the row after lane `lane` (of the 64 that it is among)
     if (counting || biases) count_tokens<THREADS, SPAN>(p, seq, t0, counts, biases);
-    // Logits times the temperature's reciprocal, for exponentials (but for greedy sequences) times log2 e too.  z becomes z by - less: by is that
-    // factor (and the unit's), for a token said before with its repetition's, less its penalties without its biases.
-    const float scale = WHAT == 0 || k.greedy ? k.heat : k.heat * (1.4426950408889634f / kLogitUnit);
+    // Logits times the temperature's reciprocal, or for exponentials (but for greedy sequences) in their unit.  z becomes z by - less: by is that
+    // factor, for a token said before with its repetition's, less its penalties without its biases.
+    const float scale = WHAT == 0 || k.greedy ? k.heat : 1.f / kLogitUnit, heat = k.heat * (1.4426950408889634f * kLogitUnit);
     const float again = k.repetition * scale, inverse = 1.f / k.repetition * scale;
     auto less_of = [&](uint32_t c, float bias) {
         const uint32_t said = c & ~kInPrompt;
@@ -350,7 +354,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
         float by = 0.f;                                         // makes probabilities of z's exponentials
         if constexpr (WHAT == 1 || WHAT == 3) {
             f32x2 mine;
-            float top = -INFINITY;
+            float top = -INFINITY, fix = 1.f;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -371,28 +375,28 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const LogitsParams p) {
                 mine = (f32x2){__any(bad) ? __uint_as_float(0x7fc00000u) : top, __int_as_float(lowest_of_wave(at))};
             } else {
                 float all = 0.f;
-                exps_of(z, top);                                // (all -infinity: sum 0, but for a NaN)
+                fix = exps_of(z, top, heat);                    // (all -infinity: sum 0, but for a NaN)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) all += z[u][i];
-                mine = (f32x2){top, sum_of_wave(all)};
+                mine = (f32x2){top, sum_of_wave(all) * fix};
             }
             f32x2* mine_at = pairs + (row & 1) * WAVES;         // (the other ones may still be read)
             if (lane == 0) mine_at[wave] = mine;
             __syncthreads();
             if (WHAT == 1 && wave > 0) continue;
-            sum = row_sum(mine_at[lane < WAVES ? lane : 0], mine_at, WAVES, k.greedy);
+            sum = row_sum(mine_at[lane < WAVES ? lane : 0], mine_at, WAVES, k.greedy, heat);
             if (WHAT == 1) {
                 if (lane == 0) p.stats[r * p.spans + span] = (f32x2){sum.top, k.greedy ? __int_as_float(sum.at) : sum.sum};
                 continue;
             }
-            by = sum.sum == 0.f ? 0.f : (mine[0] == -INFINITY ? 1.f : exp_of(mine[0], sum.top)) / sum.sum;
+            by = sum.sum == 0.f ? 0.f : fix * (mine[0] == -INFINITY ? 1.f : exp_of(mine[0], sum.top, heat)) / sum.sum;
         }
         if constexpr (WHAT == 2) {
-            sum = row_sum(my_pair, p.stats + r * p.spans, p.spans, k.greedy);
-            by = sum.sum == 0.f ? 0.f : 1.f / sum.sum;
-            if (!k.greedy) exps_of(z, sum.top);
+            sum = row_sum(my_pair, p.stats + r * p.spans, p.spans, k.greedy, heat);
+            const float fix = k.greedy ? 1.f : exps_of(z, sum.top, heat);
+            by = sum.sum == 0.f ? 0.f : fix / sum.sum;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
