@@ -623,6 +623,7 @@ biq_status biq_unpack4(const uint8_t* packed, float* W, int64_t stride, int m, i
  *
  * Weights' codes, X's codes and 16-bit floats enter the matrix cores as they are.  32-bit and bfloat16 elements are scaled by a power
  * of two per 128 elements and keep 22 bits (bfloat16 all of theirs), none below 2^-39 of the largest of the 128.  Sums are in 32 bits.
+ * Weights' scales above 2^100 may make infinities of products that are in range; large inputs do not.
  * Deterministic.  A vector with an infinity or a NaN gives NaN or infinities.
  * batch <= 65535 (BIQ_EUNSUPPORTED beyond).  workspace: biq_gemm4_workspace_bytes(), 16-byte aligned (0 for a few vectors).
  */

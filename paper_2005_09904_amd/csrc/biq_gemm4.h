@@ -274,6 +274,9 @@ struct Part4 {
     }
 };
 
+// Sums of a group are multiplied by the weights' scale, then by X's unit or scale: with scales up to 2^100 the first product stays in range (sums are
+// at most 2^26), and the second is the result.  (X's first would leave 32 bits from 1e36 on, whatever the weights are.)
+//
 // A wave's share of a tile of 16 rows: blocks `from`, from + step, ..., of NC times 16 columns.  F spans of 32 share both scales, G the
 // weights'.  AHEAD records are requested before the first of them is used.
 template <int TERMS, int F, int G, int NC, int AHEAD>
@@ -313,7 +316,7 @@ __device__ __forceinline__ void tile4(const uint8_t* tile, int record, int block
                     for (int c = 0; c < NC; ++c) {
                         const float unit = x.units[(block * x_scales + f * x_scales / FLUSHES) * x.columns + col[c]];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[c][e] = __builtin_fmaf(part[c][e] * unit, ws[e], acc[c][e]);
+                        for (int e = 0; e < 4; ++e) acc[c][e] = __builtin_fmaf(part[c][e] * ws[e], unit, acc[c][e]);
                     }
                 }
             }
@@ -544,7 +547,7 @@ __global__ __launch_bounds__(64 * kWaves4, 2) void gemm4_many_kernel(const Gemm4
                         } else {
                             const float v = unit[f * x_scales / FLUSHES * COLS + 16 * k + (lane & 15)];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[r][k][e] = __builtin_fmaf(part[r][k][e] * v, ws[e], acc[r][k][e]);
+                            for (int e = 0; e < 4; ++e) acc[r][k][e] = __builtin_fmaf(part[r][k][e] * ws[e], v, acc[r][k][e]);
                         }
                     }
                 }
