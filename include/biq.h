@@ -653,7 +653,8 @@ biq_status biq_gemm4(const biq_gemm4_args* args, void* workspace, size_t workspa
  * several, 0 elsewhere).  A row whose every z is -infinity has probabilities 0.  (On the way to
  * probabilities finite numbers up to 2^143 are held: a row all of its type's lowest value is no row of infinities.)
  * A NaN that is not masked makes its row's probabilities NaN.
- * out may be x (same data, type and strides).  vocab <= 2^22, biases <= 4096 (BIQ_EUNSUPPORTED beyond).  Deterministic.
+ * out may be x (same data, type and strides).  vocab <= 2^22, biases <= 4096, width < 2^31 - 2^16 (BIQ_EUNSUPPORTED beyond).
+ * Deterministic.
  * workspace: biq_logits_workspace_bytes(), 16-byte aligned (may be 0; none is needed without probabilities).
  */
 typedef struct {

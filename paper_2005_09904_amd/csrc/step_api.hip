@@ -230,6 +230,8 @@ biq_status biq_logits(const biq_logits_args* a, void* workspace, size_t workspac
     if (!write_ok(a->out_stride, a->rows, a->vocab) || !write_ok(a->out_seq_stride, a->seqs, a->vocab)) return BIQ_EINVAL;
     if (a->x == a->out && (a->type != a->out_type || a->x_seq_stride != a->out_seq_stride || a->x_stride != a->out_stride)) return BIQ_EINVAL;
     if (a->vocab > (1 << 22) || a->biases > 4096 || static_cast<long long>(a->seqs) * a->rows > kMaxInt) return BIQ_EUNSUPPORTED;
+    // (a workgroup steps over a history by up to 2^14 tokens, in 32 bits)
+    if (a->history && a->width > kMaxInt - (1 << 16)) return BIQ_EUNSUPPORTED;
     const bool whole = logits_whole(a->vocab, a->biases > 0, a->seqs);
     const size_t need = a->probabilities ? biq_logits_workspace_bytes(a->seqs, a->rows, a->vocab) : 0;
     if (need > workspace_bytes) return BIQ_EWORKSPACE;
