@@ -89,9 +89,17 @@ __device__ __forceinline__ T over_row(T x, T* lds, const Join& join) {
 struct Add { template <typename T> __device__ __forceinline__ T operator()(T a, T b) const { return a + b; } };
 struct Largest { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; } };
 
+// 1 / sqrt(mean(s^2) + eps) as r up, up a power of two: without eps, rows of the least numbers there are have one beyond 32 bits.  (Infinite for zeros.)
+struct Root { float r, up; };
+__device__ __forceinline__ Root root64(double sum, int n, float eps) {
+    const double root = 1.0 / sqrt(sum / n + static_cast<double>(eps));
+    const float up = root > 0x1p120 ? 0x1p64f : 1.f;
+    return {static_cast<float>(root / up), up};
+}
+
 // Codes of 8 values and their group's scale.  bits: the group's largest magnitude as an integer.
 template <int FMT>
-__device__ __forceinline__ void put_codes8(const NormParams& p, long long row, int e, const float (&t)[8], uint32_t bits, float r) {
+__device__ __forceinline__ void put_codes8(const NormParams& p, long long row, int e, const float (&t)[8], uint32_t bits, Root root) {
 #pragma clang fp contract(off)
     const BlockScale b = block_scale<FMT>(bits, 0.f);
     const bool none = b.fresh == 0.f;                           // zeros, or a group that is NaN altogether
@@ -106,7 +114,9 @@ __device__ __forceinline__ void put_codes8(const NormParams& p, long long row, i
         c[4 + i] = static_cast<uint8_t>(hi >> (8 * i));
     }
     store8(p.codes + row * p.code_stride, e, p.n, c);
-    if (p.group == 0 ? e == 0 : e % p.group == 0) p.scales[row * p.groups + (p.group == 0 ? 0 : e / p.group)] = b.scale * r;
+    // (0 for zeros, with any r that is a number)
+    const float r = root.r == INFINITY ? 0x1.fffffep127f : root.r;
+    if (p.group == 0 ? e == 0 : e % p.group == 0) p.scales[row * p.groups + (p.group == 0 ? 0 : e / p.group)] = b.scale * root.up * r;
 }
 
 // 1 / sqrt(sum / n + eps) where the sum of squares is a number that 32 bits hold with all their precision.
@@ -151,7 +161,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(con
         }
     }
     total = over_row<THREADS>(total, reinterpret_cast<float*>(lds), Add());
-    float r = root_of(total, p.n, p.eps);
+    Root root = {root_of(total, p.n, p.eps), 1.f};
     if (!sum_fits(total)) {                                     // squares that leave 32 bits: the same in 64
         double wide = 0.0;
 #pragma unroll
@@ -159,7 +169,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(con
 #pragma unroll
             for (int i = 0; i < 8; ++i) wide += static_cast<double>(s[k][i]) * s[k][i];
         wide = over_row<THREADS>(wide, lds, Add());
-        r = static_cast<float>(1.0 / sqrt(wide / p.n + static_cast<double>(p.eps)));
+        root = root64(wide, p.n, p.eps);
     }
     if (p.sum) {
 #pragma unroll
@@ -174,7 +184,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(con
             const int e = (k * THREADS + me) * 8;
             float y[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = s[k][i] * r * w[k][i];
+            for (int i = 0; i < 8; ++i) y[i] = s[k][i] * root.up * root.r * w[k][i];
             if (e < p.n) store8_type(p.y_type, p.y, row * p.y_stride, e, p.n, y);
         }
     }
@@ -198,8 +208,8 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(con
 #pragma unroll
         for (int i = 0; i < 8; ++i) t[i] = s[k][i] * w[k][i];
         if (e >= p.n) continue;
-        if (p.format == BIQ_CACHE_INT8) put_codes8<BIQ_CACHE_INT8>(p, row, e, t, bits, r);
-        else put_codes8<BIQ_CACHE_FP8>(p, row, e, t, bits, r);
+        if (p.format == BIQ_CACHE_INT8) put_codes8<BIQ_CACHE_INT8>(p, row, e, t, bits, root);
+        else put_codes8<BIQ_CACHE_FP8>(p, row, e, t, bits, root);
     }
 }
 
@@ -239,7 +249,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p) {
     }
     total = over_row<1024>(total, lds, Add());
     all = over_row<1024>(all, reinterpret_cast<uint32_t*>(lds), Largest());
-    const float r = static_cast<float>(1.0 / sqrt(total / p.n + static_cast<double>(p.eps)));
+    const Root root = root64(total, p.n, p.eps);
     // (all threads together, as groups are lanes' that exchange their largest)
     for (int e0 = 0; e0 < p.n; e0 += 8192) {
         const int e = e0 + threadIdx.x * 8;
@@ -248,7 +258,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p) {
         uint32_t bits = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            y[i] = s[i] * r * w[i];
+            y[i] = s[i] * root.up * root.r * w[i];
             t[i] = s[i] * w[i];
             const uint32_t b = __float_as_uint(t[i]) & 0x7fffffffu;
             bits = e < p.n && b > bits ? b : bits;
@@ -262,8 +272,8 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p) {
         if (p.sum) store8_as<TYPE>(p.sum, row * p.sum_stride, e, p.n, s);
         if (p.y) store8_type(p.y_type, p.y, row * p.y_stride, e, p.n, y);
         if (!p.codes) continue;
-        if (p.format == BIQ_CACHE_INT8) put_codes8<BIQ_CACHE_INT8>(p, row, e, t, bits, r);
-        else put_codes8<BIQ_CACHE_FP8>(p, row, e, t, bits, r);
+        if (p.format == BIQ_CACHE_INT8) put_codes8<BIQ_CACHE_INT8>(p, row, e, t, bits, root);
+        else put_codes8<BIQ_CACHE_FP8>(p, row, e, t, bits, root);
     }
 }
 
