@@ -9,6 +9,7 @@ from . import binding
 from .serving import FORMATS, I, L, P, _need, _Prepared, _type, _whole
 
 F = ctypes.c_float
+INT_MAX = (1 << 31) - 1
 X_CODES = {"torch.int8": 3, "torch.float8_e4m3fn": 4}
 
 
@@ -33,6 +34,7 @@ class _LogitsArgs(ctypes.Structure):
 def _matrix(t, name, shape=None, like=None, device=None):
     """[rows, n] with adjacent elements; its address and stride."""
     _need(t.dim() == 2 and t.numel() > 0, "%s: [rows, elements] expected" % name)
+    _need(max(t.shape) <= INT_MAX, "%s: sizes below 2^31 expected" % name)
     _need(t.shape[1] <= 1 or t.stride(1) == 1, "%s: the elements of a row have to be adjacent" % name)
     _need(shape is None or tuple(t.shape) == tuple(shape), "%s: %s expected" % (name, list(shape or ())))
     _need(like is None or t.dtype == like.dtype, "%s: another type" % name)
@@ -159,6 +161,7 @@ class PreparedLogits(_Prepared):
                  bias_tokens=None, bias_values=None, mask=None, probabilities=False, workspace=None, stream=None):
         for t, name in ((x, "x"), (out, "out")):
             _need(t.dim() == 3 and t.numel() > 0 and (t.shape[2] <= 1 or t.stride(2) == 1), "%s: [seqs, rows, vocab] with adjacent tokens expected" % name)
+            _need(max(t.shape) <= INT_MAX, "%s: sizes below 2^31 expected" % name)
         _need(out.shape == x.shape and out.device == x.device, "out: %s on %s expected" % (list(x.shape), x.device))
         seqs, rows, vocab = x.shape
         a = _LogitsArgs(x=x.data_ptr(), out=out.data_ptr(), x_seq_stride=x.stride(0), x_stride=x.stride(1), out_seq_stride=out.stride(0),
@@ -166,7 +169,7 @@ class PreparedLogits(_Prepared):
                         probabilities=int(bool(probabilities)))
         _need((history is None) == (lens is None), "history and lens come together")
         if history is not None:
-            _need(history.dim() == 2, "history: [seqs, tokens] expected")
+            _need(history.dim() == 2 and history.shape[1] <= INT_MAX, "history: [seqs, tokens] expected, fewer than 2^31")
             a.width = history.shape[1]
             a.history = _whole(history, "history", "int32", [seqs, a.width], x.device)
             if a.width == 0:                                        # nothing said yet
@@ -179,7 +182,7 @@ class PreparedLogits(_Prepared):
                 setattr(a, name, _whole(t, name, kind, shape, x.device) or None)
         _need((bias_tokens is None) == (bias_values is None), "bias_tokens and bias_values come together")
         if bias_tokens is not None:
-            _need(bias_tokens.dim() == 2, "bias_tokens: [seqs, biases] expected")
+            _need(bias_tokens.dim() == 2 and bias_tokens.shape[1] <= INT_MAX, "bias_tokens: [seqs, biases] expected, fewer than 2^31")
             a.biases = bias_tokens.shape[1]
             a.bias_tokens = _whole(bias_tokens, "bias_tokens", "int32", [seqs, a.biases], x.device)
             a.bias_values = _whole(bias_values, "bias_values", "float32", [seqs, a.biases], x.device)

@@ -11,3 +11,20 @@ def test_histories_whose_places_leave_32_bits(biq):
     for width in ((1 << 31) - 1, (1 << 31) - (1 << 14), (1 << 31) - (1 << 16)):
         assert lib.biq_logits(at(logits(width=width)), A, 1 << 40, None) == EUNSUPPORTED, width
     assert lib.biq_logits(at(logits(width=-1)), A, 1 << 40, None) == EINVAL
+
+
+def test_tensors_whose_sizes_leave_32_bits(biq):
+    """The descriptors' sizes are int: larger ones must not come through as what is left of them.  (Broadcast tensors take no memory.)"""
+    many = (1 << 32) + 3
+    rows = lambda *shape: torch.zeros(1, *shape[1:]).expand(*shape)
+    packed = torch.zeros(biq.biq_packed4_bytes(16, 8, 32), dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        biq.PreparedNorm(rows(many, 8), rows(many, 8), stream=Stream())
+    with pytest.raises(ValueError):
+        biq.PreparedGemm4(packed, rows(many, 8), rows(many, 16), 32, stream=Stream())
+    with pytest.raises(ValueError):
+        biq.biq_gemm4_workspace_bytes(packed, rows(many, 8), rows(many, 16), 32)
+    with pytest.raises(ValueError):
+        biq.PreparedLogits(rows(many, 1, 8), rows(many, 1, 8), stream=Stream())
+    with pytest.raises(ValueError):
+        biq.biq_quantize4(rows(many, 8), packed, many, 8, 32, stream=Stream())
