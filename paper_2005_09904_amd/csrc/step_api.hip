@@ -27,6 +27,22 @@ biq_status status(hipError_t e) { return e == hipSuccess ? BIQ_OK : BIQ_EHIP; }
 bool read_ok(long long stride) { return stride >= 0 && stride <= kMaxStride; }
 bool write_ok(long long stride, long long rows, int n) { return read_ok(stride) && (rows == 1 || stride >= n); }
 
+// The rows (i, j), i < few, j < many, of n elements at i a + j b: no two of them share an element.  Of sequences' rows one stride spans the others'
+// as a rule; else every difference of i is looked at with the two nearest ones of j.
+bool rows_apart(long long few, long long a, long long many, long long b, int n) {
+    typedef __int128 Wide;
+    if (few > many) return rows_apart(many, b, few, a, n);
+    if (few == 1) return many == 1 || b >= n;
+    if (a < n || b < n) return false;
+    if (a >= static_cast<Wide>(many - 1) * b + n || b >= static_cast<Wide>(few - 1) * a + n) return true;
+    for (long long i = 1; i < few; ++i)
+        for (Wide j = static_cast<Wide>(i) * a / b, last = j + 1; j <= last && j < many; ++j) {
+            const Wide gap = static_cast<Wide>(i) * a - j * b;
+            if (gap < n && gap > -n) return false;
+        }
+    return true;
+}
+
 // ---- products with 4-bit weights: how a call is mapped -------------------------------------------------------
 
 struct Gemm4Plan {
@@ -232,6 +248,7 @@ biq_status biq_logits(const biq_logits_args* a, void* workspace, size_t workspac
     if (a->vocab > (1 << 22) || a->biases > 4096 || static_cast<long long>(a->seqs) * a->rows > kMaxInt) return BIQ_EUNSUPPORTED;
     // (a workgroup steps over a history by up to 2^14 tokens, in 32 bits)
     if (a->history && a->width > kMaxInt - (1 << 16)) return BIQ_EUNSUPPORTED;
+    if (!rows_apart(a->seqs, a->out_seq_stride, a->rows, a->out_stride, a->vocab)) return BIQ_EINVAL;
     const bool whole = logits_whole(a->vocab, a->biases > 0, a->seqs);
     const size_t need = a->probabilities ? biq_logits_workspace_bytes(a->seqs, a->rows, a->vocab) : 0;
     if (need > workspace_bytes) return BIQ_EWORKSPACE;
