@@ -148,9 +148,9 @@ struct Factor {
 template <int TYPE> struct RowTerms { static constexpr int value = TYPE == BIQ_F32 ? 2 : 1; };
 // Terms of the weights: one (11 bits) where the output has 8 bits, two otherwise.  (Prompts of 4096 rows in bf16 are off by 1.67e-3 from
 // 64 bits with one, 1.66e-3 with 32-bit weights: the output's own rounding.)  Behind shared tokens there are
-// two for every output: with one, those in bf16 that lie near the middle of two numbers round to the farther one (2 to 7 % of them, which is
-// a difference of 7.7e-4 from 32-bit weights over 9000 tokens).  That costs 1.5 us where rows are few (32 behind 8192 tokens 25.4 > 26.9) and a third
-// of the tile kernel's products (24 x 5 behind 32768 in bf16 89 > 117, four prompts of 70 behind 4096 46 > 53.5).
+// two for every output: with one, 8.4 % of bf16 outputs over 9000 tokens round to another number than those of 32-bit weights (7.3e-4 of the
+// result), with two 0.14 %.  That costs 1.5 us where rows are few (32 behind 8192 tokens 25.4 > 26.9) and a quarter of the tile kernel's time
+// (24 x 5 behind 32768 in bf16 89 > 117, four prompts of 70 behind 4096 46 > 53.5).
 template <int TYPE, bool SHARED> struct WeightTerms { static constexpr int value = TYPE == BIQ_BF16 && !SHARED ? 1 : 2; };
 
 template <int TERMS>
@@ -200,8 +200,10 @@ __device__ __forceinline__ RowPlace row_place(const AttendParams& p, RowRange ra
 //
 // Sharing divides the cache's reads by the sequences, and makes one large product of their small ones, which bounds it: 24 sequences of 5 rows,
 // 32 / 8 heads of 128, fp32, behind 32768 shared tokens take 128 us for the shared part (matrix cores busy 42 % of it, in two terms, vector
-// instructions 39 %), 15.5 for the own, 8.7 for the join.  32 single rows in bfloat16 behind 8192 tokens (52 MB) take 25.3 + 4.9 us: 12 waves a CU,
-// each with a chain of loads (page, codes, rows) of 9 us around its steps.
+// instructions 39 %), 15.5 for the own, 8.7 for the join.  32 single rows in bfloat16 behind 8192 tokens (52 MB) take 27 + 4.7 us: three workgroups
+// a CU, of which its registers hold two at a time, each with a chain of loads (page, codes, rows) of 9 us around its steps.
+// All shared tokens are read whatever the window is: behind 32768 with a window of 1024 four sequences take 21.5 us a call and 32 take
+// 66 where biq_attention takes 11.4 and 13.9.
 // The kernels are those of other calls, in a second form: registers of the first stay what they were.
 
 // Sequence of row r of the call, -1 if it has none: the last one that begins at r or before.  All lanes of a wave take part, each

@@ -6,7 +6,8 @@
 // of codes, then the bfloat16 scales [rows / 4][128 / group][4].  Lane l of a wave takes the l-th 16 bytes: row l % 16, and of each of
 // the four spans of 32 elements the 8 from 8 (l / 16) on (a dword): the left operand of one 16 x 16 x 32 product per dword, whose
 // 32 elements belong to one group.  A dword holds code + 8 of element 2 i in its bits 4 i and of element 2 i + 1 in its bits
-// 16 + 4 i: ((w >> 4 i) & 0x000f000f) | 0x64006400 is two 16-bit floats 1024 + code + 8.
+// 16 + 4 i: ((w >> 4 i) & 0x000f000f) | 0x64006400 is two 16-bit floats 1024 + code + 8.  (Small whole numbers set under the exponent of
+// 1024 instead of converted: published for 8- and 4-bit weights in arXiv 2211.10017.)
 // What is missing of the last rows and elements has code 0 and scale 0.
 #pragma once
 
@@ -200,7 +201,8 @@ __device__ __forceinline__ int late8(int e, int n) { return n < 8 || e <= n - 8 
 
 // As terms (zeros behind the vector's end); returned is what a 1 stands for.  The 16 lanes of a block of 128 call this together:
 // 32-bit and bf16 elements are scaled by a power of two, the block's largest magnitude to [2^14, 2^15).  Elements keep 22 bits (8 of bf16), and
-// none below 2^-39 of the block's largest.
+// none below 2^-39 of the block's largest.  A third term would keep 32-bit elements whole for half as many products and operands again; two
+// leave 1.2e-7 of the result (48 vectors of 16384), the rounding of an output in 32 bits and less than a product in 32 bits loses by its sums (2.1e-6).
 template <int XT>
 __device__ __forceinline__ float operand8(const Raw8<XT>& raw, int e, int n, f16x8 (&out)[kTerms4<XT>]) {
     float x[8];
@@ -391,12 +393,12 @@ __device__ __forceinline__ void store_y4(const Gemm4Params& p, int column, int r
 // share its blocks and are joined through LDS.  Splitting blocks over waves costs a round through LDS, and pays as long as the chip is not full
 // of waves: there are twice as many splits until tiles x splits fill 2048 waves.
 //
-// The weights bound large products: 32000 x 4096 with groups of 64 (70 MB) and one vector of bfloat16 16.7 us, 4.4 TB/s as the workgroups' start (X is
-// the operand that all of it waits for) is not covered by loads; 16384 x 4096 with five vectors of codes (35 MB) 11.4 us.  One load a wave touches the
-// lines of its first four records while X is converted: a pass among others takes 15.2 us instead of 15.7, 10.4 instead of 10.8, and 5.6
-// instead of 5.5 for 4096 x 4096, whose weights the caches hold.  4096 x 4096 with one vector
-// takes 6.3 us, X, weights and join one after the other.  AHEAD records of weights are in flight: with 8 the head takes 23 us, with 2 17.4, with
-// the weights asked for before X becomes operands 19.7 (registers).
+// The weights bound large products: 32000 x 4096 with groups of 64 (70 MB) and one vector of bfloat16 takes 16.7 us from the kernel's start to its end,
+// 15.2 a call among others (whose starts and ends overlap: 4.6 TB/s); the workgroups' start (X is the operand that all of it waits for) is
+// not covered by loads.  16384 x 4096 with five vectors of codes (35 MB) 11.4 us, 10.3 a call; 4096 x 4096 with one vector 6.5 us, 5.6 a call, X, weights
+// and join one after the other.  One load a wave touches the lines of its first four records while X is converted: without, a call takes 15.7, 10.8 and
+// 5.5 us.  AHEAD records of weights are in flight: with 8 the head's kernel takes 23 us, with 2 17.4, with the weights asked for before X becomes
+// operands 19.7 (registers).
 template <int XT, int F, int G>
 __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Params p, int x_scales) {
     extern __shared__ float lds[];
@@ -434,7 +436,10 @@ __global__ __launch_bounds__(64 * kWaves4) void gemm4_few_kernel(const Gemm4Para
 // nor the lanes that read 16 vectors' meet on a bank.
 //
 // 256 rows share the conversion of X, and 32 rows a wave the reads of its operands: that costs as many instructions as unpacking the weights.  48
-// vectors of 32 bits, 4096 x 16384 with groups of 32 (37 MB, 6.4 GFLOP counted once): 23 us and 4.8 for the join, 95 with the kernel of few vectors.
+// vectors of 32 bits, 4096 x 16384 with groups of 32 (37 MB, 6.4 GFLOP counted once): 22.8 us and 4.6 for the join, 24.7 a call among others (the
+// join's start lies within the products' end); 95 with the kernel of few vectors.  64 vectors are what registers hold of sums and operands (up to 229
+// of a wave's 256); more of them read and unpack the weights again for each 64.  4096 x 4096 in bfloat16: 64 vectors 14.4 us, 128 17.0, 512 34 (503 TFLOP/s),
+// 2048 109 (628); int8 codes 14.1, 16.6, 32, 98 (699); 32 bits 16.6, 20.1, 47, 163 (422).
 // A SIMD's vector instructions (3300 a wave: unpacking, X's terms, both scales every 32 elements) and its products (6100 cycles a wave, two
 // terms) add up; memory waits 30 % of the time.  Requests fenced against the compiler's order gave nothing and spilt registers at groups of 32.
 constexpr int kRows4 = 32 * kWaves4;

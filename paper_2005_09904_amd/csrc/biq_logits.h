@@ -8,9 +8,9 @@
 // needs the whole row: of spans, a first launch leaves the largest logit and the sum of exponentials, the second computes the logits again
 // and writes; nothing that is rounded is stored between them.
 //
-// Many rows are bound by instructions, then by what is written: 32 sequences of 5 rows of 120011, bfloat16 to float (118 MB), 26.5 us
-// for the sums (1.4 TB/s read; half of a SIMD's time goes to vector instructions, 1130 a wave) and 31.6 for the probabilities (3.7 TB/s
-// read and written).  A few rows are two launches of dependent loads (lengths, tokens, counts, logits): one of 32000 4.2 and 5.1 us.
+// Many rows are bound by instructions, then by what is written: 32 sequences of 5 rows of 120011, bfloat16 to float (118 MB), 26.9 us
+// for the sums (1.4 TB/s read; half of a SIMD's time goes to vector instructions, 1160 a wave) and 31.9 for the probabilities (3.7 TB/s
+// read and written).  A few rows are two launches of dependent loads (lengths, tokens, counts, logits): one of 32000 5.0 and 5.3 us.
 #pragma once
 
 #include "biq_norm.h"

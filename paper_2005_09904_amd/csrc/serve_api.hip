@@ -173,6 +173,10 @@ SharedPlan shared_plan(const biq_attention_shared_args& args) {
     const long long own_rows = static_cast<long long>(a.ragged.max_rows) * group;
     const bool joint = own_rows <= 16 && rows <= 128 && c.heads * ((rows + 31) / 32) * steps <= 40 * kCus;
     const int few = rows <= 16 || ch > 1 || joint ? 16 : 32, many = ch <= 1 ? 128 : 64;
+    // Pieces of 4 steps at least (8 for the kernel for many rows), 32 at most of the shared tokens, 16 of the own ones.  Least: 4 behind 512 tokens 10.1
+    // us with 4, 10.3 with 2, 11.5 with 8; one head and 8 sequences behind 32768 22.8, 23.5, 22.6 (own tokens); four prompts of 70 behind 4096 59.6
+    // with 8, 59.4 with 4, 65.0 with 16, two of 128 behind 16384 54.4, 54.3, 50.4.  Most: one head and 8 sequences behind 32768 22.8 with 32,
+    // 26.9 with 16, 24.0 with 48; two sequences of 30000 own tokens 16.3 with 16, 19.9 with 8, 17.5 with 32.
     auto pieces = [](long long units, long long places, long long steps, long long least, long long most) {
         long long n = units >= places ? 1 : places / units;
         n = n > (steps + least - 1) / least ? (steps + least - 1) / least : n;

@@ -95,7 +95,9 @@ Gemm4Plan gemm4_plan(const biq_gemm4_args& a) {
 // Whether workgroups hold whole rows (1024 threads with up to 32 tokens each, whose counts and biases take 4 bytes of LDS each) in one launch,
 // or spans in two.  Up to 16384 tokens a workgroup is quicker: one row of 8000 6.6 us instead of 9.6, of 16000 9.2 and 10.0 with
 // the second launch's own time not counted.  Beyond, one row of 32000 takes 13.1 us and 10.4, so that it is left to spans until the
-// sequences fill half of the CUs (256 of them: 22.7 and 36.6; 64 with four rows each 44.8 and 27).
+// sequences fill half of the CUs (256 of them: 22.7 and 36.6; 64 with four rows each 44.8 and 27).  A workgroup's rows follow one another: 5 rows
+// of 8000 take 15.0 us instead of 18.4, of 2000 11.0 instead of 18.5, but 5 of 12000 20.6 and 18.5, of 16000 21.9 and 18.5 (64 rows: 215 and 153).
+// Callers hold no workspace for these, so they stay.
 bool logits_whole(int vocab, bool biases, int seqs) { return vocab <= 16384 || (vocab <= 32768 && !biases && seqs >= 128); }
 
 }  // namespace

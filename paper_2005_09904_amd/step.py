@@ -1,5 +1,6 @@
 """The operators at the end of a decoder step (include/biq.h, its last part): the norm with the residual's addition, products
-with 4-bit weights, penalties and masks on logits.  Functions and Prepared* objects as in serving.py.
+with 4-bit weights, penalties and masks on logits.  Functions and Prepared* objects as in serving.py: a function looks at its
+tensors anew, 10 to 15 us of host time, where calling a prepared object takes 2.5 to 3.5.
 """
 from __future__ import annotations
 
